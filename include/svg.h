@@ -366,6 +366,143 @@ int svg_probe_mfma_bf16(int form, int32_t workgroups, int32_t iterations, const 
 int svg_probe_lds(int form, int32_t waves, int32_t iterations, void* scratch, size_t scratch_bytes,
                   void* stream);
 
+/*
+ * ==========================================================================================
+ * Around the attention: the other operators of a video transformer's layer.
+ *
+ * A layer runs its attention between a gate + residual + norm + modulation on either side and
+ * four linear projections.  The calls below work on token rows ([tokens, channels], any row
+ * stride) instead of [B,H,N,D]; the projections read and write the [B,H,N,D] tensors of the
+ * attention in place (svg_tokens_t).  As above: device pointers owned by the caller, no
+ * allocation, no host synchronisation, arguments checked on the host before anything is
+ * enqueued, graph capturable.  Calls with no rows return SVG_OK and enqueue nothing.
+ * ==========================================================================================
+ */
+enum { SVG_BF16 = 0, SVG_F16 = 1, SVG_F32 = 2 };   /* element types */
+
+/*
+ * Gate, residual, norm and modulation between two branches of a layer.  For token row m of
+ * group g and channel c
+ *     p = Post(y)                          the branch's output through its own norm
+ *     r = residual_scale x + gate[g] p     the residual stream
+ *     h = Pre(r) (1 + scale[g]) + shift[g] the next branch's input
+ * where Post and Pre are SVG_NORM_NONE, SVG_NORM_RMS (v / sqrt(mean v^2 + eps) * weight) or
+ * SVG_NORM_LAYER ((v - mean) / sqrt(var + eps) * weight + bias, biased variance) over the C
+ * channels of a row.  All arithmetic is in fp32, r and h are rounded once each, and h is taken
+ * from the unrounded r.
+ *
+ * The rows of a call may belong to several sequences with modulation tables of their own:
+ * group g holds rows group_ptr[g] to group_ptr[g + 1] - 1 (device int32 [groups + 1],
+ * ascending; the first and the last entry are taken to be 0 and rows, groups may be empty).
+ * group_ptr == NULL: groups of rows / groups rows each (rows must be a multiple).  groups ==
+ * rows gives every token its own modulation.
+ */
+typedef struct svg_gate_norm {
+  int64_t rows;                     /* token rows, 0 .. 2^31 - 64 */
+  int32_t C, groups;                /* channels, 1 .. 16384; groups >= 1 */
+  int32_t stream_type;              /* x, r, dr, dx: SVG_BF16 or SVG_F32 */
+  int32_t branch_type;              /* y, h, dy, dh: SVG_BF16 or SVG_F16 */
+  int32_t post_norm, pre_norm;      /* SVG_NORM_* */
+  float residual_scale, post_eps, eps;
+  int32_t reserved;                 /* 0 */
+  int64_t ld_x, ld_y, ld_r, ld_h;   /* row strides in elements (0: C); dx has ld_x, dr ld_r, dy ld_y, dh ld_h */
+  int64_t ld_mod;                   /* row stride of gate, scale and shift (0: C) */
+  const float *gate, *scale, *shift;            /* device [groups, C]; NULL: 1, 0, 0 */
+  const int32_t* group_ptr;                     /* device [groups + 1] or NULL */
+  const float *post_weight, *post_bias;         /* device [C]; NULL: 1, 0 (bias: layer form only) */
+  const float *weight, *bias;
+} svg_gate_norm_t;
+
+/*
+ * x  stream [rows, C];  y  branch [rows, C], or NULL (r = residual_scale x)
+ * r  stream, written, or NULL;  r == x (same stride) is allowed
+ * h  branch, written, or NULL
+ * codes, scales  the same h as a microscaled 4-bit operand (below), rounded from fp32; both or
+ *    neither; C must be a multiple of 32, and all tensors 16-byte aligned with strides that are multiples of 8
+ * At least one output.  Any other overlap of an output with a tensor: SVG_ERR_ALIAS.
+ */
+int svg_gate_norm_fwd(const svg_gate_norm_t* desc, const void* x, const void* y, void* r, void* h,
+                      void* codes, void* scales, void* stream);
+
+/* Gradients of the parameters, device fp32, written (not accumulated into); NULL: not wanted. */
+typedef struct svg_gate_norm_grads {
+  int64_t ld_mod;                               /* row stride of gate, scale and shift (0: C) */
+  float *gate, *scale, *shift;                  /* [groups, C]; an empty group's rows are zero */
+  float *post_weight, *post_bias, *weight, *bias;   /* [C] */
+} svg_gate_norm_grads_t;
+
+/*
+ * The gradients of svg_gate_norm_fwd.
+ *   r   stream [rows, C]: the stream that the forward pass wrote (its statistics are taken again)
+ *   y   branch [rows, C]: the branch's output; NULL if there was none
+ *   dr  stream [rows, C]: gradient of r from what follows, or NULL (zero)
+ *   dh  branch [rows, C]: gradient of h, or NULL (the forward pass had no h)
+ *   dx, dy  written, or NULL.  dx == dr and dy == y or dy == dh (same stride) are allowed.
+ * Sums over rows are fp32, their order depends on rows, C and groups only: results repeat bit for bit.
+ * workspace: >= svg_gate_norm_workspace_bytes(desc), 16-byte aligned.
+ */
+size_t svg_gate_norm_workspace_bytes(const svg_gate_norm_t* desc);
+int svg_gate_norm_bwd(const svg_gate_norm_t* desc, const void* r, const void* y, const void* dr, const void* dh,
+                      void* dx, void* dy, const svg_gate_norm_grads_t* grads, void* workspace,
+                      size_t workspace_bytes, void* stream);
+
+/*
+ * A matrix of B*N token rows and H*D columns: row b*N + n, column h*D + d is the element at
+ * b*stride_b + n*stride_n + h*stride_h + d.  A plain [rows, K] tensor is B = H = 1, N = rows,
+ * D = K, stride_n its row stride; the attention's [B,H,N,D] is stride_b = H*N*D, stride_h = N*D,
+ * stride_n = D.  Strides in elements, >= 0.
+ */
+typedef struct svg_tokens {
+  int64_t B, N;
+  int32_t H, D;
+  int64_t stride_b, stride_n, stride_h;
+  int32_t type;                     /* SVG_BF16, SVG_F16 or SVG_F32 */
+  int32_t reserved;                 /* 0 */
+} svg_tokens_t;
+
+/*
+ * Microscaled 4-bit floating point (OCP Microscaling Formats 1.0, MXFP4): 32 neighbouring
+ * elements of a row share a power of two 2^E, E = clamp(floor(log2 max|v|) - 2, -127, 127), held as
+ * the byte E + 127, and every element is the E2M1 value (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their
+ * negatives) nearest to v / 2^E, ties to even, at most 6 in magnitude.  A block that holds an infinity or a NaN
+ * gets the byte 255 and stands for 32 NaNs.
+ *
+ * A matrix [rows, cols] is held in operand order, the order the matrix instructions take it in:
+ *   codes   row tiles of 16 rows, in each ceil(cols / 256) * 2 column tiles of 128 columns, in each 64
+ *           pieces of 16 bytes; piece 16 g + i holds row i's columns 32 g .. 32 g + 31 of the
+ *           tile, the even column of two in the low half of a byte
+ *   scales  per row tile groups of four column tiles (the last group may be half used), in each
+ *           64 pieces of 4 bytes; byte j of piece 16 g + i belongs to piece 16 g + i of the group's column tile j
+ * Rows are padded to a multiple of 16 and columns to one of 256; the padding's codes are zero.
+ * svg_fp4_buffer_bytes(rows, cols, SVG_FP4_CODES / _SCALES): sizes (0 for sizes out of range).
+ * Buffers are 16-byte aligned.  rows 0 .. 2^31 - 64, cols 1 .. 2^20.
+ *
+ * svg_fp4_quantize    act(x) of a token matrix -> codes, scales (act in fp32, not rounded between)
+ * svg_fp4_dequantize  codes, scales -> x, rounded to x's type (exact in bf16 and fp32 but for underflow)
+ */
+enum { SVG_FP4_CODES = 0, SVG_FP4_SCALES = 1 };
+enum { SVG_ACT_NONE = 0, SVG_ACT_SILU = 1, SVG_ACT_GELU_TANH = 2 };
+size_t svg_fp4_buffer_bytes(int64_t rows, int64_t cols, int which);
+int svg_fp4_quantize(const svg_tokens_t* tokens, const void* x, int activation, void* codes, void* scales, void* stream);
+int svg_fp4_dequantize(const svg_tokens_t* tokens, const void* codes, const void* scales, void* x, void* stream);
+
+/*
+ * Linear projection of 4-bit operands on the microscaled matrix instructions:
+ *     out[m, n] = act(sum_k a[m, k] w[n, k] + bias[n])        m < M, n < N, k < K
+ * with fp32 accumulation; a is an operand [M, K], w an operand [N, K], bias device fp32 [N] or
+ * NULL.  svg_fp4_linear writes the token matrix `out` (out_desc: B*N rows = M, H*D columns = N), so a projection
+ * can write [B,H,N,D] heads directly; svg_fp4_linear_quantize writes the operand [M, N] of the
+ * next product, rounded from fp32.  K >= 1, N >= 1; results repeat bit for bit.
+ * workspace: >= svg_fp4_linear_workspace_bytes(M, N, K), 16-byte aligned; NULL where that is 0.
+ */
+size_t svg_fp4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
+int svg_fp4_linear(int64_t M, int64_t N, int64_t K, const void* a, const void* a_scales, const void* w,
+                   const void* w_scales, const float* bias, int activation, const svg_tokens_t* out_desc,
+                   void* out, void* workspace, size_t workspace_bytes, void* stream);
+int svg_fp4_linear_quantize(int64_t M, int64_t N, int64_t K, const void* a, const void* a_scales, const void* w,
+                            const void* w_scales, const float* bias, int activation, void* codes, void* scales,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -25,6 +25,9 @@ SVG_FP8_Q, SVG_FP8_K, SVG_FP8_VT, SVG_FP8_SCALES = 0, 1, 2, 3   # svg_fp8_buffer
 SVG_ATTN_QO_TOKEN_ORDER = 1          # svg_sparse_attn_fwd_ex: q read and o written in token order
 SVG_ATTN_ELEMENT_MASK = 2            # svg_sparse_attn_fwd_ex: the pattern's element mask inside every visited tile
 SVG_ATTN_KV_TOKEN_ORDER = 4          # svg_sparse_attn_fwd_ex: k, v of temporal heads stay in token order (gathered in the kernel)
+SVG_BF16, SVG_F16, SVG_F32 = 0, 1, 2                            # element types of the operators around the attention
+SVG_FP4_CODES, SVG_FP4_SCALES = 0, 1                            # svg_fp4_buffer_bytes
+SVG_ACT_NONE, SVG_ACT_SILU, SVG_ACT_GELU_TANH = 0, 1, 2
 SVG_OK = 0
 
 EXPORTS = ("svg_strerror", "svg_version", "svg_last_hip_error", "svg_workspace_bytes", "svg_profile_plan", "svg_tile_counts",
@@ -32,7 +35,10 @@ EXPORTS = ("svg_strerror", "svg_version", "svg_last_hip_error", "svg_workspace_b
            "svg_sparse_attn_fwd", "svg_sparse_attn_fwd_ex", "svg_dense_attn_fwd",
            "svg_layout_kv_temporal", "svg_sparse_attn_fwd_kv2",
            "svg_fp8_buffer_bytes", "svg_fp8_quantize", "svg_sparse_attn_fp8_fwd", "svg_qk_norm_rope",
-           "svg_probe_mfma_bf16", "svg_probe_lds")
+           "svg_probe_mfma_bf16", "svg_probe_lds",
+           "svg_gate_norm_fwd", "svg_gate_norm_workspace_bytes", "svg_gate_norm_bwd",
+           "svg_fp4_buffer_bytes", "svg_fp4_quantize", "svg_fp4_dequantize",
+           "svg_fp4_linear_workspace_bytes", "svg_fp4_linear", "svg_fp4_linear_quantize")
 
 
 class SvgShape(C.Structure):
@@ -44,6 +50,25 @@ class SvgShape(C.Structure):
     @property
     def N(self):
         return self.F * self.P + self.T
+
+
+class SvgGateNorm(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("C", C.c_int32), ("groups", C.c_int32), ("stream_type", C.c_int32),
+                ("branch_type", C.c_int32), ("post_norm", C.c_int32), ("pre_norm", C.c_int32),
+                ("residual_scale", C.c_float), ("post_eps", C.c_float), ("eps", C.c_float), ("reserved", C.c_int32),
+                ("ld_x", C.c_int64), ("ld_y", C.c_int64), ("ld_r", C.c_int64), ("ld_h", C.c_int64), ("ld_mod", C.c_int64),
+                ("gate", C.c_void_p), ("scale", C.c_void_p), ("shift", C.c_void_p), ("group_ptr", C.c_void_p),
+                ("post_weight", C.c_void_p), ("post_bias", C.c_void_p), ("weight", C.c_void_p), ("bias", C.c_void_p)]
+
+
+class SvgGateNormGrads(C.Structure):
+    _fields_ = [("ld_mod", C.c_int64), ("gate", C.c_void_p), ("scale", C.c_void_p), ("shift", C.c_void_p),
+                ("post_weight", C.c_void_p), ("post_bias", C.c_void_p), ("weight", C.c_void_p), ("bias", C.c_void_p)]
+
+
+class SvgTokens(C.Structure):
+    _fields_ = [("B", C.c_int64), ("N", C.c_int64), ("H", C.c_int32), ("D", C.c_int32), ("stride_b", C.c_int64),
+                ("stride_n", C.c_int64), ("stride_h", C.c_int64), ("type", C.c_int32), ("reserved", C.c_int32)]
 
 
 class SvgError(RuntimeError):
@@ -111,6 +136,25 @@ def lib():
         L.svg_probe_lds.argtypes = [C.c_int, C.c_int32, C.c_int32, vp, C.c_size_t, vp]
         L.svg_dense_attn_fwd.restype = C.c_int
         L.svg_dense_attn_fwd.argtypes = [sp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+        gp, tp, i64 = C.POINTER(SvgGateNorm), C.POINTER(SvgTokens), C.c_int64
+        L.svg_gate_norm_fwd.restype = C.c_int
+        L.svg_gate_norm_fwd.argtypes = [gp, vp, vp, vp, vp, vp, vp, vp]
+        L.svg_gate_norm_workspace_bytes.restype = C.c_size_t
+        L.svg_gate_norm_workspace_bytes.argtypes = [gp]
+        L.svg_gate_norm_bwd.restype = C.c_int
+        L.svg_gate_norm_bwd.argtypes = [gp, vp, vp, vp, vp, vp, vp, C.POINTER(SvgGateNormGrads), vp, C.c_size_t, vp]
+        L.svg_fp4_buffer_bytes.restype = C.c_size_t
+        L.svg_fp4_buffer_bytes.argtypes = [i64, i64, C.c_int]
+        L.svg_fp4_quantize.restype = C.c_int
+        L.svg_fp4_quantize.argtypes = [tp, vp, C.c_int, vp, vp, vp]
+        L.svg_fp4_dequantize.restype = C.c_int
+        L.svg_fp4_dequantize.argtypes = [tp, vp, vp, vp, vp]
+        L.svg_fp4_linear_workspace_bytes.restype = C.c_size_t
+        L.svg_fp4_linear_workspace_bytes.argtypes = [i64, i64, i64]
+        L.svg_fp4_linear.restype = C.c_int
+        L.svg_fp4_linear.argtypes = [i64, i64, i64, vp, vp, vp, vp, vp, C.c_int, tp, vp, vp, C.c_size_t, vp]
+        L.svg_fp4_linear_quantize.restype = C.c_int
+        L.svg_fp4_linear_quantize.argtypes = [i64, i64, i64, vp, vp, vp, vp, vp, C.c_int, vp, vp, vp, C.c_size_t, vp]
         _lib = L
     return _lib
 
@@ -291,3 +335,82 @@ def svg_probe_lds(form, waves, iterations, scratch, stream=None) -> int:
     _check(lib().svg_probe_lds(int(form), int(waves), int(iterations), _ptr(scratch),
                                scratch.numel() * scratch.element_size(), _stream(stream)), "svg_probe_lds")
     return 1024 if form in (0, 3) else 512
+
+
+# ---- around the attention ----------------------------------------------------------------------
+
+_TYPE_OF = {torch.bfloat16: SVG_BF16, torch.float16: SVG_F16, torch.float32: SVG_F32}
+
+
+def gate_norm_desc(rows, channels, groups=1, group_ptr=None, stream_type=SVG_BF16, branch_type=SVG_BF16, post_norm=SVG_NORM_NONE,
+                   pre_norm=SVG_NORM_NONE, residual_scale=1.0, post_eps=1e-6, eps=1e-6, ld_x=0, ld_y=0, ld_r=0, ld_h=0, ld_mod=0,
+                   gate=None, scale=None, shift=None, post_weight=None, post_bias=None, weight=None, bias=None) -> SvgGateNorm:
+    """The descriptor of svg_gate_norm_fwd / _bwd; tables and weights as fp32 tensors, which the caller keeps alive."""
+    return SvgGateNorm(rows, channels, groups, stream_type, branch_type, post_norm, pre_norm, residual_scale, post_eps, eps, 0,
+                       ld_x, ld_y, ld_r, ld_h, ld_mod, _ptr(gate), _ptr(scale), _ptr(shift), _ptr(group_ptr),
+                       _ptr(post_weight), _ptr(post_bias), _ptr(weight), _ptr(bias))
+
+
+def gate_norm_grads(gate=None, scale=None, shift=None, post_weight=None, post_bias=None, weight=None, bias=None,
+                    ld_mod=0) -> SvgGateNormGrads:
+    return SvgGateNormGrads(ld_mod, _ptr(gate), _ptr(scale), _ptr(shift), _ptr(post_weight), _ptr(post_bias), _ptr(weight),
+                            _ptr(bias))
+
+
+def tokens_of(x) -> SvgTokens:
+    """The token matrix of a tensor [rows, columns] or [B, H, N, D] with neighbouring last elements."""
+    if x.stride(-1) != 1 and x.shape[-1] > 1:
+        raise ValueError("the elements of a row (of a head) have to be neighbours")
+    if x.dim() == 2:
+        return SvgTokens(1, x.shape[0], 1, x.shape[1], 0, x.stride(0), 0, _TYPE_OF[x.dtype], 0)
+    if x.dim() != 4:
+        raise ValueError("a token matrix is [rows, columns] or [B, H, N, D]")
+    B, H, N, D = x.shape
+    sb, sh, sn, _ = x.stride()
+    return SvgTokens(B, N, H, D, sb, sn, sh, _TYPE_OF[x.dtype], 0)
+
+
+def svg_gate_norm_fwd(desc, x, y, r, h, codes=None, scales=None, stream=None):
+    _check(lib().svg_gate_norm_fwd(C.byref(desc), _ptr(x), _ptr(y), _ptr(r), _ptr(h), _ptr(codes), _ptr(scales), _stream(stream)),
+           "svg_gate_norm_fwd")
+
+
+def svg_gate_norm_workspace_bytes(desc) -> int:
+    return int(lib().svg_gate_norm_workspace_bytes(C.byref(desc)))
+
+
+def svg_gate_norm_bwd(desc, r, y, dr, dh, dx, dy, grads=None, workspace=None, workspace_bytes=0, stream=None):
+    _check(lib().svg_gate_norm_bwd(C.byref(desc), _ptr(r), _ptr(y), _ptr(dr), _ptr(dh), _ptr(dx), _ptr(dy),
+                                   C.byref(grads) if grads is not None else None, _ptr(workspace), int(workspace_bytes),
+                                   _stream(stream)), "svg_gate_norm_bwd")
+
+
+def svg_fp4_buffer_bytes(rows, cols, which) -> int:
+    return int(lib().svg_fp4_buffer_bytes(int(rows), int(cols), int(which)))
+
+
+def svg_fp4_quantize(tokens, x, activation, codes, scales, stream=None):
+    _check(lib().svg_fp4_quantize(C.byref(tokens), _ptr(x), int(activation), _ptr(codes), _ptr(scales), _stream(stream)),
+           "svg_fp4_quantize")
+
+
+def svg_fp4_dequantize(tokens, codes, scales, x, stream=None):
+    _check(lib().svg_fp4_dequantize(C.byref(tokens), _ptr(codes), _ptr(scales), _ptr(x), _stream(stream)), "svg_fp4_dequantize")
+
+
+def svg_fp4_linear_workspace_bytes(M, N, K) -> int:
+    return int(lib().svg_fp4_linear_workspace_bytes(int(M), int(N), int(K)))
+
+
+def svg_fp4_linear(M, N, K, a, a_scales, w, w_scales, bias, activation, out_tokens, out, workspace=None, workspace_bytes=0,
+                   stream=None):
+    _check(lib().svg_fp4_linear(M, N, K, _ptr(a), _ptr(a_scales), _ptr(w), _ptr(w_scales), _ptr(bias), int(activation),
+                                C.byref(out_tokens), _ptr(out), _ptr(workspace), int(workspace_bytes), _stream(stream)),
+           "svg_fp4_linear")
+
+
+def svg_fp4_linear_quantize(M, N, K, a, a_scales, w, w_scales, bias, activation, codes, scales, workspace=None, workspace_bytes=0,
+                            stream=None):
+    _check(lib().svg_fp4_linear_quantize(M, N, K, _ptr(a), _ptr(a_scales), _ptr(w), _ptr(w_scales), _ptr(bias), int(activation),
+                                         _ptr(codes), _ptr(scales), _ptr(workspace), int(workspace_bytes), _stream(stream)),
+           "svg_fp4_linear_quantize")

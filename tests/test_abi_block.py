@@ -1,0 +1,149 @@
+"""Refusals of the operators around the attention, on the host: nothing is enqueued, so no GPU is needed."""
+import ctypes as C
+
+import pytest
+
+import paper_2502_01776_amd as S
+from paper_2502_01776_amd import binding
+
+A, B_, X, Y, Z, W = (0x10000000 * k for k in range(1, 7))           # addresses that are never read
+
+
+def desc(**kw):
+    base = dict(rows=64, channels=256, groups=2, pre_norm=2, gate=A, scale=A, shift=A)
+    base.update(kw)
+    return S.gate_norm_desc(**base)
+
+
+def fwd(d, x=X, y=Y, r=Z, h=W, codes=None, scales=None):
+    return S.lib().svg_gate_norm_fwd(C.byref(d) if d else None, x, y, r, h, codes, scales, None)
+
+
+def test_struct_sizes():
+    assert C.sizeof(S.SvgGateNorm) == 8 + 9 * 4 + 4 + 5 * 8 + 8 * 8 and C.sizeof(S.SvgGateNormGrads) == 64 and C.sizeof(S.SvgTokens) == 56
+
+
+@pytest.mark.parametrize("bad", [dict(rows=-1), dict(channels=0), dict(groups=0), dict(stream_type=1), dict(branch_type=2), dict(post_norm=3),
+                                 dict(pre_norm=-1), dict(eps=-1.0), dict(post_eps=float("nan")), dict(ld_x=255), dict(ld_h=8), dict(ld_mod=1),
+                                 dict(groups=3), dict(gate=A + 2), dict(group_ptr=A + 1), dict(weight=A + 3), dict(ld_y=-4)])
+def test_gate_norm_descriptors(bad):
+    assert fwd(desc(**bad)) == -1
+    assert S.svg_gate_norm_workspace_bytes(desc(**bad)) == 0
+    with pytest.raises(S.SvgError):
+        S.svg_gate_norm_fwd(desc(**bad), X, Y, Z, W, stream=0)
+
+
+def test_gate_norm_arguments():
+    d = desc()
+    assert fwd(None) == -1
+    assert fwd(d, x=None) == -1
+    assert fwd(d, r=None, h=None) == -1
+    assert fwd(d, x=X + 1) == -1 and fwd(d, y=Y + 1) == -1
+    assert fwd(d, codes=A) == -1 and fwd(d, scales=A) == -1 and fwd(d, codes=A + 8, scales=B_) == -1
+    assert fwd(desc(channels=16385)) == -2 and fwd(desc(rows=2 ** 31, groups=1)) == -2
+    assert fwd(d, h=X) == -4 and fwd(d, r=Y) == -4 and fwd(d, h=Z) == -4 and fwd(d, r=X + 512) == -4
+    assert fwd(desc(ld_r=264), r=X) == -4                                # in place with another stride
+    assert fwd(d, codes=X, scales=A) == -4 and fwd(d, codes=A, scales=A + 16) == -4
+    assert fwd(desc(channels=40), codes=A, scales=B_) == -2              # not whole blocks
+    assert fwd(desc(ld_x=257), codes=A, scales=B_) == -2                 # unaligned rows
+    assert fwd(desc(rows=0)) == 0
+    d.reserved = 1
+    assert fwd(d) == -1
+
+
+def bwd(d, r=X, y=Y, dr=Z, dh=W, dx=7 * A, dy=8 * A, grads=None, ws=9 * A, n=None):
+    n = S.svg_gate_norm_workspace_bytes(d) if n is None else n
+    return S.lib().svg_gate_norm_bwd(C.byref(d), r, y, dr, dh, dx, dy, C.byref(grads) if grads else None, ws, n, None)
+
+
+def test_gate_norm_gradient_arguments():
+    d = desc()
+    n = S.svg_gate_norm_workspace_bytes(d)
+    assert n > 0
+    assert bwd(d, ws=None) == -3 and bwd(d, n=n - 1) == -3 and bwd(d, ws=9 * A + 4) == -1
+    assert bwd(d, dx=None, dy=None) == -1                                # nothing wanted
+    assert bwd(d, dr=None, dh=None) == -1                                # nothing given
+    assert bwd(d, r=None) == -1
+    assert bwd(desc(post_norm=1), y=None) == -1
+    assert bwd(d, y=None, grads=S.gate_norm_grads(gate=B_)) == -1
+    assert bwd(d, grads=S.gate_norm_grads(gate=B_ + 1)) == -1
+    assert bwd(d, grads=S.gate_norm_grads(gate=B_, ld_mod=10)) == -1
+    assert bwd(d, dx=X) == -4 and bwd(d, dy=X) == -4 and bwd(d, dx=W) == -4 and bwd(d, dy=7 * A) == -4 and bwd(d, ws=Z) == -4
+    assert bwd(desc(ld_x=264), dx=Z) == -4                               # in place with another stride
+
+
+def tokens(**kw):
+    t = dict(B=2, N=10, H=4, D=64, stride_b=2560, stride_n=64, stride_h=640, type=0, reserved=0)
+    t.update(kw)
+    return S.SvgTokens(*t.values())
+
+
+def quant(t, x=X, act=0, codes=Y, scales=Z):
+    return S.lib().svg_fp4_quantize(C.byref(t) if t else None, x, act, codes, scales, None)
+
+
+def dequant(t, x=X, codes=Y, scales=Z):
+    return S.lib().svg_fp4_dequantize(C.byref(t) if t else None, codes, scales, x, None)
+
+
+@pytest.mark.parametrize("bad", [dict(B=-1), dict(N=-2), dict(H=0), dict(D=0), dict(stride_b=-1), dict(stride_n=-64), dict(stride_h=-5),
+                                 dict(type=3), dict(type=-1), dict(reserved=1), dict(stride_n=2 ** 41)])
+def test_token_matrices(bad):
+    assert quant(tokens(**bad)) == -1 and dequant(tokens(**bad)) == -1
+
+
+def test_quantiser_arguments():
+    t = tokens()
+    assert quant(None) == -1 and dequant(None) == -1
+    assert quant(t, x=None) == -1 and quant(t, codes=None) == -1 and quant(t, scales=None) == -1 and quant(t, act=3) == -1 and quant(t, act=-1) == -1
+    assert quant(t, x=X + 1) == -1 and quant(t, codes=Y + 8) == -1 and quant(t, scales=Z + 4) == -1
+    assert quant(t, codes=X) == -4 and quant(t, scales=X) == -4 and quant(t, scales=Y) == -4 and dequant(t, codes=X) == -4
+    assert quant(tokens(B=2 ** 20, N=2 ** 20)) == -2 and quant(tokens(H=2 ** 12, D=2 ** 12)) == -2
+    assert quant(tokens(stride_b=2 ** 40, B=2 ** 22, N=1)) == -2
+    # an output whose elements share places
+    for bad in (dict(stride_n=63), dict(stride_h=0), dict(stride_b=64), dict(stride_n=64, stride_h=64)):
+        assert dequant(tokens(**bad)) == -4, bad
+    assert quant(tokens(B=0)) == 0 and quant(tokens(N=0)) == 0 and dequant(tokens(N=0)) == 0
+    assert [S.svg_fp4_buffer_bytes(*a) for a in ((16, 256, 0), (17, 257, 0), (16, 256, 1), (17, 600, 1), (0, 5, 0))] == [2048, 8192, 256, 1024, 0]
+    assert [S.svg_fp4_buffer_bytes(*a) for a in ((-1, 5, 0), (1, 0, 0), (1, 2 ** 21, 0), (2 ** 31, 5, 0), (1, 5, 2))] == [0] * 5
+
+
+def linear(M=10, N=256, K=512, a=X, as_=Y, w=Z, ws=W, bias=None, act=0, t=None, out=7 * A, workspace=None, n=0):
+    t = t or tokens(B=1, N=10, stride_n=64, stride_h=640)
+    return S.lib().svg_fp4_linear(M, N, K, a, as_, w, ws, bias, act, C.byref(t), out, workspace, n, None)
+
+
+def linear_quantize(M=10, N=256, K=512, a=X, as_=Y, w=Z, ws=W, bias=None, act=0, codes=7 * A, scales=8 * A):
+    return S.lib().svg_fp4_linear_quantize(M, N, K, a, as_, w, ws, bias, act, codes, scales, None, 0, None)
+
+
+@pytest.mark.parametrize("call", [linear, linear_quantize])
+def test_product_arguments(call):
+    for bad in (dict(M=-1), dict(N=0), dict(K=0), dict(a=None), dict(as_=None), dict(w=None), dict(ws=None), dict(a=X + 8), dict(ws=W + 4),
+                dict(bias=A + 2), dict(act=7)):
+        assert call(**bad) == -1, bad
+    for bad in (dict(M=2 ** 31), dict(N=2 ** 21), dict(K=2 ** 21)):
+        assert call(**bad) == -2, bad
+
+
+def test_product_outputs():
+    assert linear(out=None) == -1 and linear(out=7 * A + 1) == -1
+    assert linear(M=11) == -1 and linear(N=128) == -1                    # not the token matrix's rows and columns
+    assert linear(t=tokens(B=1, stride_n=32)) == -4
+    assert linear(out=X) == -4 and linear(out=W) == -4
+    assert linear_quantize(codes=None) == -1 and linear_quantize(scales=8 * A + 4) == -1
+    assert linear_quantize(codes=X) == -4 and linear_quantize(scales=7 * A) == -4 and linear_quantize(scales=Z) == -4
+    assert linear(M=0, t=tokens(B=1, N=0)) == 0 and linear_quantize(M=0) == 0
+    assert S.svg_fp4_linear_workspace_bytes(0, 5, 5) == 0 and S.svg_fp4_linear_workspace_bytes(5, 0, 5) == 0
+
+
+def test_tokens_of_tensors():
+    import torch
+    t = S.tokens_of(torch.zeros(2, 5, 7, 64, dtype=torch.bfloat16))
+    assert [t.B, t.N, t.H, t.D, t.stride_b, t.stride_n, t.stride_h, t.type] == [2, 7, 5, 64, 2240, 64, 448, S.SVG_BF16]
+    t = S.tokens_of(torch.zeros(6, 40)[:, 3:20])
+    assert [t.B, t.N, t.H, t.D, t.stride_n, t.type] == [1, 6, 1, 17, 40, S.SVG_F32]
+    for bad in (torch.zeros(4, 6).t(), torch.zeros(3), torch.zeros(2, 3, 4)):
+        with pytest.raises(ValueError):
+            S.tokens_of(bad)
+    assert binding.EXPORTS.count("svg_fp4_linear") == 1
