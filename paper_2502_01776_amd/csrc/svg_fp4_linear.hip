@@ -4,6 +4,7 @@
 // holds four neighbouring columns of one token.  Two products side by side take the 32 rows of a pair of weight tiles so that
 // the lane has eight neighbouring columns, 8 q to 8 q + 7 for the lanes of quarter q: row 8 (i / 4) + 4 t + i % 4 is row i of product t.
 // The pair is then one block of a 4-bit output, spread over the four lanes l, l^16, l^32, l^48.
+#include <algorithm>
 #include <type_traits>
 #include <utility>
 
@@ -44,6 +45,10 @@ __device__ __forceinline__ f32x4 product(i32x4 w, i32x4 a, f32x4 c, unsigned ws,
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(w), operand(a), c, 4, 4, STEP, (int)ws, STEP, (int)as);
 }
 
+template <int STEP>
+__device__ __forceinline__ void product_into(f32x4& c, i32x4 w, i32x4 a, unsigned ws, unsigned as) { c = product<STEP>(w, a, c, ws, as); }
+__device__ __forceinline__ void settled(f32x4& c) { asm volatile("" : "+a"(c)); }
+
 // The largest of x over the lanes l, l^16, l^32, l^48, in all of them.
 __device__ __forceinline__ unsigned quarter_max(unsigned x) {
   const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
@@ -60,7 +65,11 @@ __device__ __forceinline__ void each_of(F f, std::integer_sequence<int, I...>) {
 template <int N, class F>
 __device__ __forceinline__ void each(F f) { each_of(f, std::make_integer_sequence<int, N>{}); }
 
-enum Output { kAny, kVectors, kOperand };      // token matrix of any kind, of whole aligned runs of eight; a 4-bit operand
+constexpr long long kComputeUnits = 256;
+
+// The output: a token matrix of any kind; one of whole aligned runs of eight columns in which a workgroup's tile spans less than 2^30 bytes;
+// a 4-bit operand.
+enum Output { kAny, kVectors, kOperand };
 
 // The activations where the result is rounded next: base-2 exponential and reciprocal of the vector unit, a few units in the last place of fp32.
 __device__ __forceinline__ float activate_fast(float v, int activation) {
@@ -70,83 +79,122 @@ __device__ __forceinline__ float activate_fast(float v, int activation) {
   return v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u));
 }
 
-// What the columns n to n + 7 of a pair have in common for all tokens.
-template <Output OUT>
-struct Columns {
-  float bias[8];
-  int n;
-  size_t at[OUT == kAny ? 8 : 1];        // elements from a token's first
-  __device__ __forceinline__ Columns(const LinearArgs& A, int n_) : n(n_) {
+// The bias of the columns n to n + 3.
+__device__ __forceinline__ f32x4 bias_of(const LinearArgs& A, int n) {
+  f32x4 b;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) bias[e] = A.bias && n + e < A.N ? A.bias[n + e] : 0.f;
-    if constexpr (OUT != kOperand) {
+  for (int e = 0; e < 4; ++e) b[e] = A.bias && n + e < A.N ? A.bias[n + e] : 0.f;
+  return b;
+}
+
+// Elements from the output's first to token m's, and from a token's first to column n.
+__device__ __forceinline__ size_t token_at(const LinearArgs& A, long long m) {
+  const unsigned row = (unsigned)m, b = row / (unsigned)A.tok.N;
+  return (size_t)b * A.tok.sb + (size_t)(row - b * (unsigned)A.tok.N) * A.tok.sn;
+}
+__device__ __forceinline__ size_t column_at(const LinearArgs& A, int n) {
+  const unsigned h = (unsigned)n / (unsigned)A.tok.D;
+  return (size_t)h * A.tok.sh + ((unsigned)n - h * (unsigned)A.tok.D);
+}
+
+// Writes accumulators: eight columns of a token a lane, tokens 16 a tile, columns 32 a pair.  m0, n0: the first token and column of the
+// wavefront's tiles, the same in all lanes; TM, TP: their number.  Offsets inside the output are taken from a descriptor whose base is
+// the wavefront's first element, in 32 bits, and what lies outside of the output is sent behind the descriptor's end, where stores have no effect.
+template <Output OUT, int TM, int TP>
+struct Writer {
+  const LinearArgs& A;
+  const long long m0;
+  const int n0;
+  const int i, q;
+  static constexpr unsigned kOutside = 0x40000000;           // the descriptor's size: more than any tile spans
+  __amdgpu_buffer_rsrc_t rsrc, rsrc_s;
+  unsigned row[TM];                                     // bytes from the first token to this lane's of tile x
+  bool inner;                                           // all tokens and columns exist
+  long long rt0;
+
+  __device__ __forceinline__ Writer(const LinearArgs& A_, long long m0_, int n0_) : A(A_), m0(m0_), n0(n0_), i(threadIdx.x & 15), q((threadIdx.x >> 4) & 3) {
+    inner = m0 + TM * kFp4Rows <= A.M && n0 + TP * 32 <= A.N;
+    if constexpr (OUT == kVectors) {
+      const int size = type_bytes(A.tok.type);
+      const size_t first = token_at(A, min(m0, A.M - 1)) + column_at(A, min(n0, A.N - 1));
+      rsrc = __builtin_amdgcn_make_buffer_rsrc(static_cast<char*>(A.out) + first * size, 0, (int)kOutside, attn::kRsrcFlags);
+      const size_t token0 = token_at(A, min(m0, A.M - 1));
+      each<TM>([&](auto x) {
+        const long long m = m0 + x * kFp4Rows + i;
+        row[x] = m < A.M ? (unsigned)(token_at(A, m) - token0) * size : kOutside;
+      });
+    } else if constexpr (OUT == kOperand) {
+      rt0 = m0 / kFp4Rows;
+      rsrc = __builtin_amdgcn_make_buffer_rsrc(A.codes + (size_t)rt0 * A.out_tiles * 256, 0, (int)kOutside, attn::kRsrcFlags);
+      rsrc_s = __builtin_amdgcn_make_buffer_rsrc(A.scales + (size_t)rt0 * A.out_groups * 256, 0, (int)kOutside, attn::kRsrcFlags);
+    }
+  }
+
+  // the values of tile x and pair y; all 64 lanes call it together
+  template <int X, int Y>
+  __device__ __forceinline__ void write(f32x4 lo, f32x4 hi, unsigned col) const {
+    float v[8];
 #pragma unroll
-      for (int e = 0; e < (OUT == kAny ? 8 : 1); ++e) {
-        const unsigned c = (unsigned)min(n + e, A.N - 1), h = c / (unsigned)A.tok.D;
-        at[e] = (size_t)h * A.tok.sh + (c - h * (unsigned)A.tok.D);
+    for (int e = 0; e < 8; ++e) v[e] = e < 4 ? lo[e & 3] : hi[e & 3];
+    if (A.activation != SVG_ACT_NONE) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = activate_fast(v[e], A.activation);
+    }
+    const int n = n0 + Y * 32 + 8 * q;
+    if constexpr (OUT == kOperand) {
+      if (!inner) {                                     // the padding
+        const bool token = m0 + X * kFp4Rows + i < A.M;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = token && n + e < A.N ? v[e] : 0.f;
+      }
+      const unsigned s = fp4_scale(quarter_max(magnitude8(v)));
+      const unsigned c = fp4_codes8(v, s);
+      const int block = n0 / 32 + Y, ct = block >> 2, g = block & 3;
+      const bool there = rt0 + X < A.m_tiles && ct < A.out_tiles;
+      __builtin_amdgcn_raw_buffer_store_b32(c, rsrc, i * 16 + q * 4, there ? X * A.out_tiles * 1024 + ct * 1024 + g * 256 : (int)kOutside, 0);
+      __builtin_amdgcn_raw_buffer_store_b8((unsigned char)s, rsrc_s, (int)(i * 4 + (q ? kOutside : 0)),
+                                           there ? X * A.out_groups * 256 + (ct >> 2) * 256 + g * 64 + (ct & 3) : (int)kOutside, 0);
+    } else if constexpr (OUT == kVectors) {
+      // Results are read by another pass, if at all from L2's far side: not kept in L2, where they would take the operands' place.
+      constexpr int kStream = 2;
+      const int at = (int)(row[X] + col);
+      if (A.tok.type == SVG_F32) {
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(attn::u32x4, f32x4{v[0], v[1], v[2], v[3]}), rsrc, at, 0, kStream);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(attn::u32x4, f32x4{v[4], v[5], v[6], v[7]}), rsrc, at, 16, kStream);
+      } else {
+        const block_f32x8 f = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
+        const attn::u32x4 bits = A.tok.type == SVG_BF16 ? __builtin_bit_cast(attn::u32x4, __builtin_convertvector(f, block_bf16x8))
+                                                        : __builtin_bit_cast(attn::u32x4, __builtin_convertvector(f, block_f16x8));
+        __builtin_amdgcn_raw_buffer_store_b128(bits, rsrc, at, 0, kStream);
+      }
+    } else {
+      const long long m = m0 + X * kFp4Rows + i;
+      if (m >= A.M) return;
+      const size_t first = token_at(A, m);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (n + e >= A.N) continue;
+        const size_t at = first + column_at(A, n + e);
+        if (A.tok.type == SVG_BF16) store1<SVG_BF16>(A.out, at, v[e]);
+        else if (A.tok.type == SVG_F16) store1<SVG_F16>(A.out, at, v[e]);
+        else store1<SVG_F32>(A.out, at, v[e]);
       }
     }
   }
+  // bytes from the first column to this lane's of pair Y
+  template <int Y>
+  __device__ __forceinline__ unsigned column() const {
+    if constexpr (OUT != kVectors) return 0;
+    const int n = n0 + Y * 32 + 8 * q;                   // N is a multiple of 8: D is
+    return n < A.N ? (unsigned)(column_at(A, n) - column_at(A, min(n0, A.N - 1))) * type_bytes(A.tok.type) : kOutside;
+  }
+  __device__ __forceinline__ void all(const f32x4 (&acc)[TM][TP][2]) const {
+    each<TP>([&](auto y) {
+      const unsigned col = column<y>();
+      each<TM>([&](auto x) { write<x, y>(acc[x][y][0], acc[x][y][1], col); });
+    });
+  }
 };
-
-// Elements from the output's first to token m's.
-__device__ __forceinline__ size_t token_at(const LinearArgs& A, long long m) {
-  const unsigned row = (unsigned)min(m, A.M - 1), b = row / (unsigned)A.tok.N;
-  return (size_t)b * A.tok.sb + (size_t)(row - b * (unsigned)A.tok.N) * A.tok.sn;
-}
-
-// Token m's eight columns to the output.  All 64 lanes call it together.
-template <Output OUT>
-__device__ __forceinline__ void finish(const LinearArgs& A, long long m, size_t row, const Columns<OUT>& col, f32x4 lo, f32x4 hi) {
-  float v[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = (e < 4 ? lo[e & 3] : hi[e & 3]) + col.bias[e];
-  if (A.activation != SVG_ACT_NONE) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = activate_fast(v[e], A.activation);
-  }
-  const int n = col.n;
-  if constexpr (OUT == kOperand) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = m < A.M && n + e < A.N ? v[e] : 0.f;      // the padding
-    const unsigned s = fp4_scale(quarter_max(magnitude8(v)));
-    const unsigned c = fp4_codes8(v, s);
-    const long long rt = m / kFp4Rows;
-    const int i = (int)(m % kFp4Rows), ct = n / kFp4Cols, g = (n >> 5) & 3;
-    if (rt < A.m_tiles && ct < A.out_tiles) {
-      A.codes[((size_t)rt * A.out_tiles + ct) * 256 + g * 64 + i * 4 + ((n >> 3) & 3)] = c;
-      if ((n & 31) == 0) A.scales[(((size_t)rt * A.out_groups + ct / kFp4Group) * 64 + g * 16 + i) * 4 + ct % kFp4Group] = (unsigned char)s;
-    }
-  } else if constexpr (OUT == kVectors) {                   // N is a multiple of 8: D is
-    if (m >= A.M || n >= A.N) return;
-    const size_t at = row + col.at[0];
-    if (A.tok.type == SVG_BF16) store8<SVG_BF16>(A.out, at, v);
-    else if (A.tok.type == SVG_F16) store8<SVG_F16>(A.out, at, v);
-    else store8<SVG_F32>(A.out, at, v);
-  } else {
-    if (m >= A.M) return;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if (n + e >= A.N) continue;
-      const size_t at = row + col.at[e];
-      if (A.tok.type == SVG_BF16) store1<SVG_BF16>(A.out, at, v[e]);
-      else if (A.tok.type == SVG_F16) store1<SVG_F16>(A.out, at, v[e]);
-      else store1<SVG_F32>(A.out, at, v[e]);
-    }
-  }
-}
-
-// The accumulators of TM token tiles and TP pairs to the output.
-template <Output OUT, int TM, int TP>
-__device__ __forceinline__ void finish_all(const LinearArgs& A, long long m, int n, const f32x4 (&acc)[TM][TP][2]) {
-  size_t row[TM];
-  if constexpr (OUT != kOperand) each<TM>([&](auto x) { row[x] = token_at(A, m + x * kFp4Rows); });
-  else each<TM>([&](auto x) { row[x] = 0; });
-  each<TP>([&](auto y) {
-    const Columns<OUT> col(A, n + y * 32);
-    each<TM>([&](auto x) { finish<OUT>(A, m + x * kFp4Rows, row[x], col, acc[x][y][0], acc[x][y][1]); });
-  });
-}
 
 // A wavefront computes MT token tiles times NP pairs of column tiles, operands straight from memory; WK wavefronts share
 // the columns of K and add up through LDS in the order of their number.
@@ -176,7 +224,12 @@ __global__ __launch_bounds__(64 * WK) void linear_rows_kernel(LinearArgs A) {
       wp[x][t] = A.w + (size_t)tile * A.kt * kFp4Tile + piece * 16;
       wsp[x][t] = A.ws + (size_t)tile * A.kg * 64 + piece;
     }
-  f32x4 acc[MT][NP][2] = {};
+  f32x4 acc[MT][NP][2];
+  // the first of the wavefronts that share K begins with the bias
+  each<NP * 2>([&](auto n) {
+    const f32x4 b = wave % WK == 0 ? bias_of(A, (nb * NP + n / 2) * 32 + 8 * q + n % 2 * 4) : f32x4{};
+    each<MT>([&](auto x) { acc[x][n / 2][n % 2] = b; });
+  });
   for (int k = wave; k < A.kg; k += WK) {
     unsigned as[MT], ws[NP][2];
 #pragma unroll
@@ -221,189 +274,234 @@ __global__ __launch_bounds__(64 * WK) void linear_rows_kernel(LinearArgs A) {
         lo += part[w][2 * p][lane];
         hi += part[w][2 * p + 1][lane];
       }
-      const long long m = ((long long)mb * MT + p / NP) * kFp4Rows + i;
-      const Columns<OUT> col(A, (nb * NP + p % NP) * 32 + 8 * q);
-      finish<OUT>(A, m, OUT == kOperand ? 0 : token_at(A, m), col, lo, hi);
+      const Writer<OUT, 1, 1> out(A, ((long long)mb * MT + p / NP) * kFp4Rows, (nb * NP + p % NP) * 32);
+      out.template write<0, 0>(lo, hi, out.template column<0>());
     }
   } else {
-    finish_all<OUT, MT, NP>(A, (long long)mb * MT * kFp4Rows + i, nb * NP * 32 + 8 * q, acc);
+    Writer<OUT, MT, NP>(A, (long long)mb * MT * kFp4Rows, nb * NP * 32).all(acc);
   }
 }
 
 // Row of the weights' pair that lane 16 q + i gives product t.
 __device__ __forceinline__ int pair_row(int i, int t) { return 8 * (i >> 2) + 4 * t + (i & 3); }
 
-// One load of 16 bytes a lane from memory into LDS, lane l at lds_address + 16 l; as load_to_lds, which takes two at a time.
+// One load of 4 bytes a lane from memory into LDS, lane l at lds_address + 4 l; as load_to_lds, which takes two of 16 bytes.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void load_one_to_lds(const attn::u32x4 rsrc, int voffset, int soffset, unsigned lds_address) {
-  asm volatile("s_mov_b32 m0, %3\n\ts_nop 3\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds"
+__device__ __forceinline__ void load_words_to_lds(const attn::u32x4 rsrc, int voffset, int soffset, unsigned lds_address) {
+  asm volatile("s_mov_b32 m0, %3\n\ts_nop 3\n\tbuffer_load_dword %0, %1, %2 offen lds"
                :: "v"(voffset), "s"(rsrc), "s"(soffset), "s"(lds_address)
                : "memory", "m0");
 }
 #pragma clang diagnostic pop
 
-// Waits until at most N of this wavefront's loads to LDS are outstanding and its own LDS reads have arrived.
+// Waits until at most N of this wavefront's loads are outstanding and its LDS reads have arrived.
 template <int N>
 __device__ __forceinline__ void wait_stage() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory"); }
 
-// Output tiles of WM x WN wavefronts, each TM token tiles times TP pairs of column tiles, operands through LDS.
+// Output tiles of WM x WN wavefronts, each TM token tiles times TP pairs of column tiles.
 //
-// One step is one column tile of K (128 columns) of every row tile: 1 KB an operand, moved from memory straight into LDS
-// by loads of 1 KB, kStages - 1 steps ahead.  The lanes of a weight tile's load fetch the pieces in the order in which the products
-// take the rows of a pair, so every LDS read is 1 KB in one run.  The scale bytes of four steps follow as one
-// 256-byte run a row tile.
-// A token operand is read where the last product that uses its predecessor has been issued, a pair of weight operands one
-// pair ahead, so one set of token operands and two pairs of weights are all that is held beside the accumulators.  In front of the last pair of a
-// step a wavefront waits for the loads of the next step and meets the others at the barrier, which also says that everybody has
-// read the present stage; then it refills that stage.
-constexpr int kStages = 4;
-
+// A step is one column tile of K (128 columns); four steps, whose scale bytes share a word, are a group.  The token operands,
+// which the WN wavefronts of a row share, go straight from memory into LDS, a group ahead and in two halves of LDS in turn; the weight
+// operands, which are a wavefront's own, go from memory into registers, a pair where the same pair has last been used two
+// steps earlier.  So LDS carries 8 KB a wavefront and step instead of 12, and one barrier a group is enough: in front of the last pair of a
+// group a wavefront waits for the token operands of the next group and meets the others, which also says that the present
+// half has been read.  A token operand is read where the last product that uses its predecessor has been issued.
 template <int TM, int TP, int WM, int WN>
 struct TileShape {
   static constexpr int waves = WM * WN;
   static constexpr int m_tiles = TM * WM, n_tiles = 2 * TP * WN;     // row tiles of a workgroup
-  static constexpr int tiles = m_tiles + n_tiles;
-  static constexpr int loads = tiles / waves;                         // of a wavefront for one step
-  static constexpr int scale_loads = (tiles * 256 / 1024 + waves - 1) / waves;
-  static constexpr int lds = kStages * tiles * kFp4Tile + tiles * 256;
-  static_assert(tiles % (2 * waves) == 0 && (tiles * 256) % (1024 * waves) == 0, "whole loads");
+  static constexpr int share = m_tiles / waves;                       // token tiles whose loads are a wavefront's
+  static constexpr int stage = m_tiles * kFp4Tile;                    // LDS of a step's token operands
+  static constexpr int half = kFp4Group * stage + m_tiles * 256;      // of a group's, with the scale bytes
+  static constexpr int bias = 2 * half;                               // the bias of two output tiles in turn
+  static constexpr int bias_bytes = n_tiles * kFp4Rows * 4;
+  static constexpr int lds = bias + 2 * bias_bytes;
+  static constexpr int per_unit = lds <= 81920 && waves <= 4 ? 2 : 1; // workgroups of a compute unit
+  static_assert(share * waves == m_tiles && TP % 2 == 0 && bias_bytes % 256 == 0, "whole loads");
 };
 
 template <int TM, int TP, int WM, int WN, Output OUT>
-__global__ __launch_bounds__(64 * WM * WN, 1) void linear_tile_kernel(LinearArgs A, int m_blocks, int n_blocks) {
+__global__ __launch_bounds__(64 * WM * WN, (TileShape<TM, TP, WM, WN>::per_unit * WM * WN / 4)) void linear_tile_kernel(LinearArgs A, int m_blocks,
+                                                                                                                      int n_blocks) {
   using Shape = TileShape<TM, TP, WM, WN>;
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave % WM, wn = wave / WM;
   const int i = lane & 15, q = lane >> 4;
-  int mb, nb;
-  {
-    // consecutive workgroups go to the 8 XCDs in turn: each takes a run of the tiles, in groups of 4 rows of tiles
-    const int total = m_blocks * n_blocks, per = (total + 7) / 8;
-    const int xcd = blockIdx.x & 7, at = xcd * per + (int)(blockIdx.x >> 3);
-    if ((int)(blockIdx.x >> 3) >= per || at >= total) return;
-    const int group = at / (4 * n_blocks), rows = min(4, m_blocks - 4 * group), in = at - group * 4 * n_blocks;
-    mb = 4 * group + in % rows;
-    nb = in / rows;
-  }
-  // descriptors of this workgroup's row tiles; tiles behind the end of a matrix read as zeros
-  const long long m0 = (long long)mb * Shape::m_tiles, n0 = (long long)nb * Shape::n_tiles;
-  const int mv = (int)min((long long)Shape::m_tiles, A.m_tiles - m0);
-  const int nv = (int)max(0ll, min((long long)Shape::n_tiles, A.n_tiles - n0));
   const unsigned tile_bytes = (unsigned)A.kt * kFp4Tile, scale_bytes = (unsigned)A.kg * 256;
-  const bool weights = wave < Shape::waves / 2;                       // which operand this wavefront's loads fetch
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
-  constexpr int kStageBytes = Shape::tiles * kFp4Tile;
-  constexpr int kScales = kStages * kStageBytes;                      // where the scale bytes are
-  static_assert(Shape::m_tiles == Shape::n_tiles, "half of the wavefronts load each operand");
-  const int first = (wave % (Shape::waves / 2)) * Shape::loads;       // first row tile of its operand that this wavefront loads
-  const auto rsrc = weights ? buffer_words(A.w + (size_t)n0 * tile_bytes, (unsigned)nv * tile_bytes)
-                            : buffer_words(A.a + (size_t)m0 * tile_bytes, (unsigned)mv * tile_bytes);
-  const auto rsrc_s = weights ? buffer_words(A.ws + (size_t)n0 * scale_bytes / 4, (unsigned)nv * scale_bytes)
-                              : buffer_words(A.as + (size_t)m0 * scale_bytes / 4, (unsigned)mv * scale_bytes);
-  int voff[2];
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const int r = pair_row(i, t);
-    voff[t] = weights ? (r >> 4) * (int)tile_bytes + (16 * q + (r & 15)) * 16 : t * (int)tile_bytes + lane * 16;
-  }
-  // scale words of four row tiles in one load: lanes 16 t to 16 t + 15 fetch tile t's 256 bytes (the order of the pieces is put right by the reader)
-  const int voff_s = (lane >> 4) * (int)scale_bytes + (lane & 15) * 16;
-  auto load_step = [&](int k, int stage) {
-    const int past = k < A.kt ? 0 : 0x40000000;                      // behind the last step: out of range, zeros without a fetch
-#pragma unroll
-    for (int x = 0; x < Shape::loads; x += 2) {
-      const int so = (first + x) * (int)tile_bytes + k * kFp4Tile + past;
-      load_to_lds(rsrc, voff[0], voff[1], so, so,
-                  lds0 + stage * kStageBytes + (weights ? 0 : Shape::n_tiles * kFp4Tile) + (first + x) * kFp4Tile, kFp4Tile);
-    }
-  };
-  auto load_scales = [&](int g) {
-    const int past = g < A.kg ? 0 : 0x40000000;
-#pragma unroll
-    for (int x = 0; x < Shape::scale_loads; ++x) {
-      const int tile = (wave % (Shape::waves / 2)) * Shape::scale_loads * 4 + x * 4;
-      load_one_to_lds(rsrc_s, voff_s, tile * (int)scale_bytes + g * 256 + past,
-                      lds0 + kScales + (weights ? 0 : Shape::n_tiles * 256) + tile * 256);
-    }
-  };
-  // this wavefront's operands: weight tiles first, then token tiles
-  const i32x4* const wl = reinterpret_cast<const i32x4*>(lds + wn * 2 * TP * kFp4Tile) + lane;
-  const i32x4* const al = reinterpret_cast<const i32x4*>(lds + (Shape::n_tiles + wm * TM) * kFp4Tile) + lane;
-  const unsigned* wsl[2];
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const int r = pair_row(i, t);
-    wsl[t] = reinterpret_cast<const unsigned*>(lds + kScales + (wn * 2 * TP + (r >> 4)) * 256) + 16 * q + (r & 15);
-  }
-  const unsigned* const asl = reinterpret_cast<const unsigned*>(lds + kScales + (Shape::n_tiles + wm * TM) * 256) + lane;
+  // Consecutive workgroups go to the 8 XCDs in turn: each XCD takes a run of the output tiles, in groups of 4 rows of
+  // tiles, and deals them to its workgroups in turn.
+  const int total = m_blocks * n_blocks, per = (total + 7) / 8;
+  const int run_end = min(total, ((int)(blockIdx.x & 7) + 1) * per), run_step = (int)(gridDim.x >> 3);
+  int at = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
+  if (at >= run_end) return;
 
-  i32x4 wv[2][2], av[TM];
-  unsigned ws[TP][2], as[TM];
-  f32x4 acc[TM][TP][2] = {};
-  auto read_pair = [&](int stage, int y, i32x4 (&w)[2]) {
-#pragma unroll
-    for (int t = 0; t < 2; ++t) w[t] = wl[stage * (kStageBytes / 16) + (2 * y + t) * 64];
+  long long m0, n0;                     // first row tiles
+  attn::u32x4 rsrc_a, rsrc_as;
+  __amdgpu_buffer_rsrc_t rsrc_w, rsrc_ws;
+  // descriptors of the present output tile's operands; tiles behind the end of a matrix read as zeros
+  auto open_tile = [&] {
+    const int group = at / (4 * n_blocks), rows = min(4, m_blocks - 4 * group), in = at - group * 4 * n_blocks;
+    m0 = (long long)(4 * group + in % rows) * Shape::m_tiles;
+    n0 = (long long)(in / rows) * Shape::n_tiles;
+    const unsigned mv = (unsigned)min((long long)Shape::m_tiles, A.m_tiles - m0);
+    rsrc_a = buffer_words(A.a + (size_t)m0 * tile_bytes, mv * tile_bytes);
+    rsrc_as = buffer_words(A.as + (size_t)m0 * scale_bytes / 4, mv * scale_bytes);
+    const long long nw = n0 + wn * 2 * TP;                            // this wavefront's own
+    const unsigned nv = (unsigned)max(0ll, min((long long)(2 * TP), A.n_tiles - nw));
+    rsrc_w = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(A.w) + (size_t)(nv ? nw : 0) * tile_bytes, 0, (int)(nv * tile_bytes), attn::kRsrcFlags);
+    rsrc_ws = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned*>(A.ws) + (size_t)(nv ? nw : 0) * scale_bytes / 4, 0, (int)(nv * scale_bytes), attn::kRsrcFlags);
   };
-  auto read_token = [&](int stage, int x) { av[x] = al[stage * (kStageBytes / 16) + x * 64]; };
-  auto read_scales = [&] {
+  constexpr int kPast = 0x40000000;     // added to an offset: out of range, zeros without a fetch
+  // The token operands of group g, part by part (a pair of loads each), and their scale bytes.
+  const int voff_a = lane * 16, voff_s = lane * 4;
+  constexpr int kParts = Shape::share * kFp4Group / 2;
+  auto load_tokens = [&](int g, int part) {
+    const unsigned to = lds0 + (g & 1) * Shape::half;
+    int so[2];
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+      const int n = 2 * part + z, t = wave * Shape::share + n % Shape::share, k = g * kFp4Group + n / Shape::share;
+      so[z] = t * (int)tile_bytes + k * kFp4Tile + (k < A.kt ? 0 : kPast);
+    }
+    const int t = wave * Shape::share + 2 * part % Shape::share, j = 2 * part / Shape::share;
+    load_to_lds(rsrc_a, voff_a, voff_a, so[0], so[1], to + j * Shape::stage + t * kFp4Tile, Shape::share == 1 ? Shape::stage : kFp4Tile);
+  };
+  auto load_token_scales = [&](int g) {
+    const unsigned to = lds0 + (g & 1) * Shape::half + kFp4Group * Shape::stage;
+#pragma unroll
+    for (int x = 0; x < Shape::share; ++x) {
+      const int t = wave * Shape::share + x;
+      load_words_to_lds(rsrc_as, voff_s, t * (int)scale_bytes + g * 256 + (g < A.kg ? 0 : kPast), to + t * 256);
+    }
+  };
+  // the bias of the tile's columns, 64 a load; the wavefronts behind the last 64 load them again
+  const auto rsrc_b = buffer_words(A.bias ? A.bias : reinterpret_cast<const float*>(A.w), A.bias ? (unsigned)A.N * 4 : 0);
+  auto load_bias = [&](int turn) {
+    const int part = wave % (Shape::bias_bytes / 256);
+    load_words_to_lds(rsrc_b, lane * 4, (int)n0 * kFp4Rows * 4 + part * 256, lds0 + Shape::bias + turn * Shape::bias_bytes + part * 256);
+  };
+  // weights: the rows of a pair in the order of the products
+  int voff_w[2], voff_ws[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int r = pair_row(i, t);
+    voff_w[t] = (r >> 4) * (int)tile_bytes + (16 * q + (r & 15)) * 16;
+    voff_ws[t] = (r >> 4) * (int)scale_bytes + (16 * q + (r & 15)) * 4;
+  }
+  i32x4 wv[2][TP][2], av[TM];
+  unsigned ws[TP][2], ws_next[TP][2], as[TM];
+  f32x4 acc[TM][TP][2];
+  auto load_pair = [&](int k, int y, i32x4 (&w)[2]) {
+    const int so = 2 * y * (int)tile_bytes + k * kFp4Tile + (k < A.kt ? 0 : kPast);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) w[t] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc_w, voff_w[t], so, 0));
+  };
+  auto load_weight_scales = [&](int g, unsigned (&s)[TP][2]) {
 #pragma unroll
     for (int y = 0; y < TP; ++y)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) ws[y][t] = wsl[t][y * 128];
-#pragma unroll
-    for (int x = 0; x < TM; ++x) as[x] = asl[x * 64];
+      for (int t = 0; t < 2; ++t)
+        s[y][t] = __builtin_amdgcn_raw_buffer_load_b32(rsrc_ws, voff_ws[t], 2 * y * (int)scale_bytes + g * 256 + (g < A.kg ? 0 : kPast), 0);
   };
-  load_scales(0);
-  load_step(0, 0);
-  load_step(1, 1);
-  load_step(2, 2);
-  load_step(3, 3);
-  wait_stage<3 * Shape::loads>();
-  barrier_loads_done();
-  read_scales();
-  read_pair(0, 0, wv[0]);
+  auto load_first = [&](int turn) {
+    load_bias(turn);
+    load_token_scales(0);
 #pragma unroll
-  for (int x = 0; x < TM; ++x) read_token(0, x);
-  static_assert(TP % 2 == 0, "the first pair of a step is in the first register pair");
-  auto step = [&](auto j, int k, int g) {
-    constexpr int J = decltype(j)::value;
-    each<TP - 1>([&](auto yc) {
+    for (int p = 0; p < kParts; ++p) load_tokens(0, p);
+    load_weight_scales(0, ws);
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int y = 0; y < TP; ++y) load_pair(k, y, wv[k][y]);
+  };
+  auto read_token = [&](int g, int j, int x) {
+    av[x] = reinterpret_cast<const i32x4*>(lds + (g & 1) * Shape::half + j * Shape::stage + (wm * TM + x) * kFp4Tile)[lane];
+  };
+  auto read_scales = [&](int g) {
+#pragma unroll
+    for (int x = 0; x < TM; ++x)
+      as[x] = reinterpret_cast<const unsigned*>(lds + (g & 1) * Shape::half + kFp4Group * Shape::stage + (wm * TM + x) * 256)[lane];
+  };
+  auto step = [&](auto jc, int g) {
+    constexpr int J = decltype(jc)::value;
+    const int k = g * kFp4Group + J;
+    each<TP>([&](auto yc) {
       constexpr int y = decltype(yc)::value;
-      read_pair(J, y + 1, wv[(y + 1) & 1]);
+      if constexpr (J == 3 && y == TP - 1) {
+        wait_stage<2 * TP * 2>();       // everything up to the weights of the next two steps: the next group's token operands are there
+        barrier_loads_done();
+      }
+      // the next group's token operands in the first two steps
+      if constexpr (y == 0 && J == 0) load_token_scales(g + 1);
+      if constexpr (y == 0 && J < 2) {
 #pragma unroll
-      for (int x = 0; x < TM; ++x)
+        for (int p = J * ((kParts + 1) / 2); p < (J ? kParts : (kParts + 1) / 2); ++p) load_tokens(g + 1, p);
+      }
+      if constexpr (y == 0 && J == 1) load_weight_scales(g + 1, ws_next);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) acc[x][y][t] = product<J>(wv[y & 1][t], av[x], acc[x][y][t], ws[y][t], as[x]);
+      for (int x = 0; x < TM; ++x) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) acc[x][y][t] = product<J>(wv[J & 1][y][t], av[x], acc[x][y][t], ws[y][t], as[x]);
+        if constexpr (y == TP - 1) {
+          read_token(J == 3 ? g + 1 : g, (J + 1) & 3, x);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      load_pair(k + 2, y, wv[J & 1][y]);
+      __builtin_amdgcn_sched_barrier(0);
     });
-    // the loads of the two steps behind the next one, and this group's loads of the next scale bytes, may be outstanding
-    wait_stage<2 * Shape::loads + (J == 1 || J == 2 ? Shape::scale_loads : 0)>();
-    barrier_loads_done();
-    if constexpr (J == 0) load_scales(g + 1);
-    load_step(k + 4, J);
-    constexpr int y = TP - 1;
-    read_pair((J + 1) & 3, 0, wv[0]);
+    if constexpr (J == 3) {
+      read_scales(g + 1);
 #pragma unroll
-    for (int x = 0; x < TM; ++x) {
+      for (int y = 0; y < TP; ++y)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) acc[x][y][t] = product<J>(wv[1][t], av[x], acc[x][y][t], ws[y][t], as[x]);
-      read_token((J + 1) & 3, x);
+        for (int t = 0; t < 2; ++t) ws[y][t] = ws_next[y][t];
     }
-    if constexpr (J == 3) read_scales();
   };
-  for (int g = 0; g < A.kg; ++g) {
-    const int k = g * kFp4Group;
-    step(std::integral_constant<int, 0>{}, k, g);
-    step(std::integral_constant<int, 1>{}, k + 1, g);
-    if (k + 2 < A.kt) {
-      step(std::integral_constant<int, 2>{}, k + 2, g);
-      step(std::integral_constant<int, 3>{}, k + 3, g);
+  open_tile();
+  load_first(0);
+  for (int turn = 0;; turn ^= 1) {
+    wait_stage<2 * TP * 2 + TP * 2>();
+    barrier_loads_done();
+    read_scales(0);
+#pragma unroll
+    for (int x = 0; x < TM; ++x) read_token(0, 0, x);
+    // the accumulators begin with the bias
+    const float* const staged = reinterpret_cast<const float*>(lds + Shape::bias + turn * Shape::bias_bytes) + wn * TP * 32 + 8 * q;
+    each<TP * 2>([&](auto n) {
+      const f32x4 b = *reinterpret_cast<const f32x4*>(staged + n / 2 * 32 + n % 2 * 4);
+      each<TM>([&](auto x) { acc[x][n / 2][n % 2] = b; });
+    });
+    int g = 0;
+    for (; g < A.kt / kFp4Group; ++g) {
+      step(std::integral_constant<int, 0>{}, g);
+      step(std::integral_constant<int, 1>{}, g);
+      step(std::integral_constant<int, 2>{}, g);
+      step(std::integral_constant<int, 3>{}, g);
     }
+    if (A.kt % kFp4Group) {             // half a group: kt is even
+      step(std::integral_constant<int, 0>{}, g);
+      step(std::integral_constant<int, 1>{}, g);
+    }
+    // No load to LDS outlives the workgroup, and LDS is everybody's again: the next tile's first group is on its way
+    // while this one's results are written.
+    wait_stage<0>();
+    const Writer<OUT, TM, TP> out(A, (m0 + wm * TM) * kFp4Rows, ((int)n0 / 2 + wn * TP) * 32);
+    at += run_step;
+    const bool more = at < run_end;
+    if (more) {
+      barrier_loads_done();
+      open_tile();
+      load_first(turn ^ 1);
+    }
+    out.all(acc);
+    if (!more) return;
   }
-  wait_stage<0>();                      // no load to LDS outlives the workgroup
-  finish_all<OUT, TM, TP>(A, (m0 + wm * TM) * kFp4Rows + i, ((int)n0 / 2 + wn * TP) * 32 + 8 * q, acc);
 }
 
 template <int TM, int TP, int WM, int WN>
@@ -411,8 +509,8 @@ int launch_tiles(const LinearArgs& a, Output out, hipStream_t stream) {
   using Shape = TileShape<TM, TP, WM, WN>;
   const long long m_blocks = (a.m_tiles + Shape::m_tiles - 1) / Shape::m_tiles;
   const long long n_blocks = (2ll * a.n_pairs + Shape::n_tiles - 1) / Shape::n_tiles;
-  const long long blocks = (m_blocks * n_blocks + 7) / 8 * 8;
-  if (blocks > 0x7fffff) return SVG_ERR_UNSUPPORTED;
+  if (m_blocks * n_blocks > 0x7fffffff - 8) return SVG_ERR_UNSUPPORTED;
+  const long long most = kComputeUnits * Shape::per_unit, blocks = std::min(most, (m_blocks * n_blocks + 7) / 8 * 8);
   auto kernel = out == kOperand   ? linear_tile_kernel<TM, TP, WM, WN, kOperand>
                 : out == kVectors ? linear_tile_kernel<TM, TP, WM, WN, kVectors>
                                   : linear_tile_kernel<TM, TP, WM, WN, kAny>;
@@ -438,6 +536,17 @@ int launch_rows(const LinearArgs& a, Output out, hipStream_t stream) {
 }  // namespace
 
 size_t fp4_linear_workspace_bytes(long long, long long, long long) { return 0; }
+
+namespace {
+// Do the tokens of an output tile of 256 x 256 ascend in memory, and does it span less than 2^29 bytes?  (They may lie in as many batch entries.)
+bool tile_spans_little(const Tokens& t, long long M, int N) {
+  if (M > t.N && t.sb < (t.N - 1) * t.sn) return false;
+  const long long tokens = std::min<long long>(M, 256), entries = std::min<long long>((M + t.N - 1) / t.N, (tokens + t.N - 1) / t.N + 1);
+  const long long heads = std::min<long long>((N + t.D - 1) / t.D, 256 / t.D + 2);
+  const __int128 span = (__int128)(entries - 1) * t.sb + (__int128)std::min(tokens, t.N) * t.sn + (__int128)(heads - 1) * t.sh + t.D;
+  return span * 4 < (1 << 29);
+}
+}  // namespace
 
 int launch_fp4_linear(long long M, int N, int K, const void* a, const void* a_scales, const void* w, const void* w_scales,
                       const float* bias, int activation, const Tokens* tok, void* out, void* codes, void* scales, void*,
@@ -465,10 +574,10 @@ int launch_fp4_linear(long long M, int N, int K, const void* a, const void* a_sc
     A.out_tiles = (int)fp4_col_tiles(N);
     A.out_groups = (int)fp4_col_groups(N);
   }
-  const Output form = codes ? kOperand : tokens_vectors(*tok, out) ? kVectors : kAny;
+  const Output form = codes ? kOperand : tokens_vectors(*tok, out) && tile_spans_little(*tok, M, N) ? kVectors : kAny;
   if (M <= 16) return launch_rows<1, 1, 8>(A, form, stream);
   if (M <= 512) return launch_rows<4, 1, 4>(A, form, stream);
-  return launch_tiles<8, 2, 2, 4>(A, form, stream);
+  return launch_tiles<8, 2, 1, 4>(A, form, stream);
 }
 
 }  // namespace svg
