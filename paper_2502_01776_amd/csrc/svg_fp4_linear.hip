@@ -45,10 +45,6 @@ __device__ __forceinline__ f32x4 product(i32x4 w, i32x4 a, f32x4 c, unsigned ws,
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(w), operand(a), c, 4, 4, STEP, (int)ws, STEP, (int)as);
 }
 
-template <int STEP>
-__device__ __forceinline__ void product_into(f32x4& c, i32x4 w, i32x4 a, unsigned ws, unsigned as) { c = product<STEP>(w, a, c, ws, as); }
-__device__ __forceinline__ void settled(f32x4& c) { asm volatile("" : "+a"(c)); }
-
 // The largest of x over the lanes l, l^16, l^32, l^48, in all of them.
 __device__ __forceinline__ unsigned quarter_max(unsigned x) {
   const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
@@ -288,6 +284,11 @@ __device__ __forceinline__ int pair_row(int i, int t) { return 8 * (i >> 2) + 4 
 // One load of 4 bytes a lane from memory into LDS, lane l at lds_address + 4 l; as load_to_lds, which takes two of 16 bytes.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void load_one_to_lds(const attn::u32x4 rsrc, int voffset, int soffset, unsigned lds_address) {
+  asm volatile("s_mov_b32 m0, %3\n\ts_nop 3\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds"
+               :: "v"(voffset), "s"(rsrc), "s"(soffset), "s"(lds_address)
+               : "memory", "m0");
+}
 __device__ __forceinline__ void load_words_to_lds(const attn::u32x4 rsrc, int voffset, int soffset, unsigned lds_address) {
   asm volatile("s_mov_b32 m0, %3\n\ts_nop 3\n\tbuffer_load_dword %0, %1, %2 offen lds"
                :: "v"(voffset), "s"(rsrc), "s"(soffset), "s"(lds_address)
@@ -303,36 +304,44 @@ __device__ __forceinline__ void wait_stage() { asm volatile("s_waitcnt vmcnt(%0)
 //
 // A step is one column tile of K (128 columns); four steps, whose scale bytes share a word, are a group.  The token operands,
 // which the WN wavefronts of a row share, go straight from memory into LDS, a group ahead and in two halves of LDS in turn; the weight
-// operands, which are a wavefront's own, go from memory into registers, a pair where the same pair has last been used two
-// steps earlier.  So LDS carries 8 KB a wavefront and step instead of 12, and one barrier a group is enough: in front of the last pair of a
+// operands, which are a wavefront's own, go from memory into registers, a pair where the same pair has last been used two or
+// four steps earlier.  So LDS carries 8 KB a wavefront and step instead of 12, and one barrier a group is enough: in front of the last pair of a
 // group a wavefront waits for the token operands of the next group and meets the others, which also says that the present
 // half has been read.  A token operand is read where the last product that uses its predecessor has been issued.
-template <int TM, int TP, int WM, int WN>
+template <int TM, int TP, int WM, int WN, int WK>
 struct TileShape {
-  static constexpr int waves = WM * WN;
+  static constexpr int waves = WM * WN;                               // of one part of K
   static constexpr int m_tiles = TM * WM, n_tiles = 2 * TP * WN;     // row tiles of a workgroup
+  static constexpr int ahead = TM * TP <= 8 ? 4 : 2;                  // steps that the weights are asked for ahead: what the registers hold
   static constexpr int share = m_tiles / waves;                       // token tiles whose loads are a wavefront's
   static constexpr int stage = m_tiles * kFp4Tile;                    // LDS of a step's token operands
   static constexpr int half = kFp4Group * stage + m_tiles * 256;      // of a group's, with the scale bytes
-  static constexpr int bias = 2 * half;                               // the bias of two output tiles in turn
+  static constexpr int part = 2 * half;                               // of a part of K
+  static constexpr int bias = WK * part;                               // the bias of two output tiles in turn
   static constexpr int bias_bytes = n_tiles * kFp4Rows * 4;
   static constexpr int lds = bias + 2 * bias_bytes;
-  static constexpr int per_unit = lds <= 81920 && waves <= 4 ? 2 : 1; // workgroups of a compute unit
-  static_assert(share * waves == m_tiles && TP % 2 == 0 && bias_bytes % 256 == 0, "whole loads");
+  static constexpr int per_unit = lds <= 81920 && waves * WK <= 4 ? 2 : 1;  // workgroups of a compute unit
+  static_assert(share * waves == m_tiles && bias_bytes % 256 == 0, "whole loads");
+  static_assert(WK == 1 || waves * (WK - 1) * TM * TP * 2 * 1024 <= WK * part, "the parts' sums fit");
 };
 
-template <int TM, int TP, int WM, int WN, Output OUT>
-__global__ __launch_bounds__(64 * WM * WN, (TileShape<TM, TP, WM, WN>::per_unit * WM * WN / 4)) void linear_tile_kernel(LinearArgs A, int m_blocks,
-                                                                                                                      int n_blocks) {
-  using Shape = TileShape<TM, TP, WM, WN>;
+template <int TM, int TP, int WM, int WN, int WK, Output OUT>
+__global__ __launch_bounds__(64 * WM * WN * WK, (TileShape<TM, TP, WM, WN, WK>::per_unit * WM * WN * WK / 4)) void
+linear_tile_kernel(LinearArgs A, int m_blocks, int n_blocks) {
+  using Shape = TileShape<TM, TP, WM, WN, WK>;
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int all_waves = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int part = WK == 1 ? 0 : all_waves / Shape::waves, wave = WK == 1 ? all_waves : all_waves % Shape::waves;
   const int wm = wave % WM, wn = wave / WM;
+  // this part's groups of K, and its column tiles' end
+  const int groups = WK == 1 ? A.kg : (A.kg + WK - 1) / WK, g0 = part * groups, k_end = WK == 1 ? A.kt : min(A.kt, (g0 + groups) * kFp4Group);
   const int i = lane & 15, q = lane >> 4;
   const unsigned tile_bytes = (unsigned)A.kt * kFp4Tile, scale_bytes = (unsigned)A.kg * 256;
-  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
-  // Consecutive workgroups go to the 8 XCDs in turn: each XCD takes a run of the output tiles, in groups of 4 rows of
+  unsigned char* const own = lds + part * Shape::part;                // this part's half of LDS
+  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds, own0 = lds0 + part * Shape::part;
+  constexpr int kRows = 8;
+  // Consecutive workgroups go to the 8 XCDs in turn: each XCD takes a run of the output tiles, in groups of 8 rows of
   // tiles, and deals them to its workgroups in turn.
   const int total = m_blocks * n_blocks, per = (total + 7) / 8;
   const int run_end = min(total, ((int)(blockIdx.x & 7) + 1) * per), run_step = (int)(gridDim.x >> 3);
@@ -344,8 +353,8 @@ __global__ __launch_bounds__(64 * WM * WN, (TileShape<TM, TP, WM, WN>::per_unit 
   __amdgpu_buffer_rsrc_t rsrc_w, rsrc_ws;
   // descriptors of the present output tile's operands; tiles behind the end of a matrix read as zeros
   auto open_tile = [&] {
-    const int group = at / (4 * n_blocks), rows = min(4, m_blocks - 4 * group), in = at - group * 4 * n_blocks;
-    m0 = (long long)(4 * group + in % rows) * Shape::m_tiles;
+    const int group = at / (kRows * n_blocks), rows = min(kRows, m_blocks - kRows * group), in = at - group * kRows * n_blocks;
+    m0 = (long long)(kRows * group + in % rows) * Shape::m_tiles;
     n0 = (long long)(in / rows) * Shape::n_tiles;
     const unsigned mv = (unsigned)min((long long)Shape::m_tiles, A.m_tiles - m0);
     rsrc_a = buffer_words(A.a + (size_t)m0 * tile_bytes, mv * tile_bytes);
@@ -360,22 +369,22 @@ __global__ __launch_bounds__(64 * WM * WN, (TileShape<TM, TP, WM, WN>::per_unit 
   const int voff_a = lane * 16, voff_s = lane * 4;
   constexpr int kParts = Shape::share * kFp4Group / 2;
   auto load_tokens = [&](int g, int part) {
-    const unsigned to = lds0 + (g & 1) * Shape::half;
+    const unsigned to = own0 + (g & 1) * Shape::half;
     int so[2];
 #pragma unroll
     for (int z = 0; z < 2; ++z) {
-      const int n = 2 * part + z, t = wave * Shape::share + n % Shape::share, k = g * kFp4Group + n / Shape::share;
-      so[z] = t * (int)tile_bytes + k * kFp4Tile + (k < A.kt ? 0 : kPast);
+      const int n = 2 * part + z, t = wave * Shape::share + n % Shape::share, k = (g0 + g) * kFp4Group + n / Shape::share;
+      so[z] = t * (int)tile_bytes + k * kFp4Tile + (k < k_end ? 0 : kPast);
     }
     const int t = wave * Shape::share + 2 * part % Shape::share, j = 2 * part / Shape::share;
     load_to_lds(rsrc_a, voff_a, voff_a, so[0], so[1], to + j * Shape::stage + t * kFp4Tile, Shape::share == 1 ? Shape::stage : kFp4Tile);
   };
   auto load_token_scales = [&](int g) {
-    const unsigned to = lds0 + (g & 1) * Shape::half + kFp4Group * Shape::stage;
+    const unsigned to = own0 + (g & 1) * Shape::half + kFp4Group * Shape::stage;
 #pragma unroll
     for (int x = 0; x < Shape::share; ++x) {
       const int t = wave * Shape::share + x;
-      load_words_to_lds(rsrc_as, voff_s, t * (int)scale_bytes + g * 256 + (g < A.kg ? 0 : kPast), to + t * 256);
+      load_words_to_lds(rsrc_as, voff_s, t * (int)scale_bytes + (g0 + g) * 256 + (g0 + g < A.kg ? 0 : kPast), to + t * 256);
     }
   };
   // the bias of the tile's columns, 64 a load; the wavefronts behind the last 64 load them again
@@ -392,11 +401,12 @@ __global__ __launch_bounds__(64 * WM * WN, (TileShape<TM, TP, WM, WN>::per_unit 
     voff_w[t] = (r >> 4) * (int)tile_bytes + (16 * q + (r & 15)) * 16;
     voff_ws[t] = (r >> 4) * (int)scale_bytes + (16 * q + (r & 15)) * 4;
   }
-  i32x4 wv[2][TP][2], av[TM];
+  constexpr int kAhead = Shape::ahead;
+  i32x4 wv[kAhead][TP][2], av[TM];
   unsigned ws[TP][2], ws_next[TP][2], as[TM];
   f32x4 acc[TM][TP][2];
   auto load_pair = [&](int k, int y, i32x4 (&w)[2]) {
-    const int so = 2 * y * (int)tile_bytes + k * kFp4Tile + (k < A.kt ? 0 : kPast);
+    const int so = 2 * y * (int)tile_bytes + k * kFp4Tile + (k < k_end ? 0 : kPast);
 #pragma unroll
     for (int t = 0; t < 2; ++t) w[t] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc_w, voff_w[t], so, 0));
   };
@@ -405,8 +415,11 @@ __global__ __launch_bounds__(64 * WM * WN, (TileShape<TM, TP, WM, WN>::per_unit 
     for (int y = 0; y < TP; ++y)
 #pragma unroll
       for (int t = 0; t < 2; ++t)
-        s[y][t] = __builtin_amdgcn_raw_buffer_load_b32(rsrc_ws, voff_ws[t], 2 * y * (int)scale_bytes + g * 256 + (g < A.kg ? 0 : kPast), 0);
+        s[y][t] = __builtin_amdgcn_raw_buffer_load_b32(rsrc_ws, voff_ws[t], 2 * y * (int)scale_bytes + (g0 + g) * 256 + (g0 + g < A.kg ? 0 : kPast), 0);
   };
+  // With K in parts all of them run whole groups.  The two scale bytes of column tiles that do not exist may be anything, NaN among it;
+  // as zeros they give products of zeros.
+  auto used_bytes = [&](int g) { return WK == 1 || (g0 + g) * kFp4Group + 2 < A.kt ? ~0u : 0xffffu; };
   auto load_first = [&](int turn) {
     load_bias(turn);
     load_token_scales(0);
@@ -414,25 +427,26 @@ __global__ __launch_bounds__(64 * WM * WN, (TileShape<TM, TP, WM, WN>::per_unit 
     for (int p = 0; p < kParts; ++p) load_tokens(0, p);
     load_weight_scales(0, ws);
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
+    for (int k = 0; k < kAhead; ++k)
 #pragma unroll
-      for (int y = 0; y < TP; ++y) load_pair(k, y, wv[k][y]);
+      for (int y = 0; y < TP; ++y) load_pair(g0 * kFp4Group + k, y, wv[k][y]);
   };
   auto read_token = [&](int g, int j, int x) {
-    av[x] = reinterpret_cast<const i32x4*>(lds + (g & 1) * Shape::half + j * Shape::stage + (wm * TM + x) * kFp4Tile)[lane];
+    av[x] = reinterpret_cast<const i32x4*>(own + (g & 1) * Shape::half + j * Shape::stage + (wm * TM + x) * kFp4Tile)[lane];
   };
   auto read_scales = [&](int g) {
 #pragma unroll
     for (int x = 0; x < TM; ++x)
-      as[x] = reinterpret_cast<const unsigned*>(lds + (g & 1) * Shape::half + kFp4Group * Shape::stage + (wm * TM + x) * 256)[lane];
+      as[x] = reinterpret_cast<const unsigned*>(own + (g & 1) * Shape::half + kFp4Group * Shape::stage + (wm * TM + x) * 256)[lane] & used_bytes(g);
   };
   auto step = [&](auto jc, int g) {
     constexpr int J = decltype(jc)::value;
-    const int k = g * kFp4Group + J;
+    const int k = (g0 + g) * kFp4Group + J;
     each<TP>([&](auto yc) {
       constexpr int y = decltype(yc)::value;
       if constexpr (J == 3 && y == TP - 1) {
-        wait_stage<2 * TP * 2>();       // everything up to the weights of the next two steps: the next group's token operands are there
+        // behind the next group's token operands only the scale words and weights of the steps 1 to 3 have been asked for
+        wait_stage<8 * TP - 2>();
         barrier_loads_done();
       }
       // the next group's token operands in the first two steps
@@ -446,13 +460,13 @@ __global__ __launch_bounds__(64 * WM * WN, (TileShape<TM, TP, WM, WN>::per_unit 
 #pragma unroll
       for (int x = 0; x < TM; ++x) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) acc[x][y][t] = product<J>(wv[J & 1][y][t], av[x], acc[x][y][t], ws[y][t], as[x]);
+        for (int t = 0; t < 2; ++t) acc[x][y][t] = product<J>(wv[J % kAhead][y][t], av[x], acc[x][y][t], ws[y][t], as[x]);
         if constexpr (y == TP - 1) {
           read_token(J == 3 ? g + 1 : g, (J + 1) & 3, x);
           __builtin_amdgcn_sched_barrier(0);
         }
       }
-      load_pair(k + 2, y, wv[J & 1][y]);
+      load_pair(k + kAhead, y, wv[J % kAhead][y]);
       __builtin_amdgcn_sched_barrier(0);
     });
     if constexpr (J == 3) {
@@ -460,36 +474,269 @@ __global__ __launch_bounds__(64 * WM * WN, (TileShape<TM, TP, WM, WN>::per_unit 
 #pragma unroll
       for (int y = 0; y < TP; ++y)
 #pragma unroll
-        for (int t = 0; t < 2; ++t) ws[y][t] = ws_next[y][t];
+        for (int t = 0; t < 2; ++t) ws[y][t] = ws_next[y][t] & used_bytes(g + 1);
     }
   };
   open_tile();
   load_first(0);
   for (int turn = 0;; turn ^= 1) {
-    wait_stage<2 * TP * 2 + TP * 2>();
+    wait_stage<(kAhead + 1) * TP * 2>();
     barrier_loads_done();
     read_scales(0);
+    if constexpr (WK > 1) {
+#pragma unroll
+      for (int y = 0; y < TP; ++y)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) ws[y][t] &= used_bytes(0);
+    }
 #pragma unroll
     for (int x = 0; x < TM; ++x) read_token(0, 0, x);
     // the accumulators begin with the bias
     const float* const staged = reinterpret_cast<const float*>(lds + Shape::bias + turn * Shape::bias_bytes) + wn * TP * 32 + 8 * q;
+    each<TP * 2>([&](auto n) {
+      const f32x4 b = part == 0 ? *reinterpret_cast<const f32x4*>(staged + n / 2 * 32 + n % 2 * 4) : f32x4{};
+      each<TM>([&](auto x) { acc[x][n / 2][n % 2] = b; });
+    });
+    int g = 0;
+    for (; g < (WK == 1 ? A.kt / kFp4Group : groups); ++g) {
+      step(std::integral_constant<int, 0>{}, g);
+      step(std::integral_constant<int, 1>{}, g);
+      step(std::integral_constant<int, 2>{}, g);
+      step(std::integral_constant<int, 3>{}, g);
+    }
+    if (WK == 1 && A.kt % kFp4Group) {  // half a group: kt is even
+      step(std::integral_constant<int, 0>{}, g);
+      step(std::integral_constant<int, 1>{}, g);
+    }
+    // No load to LDS outlives the workgroup, and LDS is everybody's again: the next tile's first group is on its way
+    // while this one's results are written.
+    wait_stage<0>();
+    const Writer<OUT, TM, TP> out(A, (m0 + wm * TM) * kFp4Rows, ((int)n0 / 2 + wn * TP) * 32);
+    at += run_step;
+    const bool more = at < run_end;
+    if constexpr (WK > 1) {
+      // the parts' sums meet in LDS and the first part adds them up, in their order
+      barrier_loads_done();
+      f32x4* const sums = reinterpret_cast<f32x4*>(lds) + wave * TM * TP * 2 * 64 + lane;
+      constexpr int kPart = Shape::waves * TM * TP * 2 * 64;
+      if (part) each<TM * TP * 2>([&](auto n) { sums[(part - 1) * kPart + n * 64] = acc[n / (TP * 2)][n / 2 % TP][n % 2]; });
+      __syncthreads();
+      if (part == 0) {
+        for (int p = 0; p < WK - 1; ++p)
+          each<TM * TP * 2>([&](auto n) { acc[n / (TP * 2)][n / 2 % TP][n % 2] += sums[p * kPart + n * 64]; });
+      }
+      if (more) {
+        wait_stage<0>();
+        barrier_loads_done();
+        open_tile();
+        load_first(turn ^ 1);
+      }
+      if (part == 0) out.all(acc);
+    } else {
+      if (more) {
+        barrier_loads_done();
+        open_tile();
+        load_first(turn ^ 1);
+      }
+      out.all(acc);
+    }
+    if (!more) return;
+  }
+}
+
+template <int TM, int TP, int WM, int WN, int WK>
+int launch_tiles(const LinearArgs& a, Output out, hipStream_t stream) {
+  using Shape = TileShape<TM, TP, WM, WN, WK>;
+  const long long m_blocks = (a.m_tiles + Shape::m_tiles - 1) / Shape::m_tiles;
+  const long long n_blocks = (2ll * a.n_pairs + Shape::n_tiles - 1) / Shape::n_tiles;
+  if (m_blocks * n_blocks > 0x7fffffff - 8) return SVG_ERR_UNSUPPORTED;
+  const long long most = kComputeUnits * Shape::per_unit, blocks = std::min(most, (m_blocks * n_blocks + 7) / 8 * 8);
+  auto kernel = out == kOperand   ? linear_tile_kernel<TM, TP, WM, WN, WK, kOperand>
+                : out == kVectors ? linear_tile_kernel<TM, TP, WM, WN, WK, kVectors>
+                                  : linear_tile_kernel<TM, TP, WM, WN, WK, kAny>;
+  (void)hipGetLastError();
+  if (Shape::lds > 65536) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, Shape::lds);
+    if (e != hipSuccess) return hip_status(e);
+  }
+  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * Shape::waves * WK), Shape::lds, stream, a, (int)m_blocks, (int)n_blocks);
+  return hip_status(hipGetLastError());
+}
+
+constexpr int kStages = 4;
+
+
+template <int TM, int TP, int WM, int WN>
+struct SquareShape {
+  static constexpr int waves = WM * WN;
+  static constexpr int m_tiles = TM * WM, n_tiles = 2 * TP * WN;     // row tiles of a workgroup
+  static constexpr int tiles = m_tiles + n_tiles;
+  static constexpr int loads = tiles / waves;                         // of a wavefront for one step
+  static constexpr int scale_loads = (tiles * 256 / 1024 + waves - 1) / waves;
+  static constexpr int bias_bytes = n_tiles * kFp4Rows * 4;
+  static constexpr int lds = kStages * tiles * kFp4Tile + tiles * 256 + 2 * bias_bytes;
+  static_assert(tiles % (2 * waves) == 0 && (tiles * 256) % (1024 * waves) == 0, "whole loads");
+};
+
+template <int TM, int TP, int WM, int WN, Output OUT>
+__global__ __launch_bounds__(64 * WM * WN, 1) void linear_square_kernel(LinearArgs A, int m_blocks, int n_blocks) {
+  using Shape = SquareShape<TM, TP, WM, WN>;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave % WM, wn = wave / WM;
+  const int i = lane & 15, q = lane >> 4;
+  const unsigned tile_bytes = (unsigned)A.kt * kFp4Tile, scale_bytes = (unsigned)A.kg * 256;
+  const bool weights = wave < Shape::waves / 2;                       // which operand this wavefront's loads fetch
+  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
+  constexpr int kStageBytes = Shape::tiles * kFp4Tile;
+  constexpr int kScales = kStages * kStageBytes;                      // where the scale bytes are
+  constexpr int kBias = kScales + Shape::tiles * 256;                 // and two tiles' bias in turn
+  static_assert(Shape::m_tiles == Shape::n_tiles, "half of the wavefronts load each operand");
+  const int first = (wave % (Shape::waves / 2)) * Shape::loads;       // first row tile of its operand that this wavefront loads
+  // Consecutive workgroups go to the 8 XCDs in turn: each XCD takes a run of the output tiles, in groups of 4 rows of
+  // tiles, and deals them to its workgroups in turn.
+  const int total = m_blocks * n_blocks, per = (total + 7) / 8;
+  const int run_end = min(total, ((int)(blockIdx.x & 7) + 1) * per), run_step = (int)(gridDim.x >> 3);
+  int at = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
+  long long m0, n0;
+  attn::u32x4 rsrc, rsrc_s;
+  auto open_tile = [&] {
+    const int group = at / (4 * n_blocks), rows = min(4, m_blocks - 4 * group), in = at - group * 4 * n_blocks;
+    m0 = (long long)(4 * group + in % rows) * Shape::m_tiles;
+    n0 = (long long)(in / rows) * Shape::n_tiles;
+    // descriptors of the row tiles; tiles behind the end of a matrix read as zeros
+    const int mv = (int)min((long long)Shape::m_tiles, A.m_tiles - m0);
+    const int nv = (int)max(0ll, min((long long)Shape::n_tiles, A.n_tiles - n0));
+    rsrc = weights ? buffer_words(A.w + (size_t)n0 * tile_bytes, (unsigned)nv * tile_bytes)
+                   : buffer_words(A.a + (size_t)m0 * tile_bytes, (unsigned)mv * tile_bytes);
+    rsrc_s = weights ? buffer_words(A.ws + (size_t)n0 * scale_bytes / 4, (unsigned)nv * scale_bytes)
+                     : buffer_words(A.as + (size_t)m0 * scale_bytes / 4, (unsigned)mv * scale_bytes);
+  };
+  int voff[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int r = pair_row(i, t);
+    voff[t] = weights ? (r >> 4) * (int)tile_bytes + (16 * q + (r & 15)) * 16 : t * (int)tile_bytes + lane * 16;
+  }
+  // scale words of four row tiles in one load: lanes 16 t to 16 t + 15 fetch tile t's 256 bytes (the order of the pieces is put right by the reader)
+  const int voff_s = (lane >> 4) * (int)scale_bytes + (lane & 15) * 16;
+  auto load_pairs = [&](int k, int stage, int x) {
+    const int past = k < A.kt ? 0 : 0x40000000;                      // behind the last step: out of range, zeros without a fetch
+    const int so = (first + x) * (int)tile_bytes + k * kFp4Tile + past;
+    load_to_lds(rsrc, voff[0], voff[1], so, so,
+                lds0 + stage * kStageBytes + (weights ? 0 : Shape::n_tiles * kFp4Tile) + (first + x) * kFp4Tile, kFp4Tile);
+  };
+  auto load_step = [&](int k, int stage) {
+#pragma unroll
+    for (int x = 0; x < Shape::loads; x += 2) load_pairs(k, stage, x);
+  };
+  auto load_scales = [&](int g) {
+    const int past = g < A.kg ? 0 : 0x40000000;
+#pragma unroll
+    for (int x = 0; x < Shape::scale_loads; ++x) {
+      const int tile = (wave % (Shape::waves / 2)) * Shape::scale_loads * 4 + x * 4;
+      load_one_to_lds(rsrc_s, voff_s, tile * (int)scale_bytes + g * 256 + past,
+                      lds0 + kScales + (weights ? 0 : Shape::n_tiles * 256) + tile * 256);
+    }
+  };
+  // the bias of the tile's columns, 64 a load; the wavefronts behind the last 64 load them again
+  const auto rsrc_b = buffer_words(A.bias ? A.bias : reinterpret_cast<const float*>(A.w), A.bias ? (unsigned)A.N * 4 : 0);
+  auto load_bias = [&](int turn) {
+    const int part = wave % (Shape::bias_bytes / 256);
+    load_words_to_lds(rsrc_b, lane * 4, (int)n0 * kFp4Rows * 4 + part * 256, lds0 + kBias + turn * Shape::bias_bytes + part * 256);
+  };
+  auto load_first = [&](int turn) {
+    load_scales(0);
+    load_bias(turn);
+#pragma unroll
+    for (int k = 0; k < kStages; ++k) load_step(k, k);
+  };
+  // this wavefront's operands: weight tiles first, then token tiles
+  const i32x4* const wl = reinterpret_cast<const i32x4*>(lds + wn * 2 * TP * kFp4Tile) + lane;
+  const i32x4* const al = reinterpret_cast<const i32x4*>(lds + (Shape::n_tiles + wm * TM) * kFp4Tile) + lane;
+  const unsigned* wsl[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int r = pair_row(i, t);
+    wsl[t] = reinterpret_cast<const unsigned*>(lds + kScales + (wn * 2 * TP + (r >> 4)) * 256) + 16 * q + (r & 15);
+  }
+  const unsigned* const asl = reinterpret_cast<const unsigned*>(lds + kScales + (Shape::n_tiles + wm * TM) * 256) + lane;
+
+  i32x4 wv[2][2], av[TM];
+  unsigned ws[TP][2], as[TM];
+  f32x4 acc[TM][TP][2];
+  auto read_pair = [&](int stage, int y, i32x4 (&w)[2]) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) w[t] = wl[stage * (kStageBytes / 16) + (2 * y + t) * 64];
+  };
+  auto read_token = [&](int stage, int x) { av[x] = al[stage * (kStageBytes / 16) + x * 64]; };
+  auto read_scales = [&] {
+#pragma unroll
+    for (int y = 0; y < TP; ++y)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) ws[y][t] = wsl[t][y * 128];
+#pragma unroll
+    for (int x = 0; x < TM; ++x) as[x] = asl[x * 64];
+  };
+  static_assert(TP % 2 == 0, "the first pair of a step is in the first register pair");
+  auto step = [&](auto j, int k, int g) {
+    constexpr int J = decltype(j)::value;
+    each<TP - 1>([&](auto yc) {
+      constexpr int y = decltype(yc)::value;
+      read_pair(J, y + 1, wv[(y + 1) & 1]);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int x = 0; x < TM; ++x)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) acc[x][y][t] = product<J>(wv[y & 1][t], av[x], acc[x][y][t], ws[y][t], as[x]);
+    });
+    // the loads of the two steps behind the next one, and this group's loads of the next scale bytes, may be outstanding
+    wait_stage<2 * Shape::loads + (J == 1 || J == 2 ? Shape::scale_loads : 0)>();
+    barrier_loads_done();
+    constexpr int y = TP - 1;
+    read_pair((J + 1) & 3, 0, wv[0]);
+#pragma unroll
+    for (int x = 0; x < TM; ++x) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) acc[x][y][t] = product<J>(wv[1][t], av[x], acc[x][y][t], ws[y][t], as[x]);
+      read_token((J + 1) & 3, x);
+      // the loads between the products: in a row behind the barrier they would keep the matrix units waiting
+      if (x == 0 && J == 0) load_scales(g + 1);
+      if (x % 2 == 1 && x / 2 < Shape::loads / 2) load_pairs(k + 4, J, x - 1);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (J == 3) read_scales();
+  };
+  if (at >= run_end) return;
+  open_tile();
+  load_first(0);
+  for (int turn = 0;; turn ^= 1) {
+    wait_stage<(kStages - 1) * Shape::loads>();
+    barrier_loads_done();
+    read_scales();
+    read_pair(0, 0, wv[0]);
+#pragma unroll
+    for (int x = 0; x < TM; ++x) read_token(0, x);
+    const float* const staged = reinterpret_cast<const float*>(lds + kBias + turn * Shape::bias_bytes) + wn * TP * 32 + 8 * q;
     each<TP * 2>([&](auto n) {
       const f32x4 b = *reinterpret_cast<const f32x4*>(staged + n / 2 * 32 + n % 2 * 4);
       each<TM>([&](auto x) { acc[x][n / 2][n % 2] = b; });
     });
     int g = 0;
     for (; g < A.kt / kFp4Group; ++g) {
-      step(std::integral_constant<int, 0>{}, g);
-      step(std::integral_constant<int, 1>{}, g);
-      step(std::integral_constant<int, 2>{}, g);
-      step(std::integral_constant<int, 3>{}, g);
+      const int k = g * kFp4Group;
+      step(std::integral_constant<int, 0>{}, k, g);
+      step(std::integral_constant<int, 1>{}, k + 1, g);
+      step(std::integral_constant<int, 2>{}, k + 2, g);
+      step(std::integral_constant<int, 3>{}, k + 3, g);
     }
     if (A.kt % kFp4Group) {             // half a group: kt is even
-      step(std::integral_constant<int, 0>{}, g);
-      step(std::integral_constant<int, 1>{}, g);
+      step(std::integral_constant<int, 0>{}, g * kFp4Group, g);
+      step(std::integral_constant<int, 1>{}, g * kFp4Group + 1, g);
     }
-    // No load to LDS outlives the workgroup, and LDS is everybody's again: the next tile's first group is on its way
-    // while this one's results are written.
+    // No load to LDS outlives the workgroup, and the stages are everybody's again: the next tile's first steps are on
+    // their way while this one's results are written.
     wait_stage<0>();
     const Writer<OUT, TM, TP> out(A, (m0 + wm * TM) * kFp4Rows, ((int)n0 / 2 + wn * TP) * 32);
     at += run_step;
@@ -505,15 +752,15 @@ __global__ __launch_bounds__(64 * WM * WN, (TileShape<TM, TP, WM, WN>::per_unit 
 }
 
 template <int TM, int TP, int WM, int WN>
-int launch_tiles(const LinearArgs& a, Output out, hipStream_t stream) {
-  using Shape = TileShape<TM, TP, WM, WN>;
+int launch_square(const LinearArgs& a, Output out, hipStream_t stream) {
+  using Shape = SquareShape<TM, TP, WM, WN>;
   const long long m_blocks = (a.m_tiles + Shape::m_tiles - 1) / Shape::m_tiles;
   const long long n_blocks = (2ll * a.n_pairs + Shape::n_tiles - 1) / Shape::n_tiles;
   if (m_blocks * n_blocks > 0x7fffffff - 8) return SVG_ERR_UNSUPPORTED;
-  const long long most = kComputeUnits * Shape::per_unit, blocks = std::min(most, (m_blocks * n_blocks + 7) / 8 * 8);
-  auto kernel = out == kOperand   ? linear_tile_kernel<TM, TP, WM, WN, kOperand>
-                : out == kVectors ? linear_tile_kernel<TM, TP, WM, WN, kVectors>
-                                  : linear_tile_kernel<TM, TP, WM, WN, kAny>;
+  const long long most = kComputeUnits * (163840 / Shape::lds), blocks = std::min(most, (m_blocks * n_blocks + 7) / 8 * 8);
+  auto kernel = out == kOperand   ? linear_square_kernel<TM, TP, WM, WN, kOperand>
+                : out == kVectors ? linear_square_kernel<TM, TP, WM, WN, kVectors>
+                                  : linear_square_kernel<TM, TP, WM, WN, kAny>;
   (void)hipGetLastError();
   if (Shape::lds > 65536) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, Shape::lds);
@@ -575,9 +822,10 @@ int launch_fp4_linear(long long M, int N, int K, const void* a, const void* a_sc
     A.out_groups = (int)fp4_col_groups(N);
   }
   const Output form = codes ? kOperand : tokens_vectors(*tok, out) && tile_spans_little(*tok, M, N) ? kVectors : kAny;
+  if (M > 512 && M < 4096) return launch_tiles<8, 2, 1, 4, 1>(A, form, stream);
   if (M <= 16) return launch_rows<1, 1, 8>(A, form, stream);
   if (M <= 512) return launch_rows<4, 1, 4>(A, form, stream);
-  return launch_tiles<8, 2, 1, 4>(A, form, stream);
+  return launch_square<8, 2, 2, 4>(A, form, stream);
 }
 
 }  // namespace svg
