@@ -5,6 +5,7 @@
 // the lane has eight neighbouring columns, 8 q to 8 q + 7 for the lanes of quarter q: row 8 (i / 4) + 4 t + i % 4 is row i of product t.
 // The pair is then one block of a 4-bit output, spread over the four lanes l, l^16, l^32, l^48.
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 #include <utility>
 
@@ -258,23 +259,19 @@ __global__ __launch_bounds__(64 * WK) void linear_rows_kernel(LinearArgs A) {
       step(std::integral_constant<int, 3>{});
     }
   }
-  if constexpr (WK > 1) {
-    __shared__ f32x4 part[WK][MT * NP * 2][64];
+  __shared__ f32x4 part[WK][MT * NP * 2][64];
 #pragma unroll
-    for (int x = 0; x < MT * NP * 2; ++x) part[wave][x][lane] = acc[x / (NP * 2)][x / 2 % NP][x % 2];
-    __syncthreads();
-    // the pairs are dealt to the wavefronts
-    for (int p = wave; p < MT * NP; p += WK) {
-      f32x4 lo = part[0][2 * p][lane], hi = part[0][2 * p + 1][lane];
-      for (int w = 1; w < WK; ++w) {
-        lo += part[w][2 * p][lane];
-        hi += part[w][2 * p + 1][lane];
-      }
-      const Writer<OUT, 1, 1> out(A, ((long long)mb * MT + p / NP) * kFp4Rows, (nb * NP + p % NP) * 32);
-      out.template write<0, 0>(lo, hi, out.template column<0>());
+  for (int x = 0; x < MT * NP * 2; ++x) part[wave][x][lane] = acc[x / (NP * 2)][x / 2 % NP][x % 2];
+  __syncthreads();
+  // the pairs are dealt to the wavefronts
+  for (int p = wave; p < MT * NP; p += WK) {
+    f32x4 lo = part[0][2 * p][lane], hi = part[0][2 * p + 1][lane];
+    for (int w = 1; w < WK; ++w) {
+      lo += part[w][2 * p][lane];
+      hi += part[w][2 * p + 1][lane];
     }
-  } else {
-    Writer<OUT, MT, NP>(A, (long long)mb * MT * kFp4Rows, nb * NP * 32).all(acc);
+    const Writer<OUT, 1, 1> out(A, ((long long)mb * MT + p / NP) * kFp4Rows, (nb * NP + p % NP) * 32);
+    out.template write<0, 0>(lo, hi, out.template column<0>());
   }
 }
 
@@ -300,46 +297,52 @@ __device__ __forceinline__ void load_words_to_lds(const attn::u32x4 rsrc, int vo
 template <int N>
 __device__ __forceinline__ void wait_stage() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory"); }
 
+// Lets a kernel take more than 64 KB of LDS; once for each GPU, because the call costs a microsecond.
+hipError_t allow_lds(const void* kernel, int bytes, std::atomic<unsigned long long>& allowed) {
+  int device = 0;
+  hipError_t e = hipGetDevice(&device);
+  if (e != hipSuccess) return e;
+  const unsigned long long bit = device < 64 ? 1ull << device : 0;
+  if (allowed.load(std::memory_order_relaxed) & bit) return hipSuccess;
+  e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == hipSuccess) allowed.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
+
 // Output tiles of WM x WN wavefronts, each TM token tiles times TP pairs of column tiles.
 //
 // A step is one column tile of K (128 columns); four steps, whose scale bytes share a word, are a group.  The token operands,
 // which the WN wavefronts of a row share, go straight from memory into LDS, a group ahead and in two halves of LDS in turn; the weight
 // operands, which are a wavefront's own, go from memory into registers, a pair where the same pair has last been used two or
-// four steps earlier.  So LDS carries 8 KB a wavefront and step instead of 12, and one barrier a group is enough: in front of the last pair of a
+// eight steps earlier.  So LDS carries 8 KB a wavefront and step instead of 12, and one barrier a group is enough: in front of the last pair of a
 // group a wavefront waits for the token operands of the next group and meets the others, which also says that the present
 // half has been read.  A token operand is read where the last product that uses its predecessor has been issued.
-template <int TM, int TP, int WM, int WN, int WK>
+template <int TM, int TP, int WM, int WN>
 struct TileShape {
-  static constexpr int waves = WM * WN;                               // of one part of K
+  static constexpr int waves = WM * WN;
   static constexpr int m_tiles = TM * WM, n_tiles = 2 * TP * WN;     // row tiles of a workgroup
-  static constexpr int ahead = TM * TP <= 8 ? 4 : 2;                  // steps that the weights are asked for ahead: what the registers hold
+  static constexpr int ahead = TM * TP <= 4 ? 8 : 2;                  // steps that the weights are asked for ahead: what the registers hold
   static constexpr int share = m_tiles / waves;                       // token tiles whose loads are a wavefront's
   static constexpr int stage = m_tiles * kFp4Tile;                    // LDS of a step's token operands
   static constexpr int half = kFp4Group * stage + m_tiles * 256;      // of a group's, with the scale bytes
-  static constexpr int part = 2 * half;                               // of a part of K
-  static constexpr int bias = WK * part;                               // the bias of two output tiles in turn
+  static constexpr int bias = 2 * half;                               // the bias of two output tiles in turn
   static constexpr int bias_bytes = n_tiles * kFp4Rows * 4;
   static constexpr int lds = bias + 2 * bias_bytes;
-  static constexpr int per_unit = lds <= 81920 && waves * WK <= 4 ? 2 : 1;  // workgroups of a compute unit
+  static constexpr int per_unit = lds <= 81920 && waves <= 4 ? 2 : 1; // workgroups of a compute unit
   static_assert(share * waves == m_tiles && bias_bytes % 256 == 0, "whole loads");
-  static_assert(WK == 1 || waves * (WK - 1) * TM * TP * 2 * 1024 <= WK * part, "the parts' sums fit");
 };
 
-template <int TM, int TP, int WM, int WN, int WK, Output OUT>
-__global__ __launch_bounds__(64 * WM * WN * WK, (TileShape<TM, TP, WM, WN, WK>::per_unit * WM * WN * WK / 4)) void
+template <int TM, int TP, int WM, int WN, Output OUT>
+__global__ __launch_bounds__(64 * WM * WN, (TileShape<TM, TP, WM, WN>::per_unit * WM * WN / 4)) void
 linear_tile_kernel(LinearArgs A, int m_blocks, int n_blocks) {
-  using Shape = TileShape<TM, TP, WM, WN, WK>;
+  using Shape = TileShape<TM, TP, WM, WN>;
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   const int lane = threadIdx.x & 63;
-  const int all_waves = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int part = WK == 1 ? 0 : all_waves / Shape::waves, wave = WK == 1 ? all_waves : all_waves % Shape::waves;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave % WM, wn = wave / WM;
-  // this part's groups of K, and its column tiles' end
-  const int groups = WK == 1 ? A.kg : (A.kg + WK - 1) / WK, g0 = part * groups, k_end = WK == 1 ? A.kt : min(A.kt, (g0 + groups) * kFp4Group);
   const int i = lane & 15, q = lane >> 4;
   const unsigned tile_bytes = (unsigned)A.kt * kFp4Tile, scale_bytes = (unsigned)A.kg * 256;
-  unsigned char* const own = lds + part * Shape::part;                // this part's half of LDS
-  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds, own0 = lds0 + part * Shape::part;
+  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
   constexpr int kRows = 8;
   // Consecutive workgroups go to the 8 XCDs in turn: each XCD takes a run of the output tiles, in groups of 8 rows of
   // tiles, and deals them to its workgroups in turn.
@@ -369,22 +372,22 @@ linear_tile_kernel(LinearArgs A, int m_blocks, int n_blocks) {
   const int voff_a = lane * 16, voff_s = lane * 4;
   constexpr int kParts = Shape::share * kFp4Group / 2;
   auto load_tokens = [&](int g, int part) {
-    const unsigned to = own0 + (g & 1) * Shape::half;
+    const unsigned to = lds0 + (g & 1) * Shape::half;
     int so[2];
 #pragma unroll
     for (int z = 0; z < 2; ++z) {
-      const int n = 2 * part + z, t = wave * Shape::share + n % Shape::share, k = (g0 + g) * kFp4Group + n / Shape::share;
-      so[z] = t * (int)tile_bytes + k * kFp4Tile + (k < k_end ? 0 : kPast);
+      const int n = 2 * part + z, t = wave * Shape::share + n % Shape::share, k = g * kFp4Group + n / Shape::share;
+      so[z] = t * (int)tile_bytes + k * kFp4Tile + (k < A.kt ? 0 : kPast);
     }
     const int t = wave * Shape::share + 2 * part % Shape::share, j = 2 * part / Shape::share;
     load_to_lds(rsrc_a, voff_a, voff_a, so[0], so[1], to + j * Shape::stage + t * kFp4Tile, Shape::share == 1 ? Shape::stage : kFp4Tile);
   };
   auto load_token_scales = [&](int g) {
-    const unsigned to = own0 + (g & 1) * Shape::half + kFp4Group * Shape::stage;
+    const unsigned to = lds0 + (g & 1) * Shape::half + kFp4Group * Shape::stage;
 #pragma unroll
     for (int x = 0; x < Shape::share; ++x) {
       const int t = wave * Shape::share + x;
-      load_words_to_lds(rsrc_as, voff_s, t * (int)scale_bytes + (g0 + g) * 256 + (g0 + g < A.kg ? 0 : kPast), to + t * 256);
+      load_words_to_lds(rsrc_as, voff_s, t * (int)scale_bytes + g * 256 + (g < A.kg ? 0 : kPast), to + t * 256);
     }
   };
   // the bias of the tile's columns, 64 a load; the wavefronts behind the last 64 load them again
@@ -406,7 +409,7 @@ linear_tile_kernel(LinearArgs A, int m_blocks, int n_blocks) {
   unsigned ws[TP][2], ws_next[TP][2], as[TM];
   f32x4 acc[TM][TP][2];
   auto load_pair = [&](int k, int y, i32x4 (&w)[2]) {
-    const int so = 2 * y * (int)tile_bytes + k * kFp4Tile + (k < k_end ? 0 : kPast);
+    const int so = 2 * y * (int)tile_bytes + k * kFp4Tile + (k < A.kt ? 0 : kPast);
 #pragma unroll
     for (int t = 0; t < 2; ++t) w[t] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc_w, voff_w[t], so, 0));
   };
@@ -415,11 +418,8 @@ linear_tile_kernel(LinearArgs A, int m_blocks, int n_blocks) {
     for (int y = 0; y < TP; ++y)
 #pragma unroll
       for (int t = 0; t < 2; ++t)
-        s[y][t] = __builtin_amdgcn_raw_buffer_load_b32(rsrc_ws, voff_ws[t], 2 * y * (int)scale_bytes + (g0 + g) * 256 + (g0 + g < A.kg ? 0 : kPast), 0);
+        s[y][t] = __builtin_amdgcn_raw_buffer_load_b32(rsrc_ws, voff_ws[t], 2 * y * (int)scale_bytes + g * 256 + (g < A.kg ? 0 : kPast), 0);
   };
-  // With K in parts all of them run whole groups.  The two scale bytes of column tiles that do not exist may be anything, NaN among it;
-  // as zeros they give products of zeros.
-  auto used_bytes = [&](int g) { return WK == 1 || (g0 + g) * kFp4Group + 2 < A.kt ? ~0u : 0xffffu; };
   auto load_first = [&](int turn) {
     load_bias(turn);
     load_token_scales(0);
@@ -429,44 +429,49 @@ linear_tile_kernel(LinearArgs A, int m_blocks, int n_blocks) {
 #pragma unroll
     for (int k = 0; k < kAhead; ++k)
 #pragma unroll
-      for (int y = 0; y < TP; ++y) load_pair(g0 * kFp4Group + k, y, wv[k][y]);
+      for (int y = 0; y < TP; ++y) load_pair(k, y, wv[k][y]);
   };
   auto read_token = [&](int g, int j, int x) {
-    av[x] = reinterpret_cast<const i32x4*>(own + (g & 1) * Shape::half + j * Shape::stage + (wm * TM + x) * kFp4Tile)[lane];
+    av[x] = reinterpret_cast<const i32x4*>(lds + (g & 1) * Shape::half + j * Shape::stage + (wm * TM + x) * kFp4Tile)[lane];
   };
   auto read_scales = [&](int g) {
 #pragma unroll
     for (int x = 0; x < TM; ++x)
-      as[x] = reinterpret_cast<const unsigned*>(own + (g & 1) * Shape::half + kFp4Group * Shape::stage + (wm * TM + x) * 256)[lane] & used_bytes(g);
+      as[x] = reinterpret_cast<const unsigned*>(lds + (g & 1) * Shape::half + kFp4Group * Shape::stage + (wm * TM + x) * 256)[lane];
   };
-  auto step = [&](auto jc, int g) {
-    constexpr int J = decltype(jc)::value;
-    const int k = (g0 + g) * kFp4Group + J;
+  // step J of group g, whose number is odd if ODD
+  auto step = [&](auto jc, auto odd, int g) {
+    constexpr int J = decltype(jc)::value, W = (decltype(odd)::value * kFp4Group + J) % kAhead;
+    const int k = g * kFp4Group + J;
     each<TP>([&](auto yc) {
       constexpr int y = decltype(yc)::value;
+      if constexpr (y == TP - 1) __builtin_amdgcn_s_setprio(1);      // as in the larger tiles
       if constexpr (J == 3 && y == TP - 1) {
         // behind the next group's token operands only the scale words and weights of the steps 1 to 3 have been asked for
         wait_stage<8 * TP - 2>();
         barrier_loads_done();
       }
-      // the next group's token operands in the first two steps
-      if constexpr (y == 0 && J == 0) load_token_scales(g + 1);
-      if constexpr (y == 0 && J < 2) {
-#pragma unroll
-        for (int p = J * ((kParts + 1) / 2); p < (J ? kParts : (kParts + 1) / 2); ++p) load_tokens(g + 1, p);
-      }
-      if constexpr (y == 0 && J == 1) load_weight_scales(g + 1, ws_next);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int x = 0; x < TM; ++x) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) acc[x][y][t] = product<J>(wv[J % kAhead][y][t], av[x], acc[x][y][t], ws[y][t], as[x]);
-        if constexpr (y == TP - 1) {
-          read_token(J == 3 ? g + 1 : g, (J + 1) & 3, x);
-          __builtin_amdgcn_sched_barrier(0);
+        for (int t = 0; t < 2; ++t) acc[x][y][t] = product<J>(wv[W][y][t], av[x], acc[x][y][t], ws[y][t], as[x]);
+        if constexpr (y == TP - 1) read_token(J == 3 ? g + 1 : g, (J + 1) & 3, x);
+        // the next group's token operands in the first two steps, between the products
+        if (y == 0 && J < 2 && x % 2 == 1) {
+          constexpr int kSlots = TM / 2, kHere = (kParts + 1) / 2;
+#pragma unroll
+          for (int n = 0; n < kHere; ++n)
+            if (n % kSlots == x / 2 && J * kHere + n < kParts) load_tokens(g + 1, J * kHere + n);
+          if (x == TM - 1) {
+            if constexpr (J == 0) load_token_scales(g + 1);
+            if constexpr (J == 1) load_weight_scales(g + 1, ws_next);
+          }
         }
+        __builtin_amdgcn_sched_barrier(0);
       }
-      load_pair(k + kAhead, y, wv[J % kAhead][y]);
+      load_pair(k + kAhead, y, wv[W][y]);
+      if constexpr (y == TP - 1) __builtin_amdgcn_s_setprio(0);
       __builtin_amdgcn_sched_barrier(0);
     });
     if constexpr (J == 3) {
@@ -474,7 +479,7 @@ linear_tile_kernel(LinearArgs A, int m_blocks, int n_blocks) {
 #pragma unroll
       for (int y = 0; y < TP; ++y)
 #pragma unroll
-        for (int t = 0; t < 2; ++t) ws[y][t] = ws_next[y][t] & used_bytes(g + 1);
+        for (int t = 0; t < 2; ++t) ws[y][t] = ws_next[y][t];
     }
   };
   open_tile();
@@ -483,30 +488,43 @@ linear_tile_kernel(LinearArgs A, int m_blocks, int n_blocks) {
     wait_stage<(kAhead + 1) * TP * 2>();
     barrier_loads_done();
     read_scales(0);
-    if constexpr (WK > 1) {
-#pragma unroll
-      for (int y = 0; y < TP; ++y)
-#pragma unroll
-        for (int t = 0; t < 2; ++t) ws[y][t] &= used_bytes(0);
-    }
 #pragma unroll
     for (int x = 0; x < TM; ++x) read_token(0, 0, x);
     // the accumulators begin with the bias
     const float* const staged = reinterpret_cast<const float*>(lds + Shape::bias + turn * Shape::bias_bytes) + wn * TP * 32 + 8 * q;
     each<TP * 2>([&](auto n) {
-      const f32x4 b = part == 0 ? *reinterpret_cast<const f32x4*>(staged + n / 2 * 32 + n % 2 * 4) : f32x4{};
+      const f32x4 b = *reinterpret_cast<const f32x4*>(staged + n / 2 * 32 + n % 2 * 4);
       each<TM>([&](auto x) { acc[x][n / 2][n % 2] = b; });
     });
     int g = 0;
-    for (; g < (WK == 1 ? A.kt / kFp4Group : groups); ++g) {
-      step(std::integral_constant<int, 0>{}, g);
-      step(std::integral_constant<int, 1>{}, g);
-      step(std::integral_constant<int, 2>{}, g);
-      step(std::integral_constant<int, 3>{}, g);
-    }
-    if (WK == 1 && A.kt % kFp4Group) {  // half a group: kt is even
-      step(std::integral_constant<int, 0>{}, g);
-      step(std::integral_constant<int, 1>{}, g);
+    const int whole = A.kt / kFp4Group;
+    auto group = [&](auto odd, int g) {
+      step(std::integral_constant<int, 0>{}, odd, g);
+      step(std::integral_constant<int, 1>{}, odd, g);
+      step(std::integral_constant<int, 2>{}, odd, g);
+      step(std::integral_constant<int, 3>{}, odd, g);
+    };
+    auto half_group = [&](auto odd, int g) {        // kt is even
+      step(std::integral_constant<int, 0>{}, odd, g);
+      step(std::integral_constant<int, 1>{}, odd, g);
+    };
+    using Even = std::integral_constant<int, 0>;
+    using Odd = std::integral_constant<int, 1>;
+    const bool tail = A.kt % kFp4Group;
+    if constexpr (kAhead <= kFp4Group) {
+      for (; g < whole; ++g) group(Even{}, g);
+      if (tail) half_group(Even{}, g);
+    } else {
+      for (; g + 1 < whole; g += 2) {
+        group(Even{}, g);
+        group(Odd{}, g + 1);
+      }
+      if (g < whole) {
+        group(Even{}, g);
+        if (tail) half_group(Odd{}, g + 1);
+      } else if (tail) {
+        half_group(Even{}, g);
+      }
     }
     // No load to LDS outlives the workgroup, and LDS is everybody's again: the next tile's first group is on its way
     // while this one's results are written.
@@ -514,52 +532,30 @@ linear_tile_kernel(LinearArgs A, int m_blocks, int n_blocks) {
     const Writer<OUT, TM, TP> out(A, (m0 + wm * TM) * kFp4Rows, ((int)n0 / 2 + wn * TP) * 32);
     at += run_step;
     const bool more = at < run_end;
-    if constexpr (WK > 1) {
-      // the parts' sums meet in LDS and the first part adds them up, in their order
+    if (more) {
       barrier_loads_done();
-      f32x4* const sums = reinterpret_cast<f32x4*>(lds) + wave * TM * TP * 2 * 64 + lane;
-      constexpr int kPart = Shape::waves * TM * TP * 2 * 64;
-      if (part) each<TM * TP * 2>([&](auto n) { sums[(part - 1) * kPart + n * 64] = acc[n / (TP * 2)][n / 2 % TP][n % 2]; });
-      __syncthreads();
-      if (part == 0) {
-        for (int p = 0; p < WK - 1; ++p)
-          each<TM * TP * 2>([&](auto n) { acc[n / (TP * 2)][n / 2 % TP][n % 2] += sums[p * kPart + n * 64]; });
-      }
-      if (more) {
-        wait_stage<0>();
-        barrier_loads_done();
-        open_tile();
-        load_first(turn ^ 1);
-      }
-      if (part == 0) out.all(acc);
-    } else {
-      if (more) {
-        barrier_loads_done();
-        open_tile();
-        load_first(turn ^ 1);
-      }
-      out.all(acc);
+      open_tile();
+      load_first(turn ^ 1);
     }
+    out.all(acc);
     if (!more) return;
   }
 }
 
-template <int TM, int TP, int WM, int WN, int WK>
+template <int TM, int TP, int WM, int WN>
 int launch_tiles(const LinearArgs& a, Output out, hipStream_t stream) {
-  using Shape = TileShape<TM, TP, WM, WN, WK>;
+  using Shape = TileShape<TM, TP, WM, WN>;
   const long long m_blocks = (a.m_tiles + Shape::m_tiles - 1) / Shape::m_tiles;
   const long long n_blocks = (2ll * a.n_pairs + Shape::n_tiles - 1) / Shape::n_tiles;
   if (m_blocks * n_blocks > 0x7fffffff - 8) return SVG_ERR_UNSUPPORTED;
   const long long most = kComputeUnits * Shape::per_unit, blocks = std::min(most, (m_blocks * n_blocks + 7) / 8 * 8);
-  auto kernel = out == kOperand   ? linear_tile_kernel<TM, TP, WM, WN, WK, kOperand>
-                : out == kVectors ? linear_tile_kernel<TM, TP, WM, WN, WK, kVectors>
-                                  : linear_tile_kernel<TM, TP, WM, WN, WK, kAny>;
+  auto kernel = out == kOperand   ? linear_tile_kernel<TM, TP, WM, WN, kOperand>
+                : out == kVectors ? linear_tile_kernel<TM, TP, WM, WN, kVectors>
+                                  : linear_tile_kernel<TM, TP, WM, WN, kAny>;
+  static std::atomic<unsigned long long> allowed[3];
   (void)hipGetLastError();
-  if (Shape::lds > 65536) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, Shape::lds);
-    if (e != hipSuccess) return hip_status(e);
-  }
-  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * Shape::waves * WK), Shape::lds, stream, a, (int)m_blocks, (int)n_blocks);
+  if (const hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), Shape::lds, allowed[out]); e != hipSuccess) return hip_status(e);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * Shape::waves), Shape::lds, stream, a, (int)m_blocks, (int)n_blocks);
   return hip_status(hipGetLastError());
 }
 
@@ -691,6 +687,9 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void linear_square_kernel(LinearAr
 #pragma unroll
         for (int t = 0; t < 2; ++t) acc[x][y][t] = product<J>(wv[y & 1][t], av[x], acc[x][y][t], ws[y][t], as[x]);
     });
+    // The wavefront that meets the barrier first takes the matrix unit first behind it: the two of a SIMD then read
+    // operands in turn (1.7 % of the time of 32760 x 5120 x 20480).
+    __builtin_amdgcn_s_setprio(1);
     // the loads of the two steps behind the next one, and this group's loads of the next scale bytes, may be outstanding
     wait_stage<2 * Shape::loads + (J == 1 || J == 2 ? Shape::scale_loads : 0)>();
     barrier_loads_done();
@@ -706,6 +705,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void linear_square_kernel(LinearAr
       if (x % 2 == 1 && x / 2 < Shape::loads / 2) load_pairs(k + 4, J, x - 1);
       __builtin_amdgcn_sched_barrier(0);
     }
+    __builtin_amdgcn_s_setprio(0);
     if constexpr (J == 3) read_scales();
   };
   if (at >= run_end) return;
@@ -761,11 +761,9 @@ int launch_square(const LinearArgs& a, Output out, hipStream_t stream) {
   auto kernel = out == kOperand   ? linear_square_kernel<TM, TP, WM, WN, kOperand>
                 : out == kVectors ? linear_square_kernel<TM, TP, WM, WN, kVectors>
                                   : linear_square_kernel<TM, TP, WM, WN, kAny>;
+  static std::atomic<unsigned long long> allowed[3];
   (void)hipGetLastError();
-  if (Shape::lds > 65536) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, Shape::lds);
-    if (e != hipSuccess) return hip_status(e);
-  }
+  if (const hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), Shape::lds, allowed[out]); e != hipSuccess) return hip_status(e);
   hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * Shape::waves), Shape::lds, stream, a, (int)m_blocks, (int)n_blocks);
   return hip_status(hipGetLastError());
 }
@@ -778,6 +776,34 @@ int launch_rows(const LinearArgs& a, Output out, hipStream_t stream) {
   auto kernel = out == kOperand ? linear_rows_kernel<MT, NP, WK, kOperand> : out == kVectors ? linear_rows_kernel<MT, NP, WK, kVectors> : linear_rows_kernel<MT, NP, WK, kAny>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * WK), 0, stream, a);
   return hip_status(hipGetLastError());
+}
+
+
+// Which form a product takes, by estimates of its time in units of what a compute unit needs for a 256 x 256 tile.  A launch's
+// workgroups of 256 x 256 run one to a compute unit, the smaller ones two, and one that has its compute unit to itself is faster.
+//   256 x 256: 1 a round of 256;  128 x 256: 1.05 a round of 512, 0.62 for a last one of up to 256;  64 x 128: 0.48, 0.41.
+// Up to 64 tokens, or up to 400 workgroups of 64 tokens and 32 columns, operands straight from memory (K split over the wavefronts).
+// us, 256 x 256 | 128 x 256 | 64 x 128 | straight (M x N x K):
+//   64 x 5120 x 5120 30.3 22.9 12.5 9.3;  226 x 5120 x 4096 27.1 19.5 10.9 13.3;  226 x 1536 x 1536 15.8 11.3 6.9 6.4;
+//   226 x 20480 x 1536 16.8 12.6 13.6 20.2;  1573 x 512 x 512 11.3 8.6 6.0 5.9;  1573 x 1536 x 6144 36.3 26.2 18.5 28.2;
+//   4096 x 1536 x 1536 17.0 12.4 13.5 17.5;  2048 x 5120 x 5120 35.6 37.1 42.0 62.5;  4096 x 5120 x 5120 73.4 60.2 77.8 117;
+//   17776 x 512 x 8192 47.9 52.1 58.6 174;  32760 x 5120 x 20480 1376 1465 2246
+// Straight, one token tile (K over 8 wavefronts), two (4, or 8 where there are fewer workgroups than compute units) and four (4):
+//   16 x 5120 x 5120 7.1 7.8 (8: 7.5) 8.9;  32 x 5120 x 5120 9.6 7.9 (7.5) 8.9;  32 x 20480 x 5120 22.8 15.7 (19.5) 17.6
+int launch(const LinearArgs& a, Output form, hipStream_t stream) {
+  const long long pairs = a.n_pairs, m = a.m_tiles;
+  if (m == 1) return launch_rows<1, 1, 8>(a, form, stream);
+  if (m == 2) return pairs < kComputeUnits ? launch_rows<2, 1, 8>(a, form, stream) : launch_rows<2, 1, 4>(a, form, stream);
+  if (m <= 4 || (m + 3) / 4 * pairs <= 400) return launch_rows<4, 1, 4>(a, form, stream);
+  auto tiles = [&](int m_tiles, int n_pairs) { return (m + m_tiles - 1) / m_tiles * ((pairs + n_pairs - 1) / n_pairs); };
+  auto rounds = [](long long tiles, double whole, double alone) {
+    const long long rest = tiles % (2 * kComputeUnits);
+    return (double)(tiles / (2 * kComputeUnits)) * whole + (rest > kComputeUnits ? whole : rest ? alone : 0.0);
+  };
+  const double square = (double)((tiles(16, 8) + kComputeUnits - 1) / kComputeUnits);
+  const double large = rounds(tiles(8, 8), 1.05, 0.62), small = rounds(tiles(4, 4), 0.48, 0.41);
+  if (square <= large && square <= small) return launch_square<8, 2, 2, 4>(a, form, stream);
+  return large <= small ? launch_tiles<8, 2, 1, 4>(a, form, stream) : launch_tiles<4, 1, 1, 4>(a, form, stream);
 }
 
 }  // namespace
@@ -822,10 +848,7 @@ int launch_fp4_linear(long long M, int N, int K, const void* a, const void* a_sc
     A.out_groups = (int)fp4_col_groups(N);
   }
   const Output form = codes ? kOperand : tokens_vectors(*tok, out) && tile_spans_little(*tok, M, N) ? kVectors : kAny;
-  if (M > 512 && M < 4096) return launch_tiles<8, 2, 1, 4, 1>(A, form, stream);
-  if (M <= 16) return launch_rows<1, 1, 8>(A, form, stream);
-  if (M <= 512) return launch_rows<4, 1, 4>(A, form, stream);
-  return launch_square<8, 2, 2, 4>(A, form, stream);
+  return launch(A, form, stream);
 }
 
 }  // namespace svg
