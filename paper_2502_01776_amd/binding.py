@@ -176,6 +176,8 @@ def _ptr(x):
     """Device (or host) address of a torch tensor / numpy array / int / None."""
     if x is None:
         return None
+    if isinstance(x, torch.Tensor):
+        return x.data_ptr()
     if isinstance(x, int):
         return x
     if isinstance(x, np.ndarray):

@@ -52,10 +52,20 @@ int launch_fp4_linear(long long M, int N, int K, const void* a, const void* a_sc
                       const float* bias, int activation, const Tokens* tok, void* out, void* codes, void* scales, void* workspace,
                       hipStream_t stream);
 
-__host__ __device__ inline int type_bytes(int type) { return type == SVG_F32 ? 4 : 2; }
+__host__ __device__ constexpr int type_bytes(int type) { return type == SVG_F32 ? 4 : 2; }
 
 // ---- device helpers -------------------------------------------------------------------------------------------------
 #if defined(__HIP_DEVICE_COMPILE__) || defined(__HIPCC__)
+
+// One load of 16 bytes a lane from memory into LDS, lane l at lds_address + 16 l; as attn::load_to_lds, which takes two at a time.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void load_one_to_lds(const block_u32x4 rsrc, int voffset, int soffset, unsigned lds_address) {
+  asm volatile("s_mov_b32 m0, %3\n\ts_nop 3\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds"
+               :: "v"(voffset), "s"(rsrc), "s"(soffset), "s"(lds_address)
+               : "memory", "m0");
+}
+#pragma clang diagnostic pop
 
 // Sum and maximum over the 64 lanes, in all of them: inside the quarters by lane moves of the vector unit, over them by swaps.
 template <class F>

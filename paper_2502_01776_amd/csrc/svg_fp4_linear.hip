@@ -281,11 +281,6 @@ __device__ __forceinline__ int pair_row(int i, int t) { return 8 * (i >> 2) + 4 
 // One load of 4 bytes a lane from memory into LDS, lane l at lds_address + 4 l; as load_to_lds, which takes two of 16 bytes.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void load_one_to_lds(const attn::u32x4 rsrc, int voffset, int soffset, unsigned lds_address) {
-  asm volatile("s_mov_b32 m0, %3\n\ts_nop 3\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds"
-               :: "v"(voffset), "s"(rsrc), "s"(soffset), "s"(lds_address)
-               : "memory", "m0");
-}
 __device__ __forceinline__ void load_words_to_lds(const attn::u32x4 rsrc, int voffset, int soffset, unsigned lds_address) {
   asm volatile("s_mov_b32 m0, %3\n\ts_nop 3\n\tbuffer_load_dword %0, %1, %2 offen lds"
                :: "v"(voffset), "s"(rsrc), "s"(soffset), "s"(lds_address)

@@ -1,15 +1,18 @@
 // Gate, residual, norm and modulation between two branches of a layer, and its gradients.  HBM-bound: the forward pass
 // reads x and y and writes r and h, the backward pass reads r, y, dr, dh and writes dx, dy; a row is read once and stays in
 // registers from its statistics to its outputs.
+#include <algorithm>
+#include <atomic>
 #include <type_traits>
 
+#include "svg_attn_common.h"
 #include "svg_block.h"
 
 namespace svg {
 
 namespace {
 
-constexpr int kMaxWaves = 8;          // wavefronts that share a row
+constexpr int kMaxWaves = 16;         // wavefronts of a workgroup
 
 struct GateNormArgs {
   long long rows;
@@ -27,14 +30,15 @@ struct GateNormArgs {
   unsigned char* scales;
   int col_tiles, col_groups;
   long long row_limit;                // rows, with a 4-bit output rounded up to whole tiles
-  int rows_per_block;
+  int strip;                          // neighbouring rows that a team takes in turn
+  int waves;                          // wavefronts of a team
   float* partial;                     // backward: [slots][4][C]
 };
 
 // The group of a row: how many of the ends group_ptr[1 .. groups-1] are not above it.  In range whatever the table holds.
 __device__ __forceinline__ int group_of(const GateNormArgs& a, long long row) {
   if (a.groups == 1) return 0;
-  if (!a.group_ptr) return (int)(row / a.group_rows);
+  if (!a.group_ptr) return (int)((unsigned)row / (unsigned)a.group_rows);
   int lo = 0, hi = a.groups - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -44,17 +48,17 @@ __device__ __forceinline__ int group_of(const GateNormArgs& a, long long row) {
   return lo;
 }
 
-// A wavefront's lanes hold VPL times eight channels of the row.  VEC: eight neighbours each; otherwise (rows that are not
-// 16-byte aligned) neighbours are in neighbouring lanes.
-template <int VPL, bool VEC>
+// ---------------------------------------------------------------------------------------------------------------------
+// Rows of any alignment: a workgroup holds a row, neighbouring channels in neighbouring lanes, VPL times eight a lane, one element an access.
+template <int VPL>
 struct Channels {
   int first, step, C;
   __device__ __forceinline__ Channels(int C_) : C(C_) {
-    first = VEC ? (int)threadIdx.x * 8 : (int)threadIdx.x;
-    step = VEC ? (int)blockDim.x * 8 : (int)blockDim.x;
+    first = (int)threadIdx.x;
+    step = (int)blockDim.x;
   }
-  __device__ __forceinline__ int at(int v, int e) const { return VEC ? first + v * step + e : first + (v * 8 + e) * step; }
-  __device__ __forceinline__ bool has(int v, int e) const { return VEC ? first + v * step < C : at(v, e) < C; }
+  __device__ __forceinline__ int at(int v, int e) const { return first + (v * 8 + e) * step; }
+  __device__ __forceinline__ bool has(int v, int e) const { return at(v, e) < C; }
 
   // the row is the same for all lanes: its address stays in scalar registers
   template <int TYPE>
@@ -66,13 +70,9 @@ struct Channels {
 #pragma unroll
     for (int v = 0; v < VPL; ++v) {
       float t[8] = {};
-      if constexpr (VEC) {
-        if (has(v, 0)) load8<TYPE>(from<TYPE>(base, row), (unsigned)at(v, 0), t);
-      } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (has(v, e)) t[e] = load1<TYPE>(from<TYPE>(base, row), (unsigned)at(v, e));
-      }
+      for (int e = 0; e < 8; ++e)
+        if (has(v, e)) t[e] = load1<TYPE>(from<TYPE>(base, row), (unsigned)at(v, e));
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[v * 8 + e] = t[e];
     }
@@ -81,16 +81,9 @@ struct Channels {
   __device__ __forceinline__ void store(void* base, size_t row, const float (&x)[VPL * 8]) const {
 #pragma unroll
     for (int v = 0; v < VPL; ++v) {
-      if constexpr (VEC) {
-        float t[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) t[e] = x[v * 8 + e];
-        if (has(v, 0)) store8<TYPE>(const_cast<void*>(from<TYPE>(base, row)), (unsigned)at(v, 0), t);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (has(v, e)) store1<TYPE>(const_cast<void*>(from<TYPE>(base, row)), (unsigned)at(v, e), x[v * 8 + e]);
-      }
+      for (int e = 0; e < 8; ++e)
+        if (has(v, e)) store1<TYPE>(const_cast<void*>(from<TYPE>(base, row)), (unsigned)at(v, e), x[v * 8 + e]);
     }
   }
   // a parameter vector, or `otherwise` where there is none
@@ -132,8 +125,8 @@ struct RowSum {
 };
 
 // v -> (v - mean) * rho, returns rho.  The mean first and the squares of what is left then: a row far from zero loses nothing.
-template <int VPL, bool VEC>
-__device__ __forceinline__ float normalise(float (&v)[VPL * 8], int norm, float eps, const Channels<VPL, VEC>& ch, RowSum& sum) {
+template <int VPL>
+__device__ __forceinline__ float normalise(float (&v)[VPL * 8], int norm, float eps, const Channels<VPL>& ch, RowSum& sum) {
   if (norm == SVG_NORM_NONE) return 1.0f;
   const float inv = 1.0f / (float)ch.C;
   if (norm == SVG_NORM_LAYER) {
@@ -155,13 +148,13 @@ __device__ __forceinline__ float normalise(float (&v)[VPL * 8], int norm, float 
   return rho;
 }
 
-template <int TS, int TB, int VPL, bool VEC, bool FP4>
+template <int TS, int TB, int VPL>
 __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_kernel(GateNormArgs a) {
   __shared__ float places[2][kMaxWaves][2];
-  const Channels<VPL, VEC> ch(a.C);
+  const Channels<VPL> ch(a.C);
   RowSum sum{places, 0, (int)(blockDim.x >> 6)};
-  const long long r0 = (long long)blockIdx.x * a.rows_per_block;
-  const long long r1 = min(r0 + a.rows_per_block, a.row_limit);
+  const long long r0 = (long long)blockIdx.x * a.strip;
+  const long long r1 = min(r0 + a.strip, a.rows);
   for (long long row = r0; row < r1; ++row) {
     float v[VPL * 8] = {};
     if (row < a.rows) {
@@ -189,7 +182,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_kernel(GateNormArgs 
         for (int i = 0; i < VPL * 8; ++i) v[i] = __builtin_fmaf(t[i], y[i], v[i]);
       }
       if (a.r) ch.template store<TS>(a.r, (size_t)row * a.ld_r, v);
-      if (a.h || FP4) {
+      if (a.h) {
         normalise(v, a.pre, a.eps, ch, sum);
         if (a.pre != SVG_NORM_NONE) {
           ch.table(a.weight, 0, 1.0f, t);
@@ -209,21 +202,6 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_kernel(GateNormArgs 
         if (a.h) ch.template store<TB>(a.h, (size_t)row * a.ld_h, v);
       }
     }
-    if constexpr (FP4) {
-      const long long rt = row / kFp4Rows;
-      const int i16 = (int)(row % kFp4Rows);
-#pragma unroll
-      for (int k = 0; k < VPL; ++k) {
-        float t[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) t[e] = v[k * 8 + e];
-        const int c = ch.at(k, 0), ct = c / kFp4Cols, g = (c >> 5) & 3;
-        const unsigned s = fp4_scale(quad_max(magnitude8(t)));
-        if (ct < a.col_tiles) a.codes[((size_t)rt * a.col_tiles + ct) * 256 + g * 64 + i16 * 4 + ((c >> 3) & 3)] = fp4_codes8(t, s);
-        if ((c & 31) == 0 && ct < a.col_groups * kFp4Group)
-          a.scales[(((size_t)rt * a.col_groups + ct / kFp4Group) * 64 + g * 16 + i16) * 4 + ct % kFp4Group] = (unsigned char)s;
-      }
-    }
   }
 }
 
@@ -233,16 +211,16 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_kernel(GateNormArgs 
 //   dweight = sum over g of (1 + scale) S2, dbias the same of S1, dpost_weight = sum over g of gate T2, dpost_bias of T1.
 // They stay in registers while the strip is in one group and go to slot (workgroup + group), of which every pair that has
 // rows has one of its own, because neither number ever falls along the rows.
-template <int TS, int TB, int VPL, bool VEC>
+template <int TS, int TB, int VPL>
 __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_grad_kernel(GateNormArgs a) {
   __shared__ float places[2][kMaxWaves][2];
-  const Channels<VPL, VEC> ch(a.C);
+  const Channels<VPL> ch(a.C);
   RowSum sum{places, 0, (int)(blockDim.x >> 6)};
   constexpr int NC = VPL * 8;
   float s1[NC] = {}, s2[NC] = {}, t1[NC] = {}, t2[NC] = {};
   const float inv = 1.0f / (float)a.C;
-  const long long r0 = (long long)blockIdx.x * a.rows_per_block;
-  const long long r1 = min(r0 + a.rows_per_block, a.rows);
+  const long long r0 = (long long)blockIdx.x * a.strip;
+  const long long r1 = min(r0 + a.strip, a.rows);
   int g = group_of(a, r0);
   auto flush = [&] {
     const size_t slot = (size_t)(blockIdx.x + (unsigned)g) * 4 * a.C;
@@ -339,20 +317,487 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_grad_kernel(GateNorm
   flush();
 }
 
+// ---------------------------------------------------------------------------------------------------------------------
+// Rows that are 16-byte aligned.
+//
+// A team of wavefronts holds a row, eight neighbouring channels a lane and 512 a wavefront (VPL times), and takes the rows of a
+// strip in turn; a workgroup is one team or several with strips of their own.  Rows come through LDS: every wavefront asks
+// for its part of the row D rows ahead, straight from memory into a ring of its own, so that 80 to 120 KB are on their way to a
+// compute unit whatever registers the row in work needs.  (One row ahead in registers: 32760 x 5120 forward 538 us, backward 992.)
+// A ring is written and read by its own wavefront alone: no barrier, a count of its outstanding operations is enough.
+constexpr int kSegment = 512;         // channels of a wavefront and vector
+
+// The lane's eight channels of one tensor in the ring.
+template <int TYPE>
+__device__ __forceinline__ void read_ring(const unsigned char* at, float (&x)[8]) {
+  const int lane = threadIdx.x & 63;
+  if constexpr (TYPE == SVG_F32) {
+    const block_f32x4* p = reinterpret_cast<const block_f32x4*>(at + lane * 32);
+    const block_f32x4 lo = p[0], hi = p[1];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { x[e] = lo[e]; x[4 + e] = hi[e]; }
+  } else if constexpr (TYPE == SVG_BF16) {
+    const block_u32x4 w = *reinterpret_cast<const block_u32x4*>(at + lane * 16);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[2 * e] = __uint_as_float(w[e] << 16);
+      x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+    }
+  } else {
+    const block_f16x8 h = *reinterpret_cast<const block_f16x8*>(at + lane * 16);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = (float)h[e];
+  }
+}
+
+// A tensor's rows: the wavefront's part of one goes to the ring in loads of 1 KB; what is behind the last channel, or of a
+// row that does not exist, arrives as zeros.
+template <int TYPE, int VPL>
+struct Rows {
+  static constexpr int size = type_bytes(TYPE);
+  static constexpr int loads = VPL * kSegment * 2 / 1024 * (size / 2);
+  static constexpr int bytes = VPL * kSegment * size;
+  const char* base;
+  size_t step;                        // bytes of a row
+  __device__ __forceinline__ void ask(long long row, bool there, int C, int waves, int wave, unsigned to) const {
+    const auto rsrc = attn::buffer_words(base + (there ? (size_t)row * step : 0), there && base ? (unsigned)C * size : 0u);
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int v = 0; v < VPL; ++v)
+#pragma unroll
+      for (int l = 0; l < loads / VPL; ++l)
+        load_one_to_lds(rsrc, lane * 16, (wave + v * waves) * kSegment * size + l * 1024, to + v * kSegment * size + l * 1024);
+  }
+};
+
+template <int VPL>
+struct Lane {
+  static constexpr int N = VPL * 8;
+  int first, step, C;                 // channel of vector v, element e: first + v step + e
+  __device__ __forceinline__ Lane(int C_, int waves, int wave) : first((wave * 64 + (int)(threadIdx.x & 63)) * 8), step(waves * kSegment), C(C_) {}
+  __device__ __forceinline__ int at(int i) const { return first + i / 8 * step + i % 8; }
+  __device__ __forceinline__ bool has(int i) const { return first + i / 8 * step < C; }
+  template <int TYPE>
+  __device__ __forceinline__ void read(const unsigned char* ring, float (&x)[N]) const {
+#pragma unroll
+    for (int v = 0; v < VPL; ++v) {
+      float t[8];
+      read_ring<TYPE>(ring + v * kSegment * type_bytes(TYPE), t);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[v * 8 + e] = t[e];
+    }
+  }
+  // Results are not kept in L2: a tensor of this size leaves it before it is read again.
+  template <int TYPE>
+  __device__ __forceinline__ void store(void* base, size_t row, const float (&x)[N]) const {
+    char* const p = static_cast<char*>(base) + row * type_bytes(TYPE);
+#pragma unroll
+    for (int v = 0; v < VPL; ++v) {
+      if (!has(v * 8)) continue;
+      block_u32x4* const q = reinterpret_cast<block_u32x4*>(p + (unsigned)at(v * 8) * (unsigned)type_bytes(TYPE));
+      const block_f32x8 f = {x[v * 8], x[v * 8 + 1], x[v * 8 + 2], x[v * 8 + 3], x[v * 8 + 4], x[v * 8 + 5], x[v * 8 + 6], x[v * 8 + 7]};
+      if constexpr (TYPE == SVG_F32) {
+        __builtin_nontemporal_store(__builtin_bit_cast(block_u32x4, block_f32x4{f[0], f[1], f[2], f[3]}), q);
+        __builtin_nontemporal_store(__builtin_bit_cast(block_u32x4, block_f32x4{f[4], f[5], f[6], f[7]}), q + 1);
+      } else if constexpr (TYPE == SVG_BF16) {
+        __builtin_nontemporal_store(__builtin_bit_cast(block_u32x4, __builtin_convertvector(f, block_bf16x8)), q);
+      } else {
+        __builtin_nontemporal_store(__builtin_bit_cast(block_u32x4, __builtin_convertvector(f, block_f16x8)), q);
+      }
+    }
+  }
+  // a parameter vector, or `otherwise` where there is none; zero where the row has no channel
+  __device__ __forceinline__ void table(const float* base, size_t row, float otherwise, float (&x)[N]) const {
+#pragma unroll
+    for (int v = 0; v < VPL; ++v) {
+      float t[8] = {};
+      if (has(v * 8)) {
+        if (base) {
+          load8<SVG_F32>(base + row, (unsigned)at(v * 8), t);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) t[e] = otherwise;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[v * 8 + e] = t[e];
+    }
+  }
+};
+
+// What a team's wavefronts tell each other through LDS: up to four numbers each.  Two sets of places in turn, so that one
+// barrier a time is enough: a wavefront writes a place again only behind the next barrier.  The barrier is a bare one: it need not
+// wait for rows on their way.
+struct Meeting {
+  block_f32x4 (*place)[kMaxWaves];
+  int turn, waves, wave, team;        // wavefronts of a team, this one's number in it, the team's first wavefront
+
+  // mine of all wavefronts, that of wavefront l in lane l and zeros behind them
+  __device__ __forceinline__ block_f32x4 tell(block_f32x4 mine) {
+    const int lane = threadIdx.x & 63;
+    if (waves == 1) return lane == 0 ? mine : block_f32x4{};
+    block_f32x4* const here = place[turn] + team;
+    if (lane == 0) here[wave] = mine;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    attn::barrier_loads_done();
+    turn ^= 1;
+    return lane < waves ? here[lane] : block_f32x4{};
+  }
+  __device__ __forceinline__ void sums(float& p, float& q) {
+    p = wave_sum(p);
+    q = wave_sum(q);
+    if (waves == 1) return;
+    const block_f32x4 all = tell({p, q, 0.f, 0.f});
+    p = wave_sum(all[0]);
+    q = wave_sum(all[1]);
+  }
+};
+
+// A row's normalisation, v -> (v - mean) rho.  A wavefront takes the mean of its own n channels first and the squares of what is left
+// then, and the wavefronts' pairs are joined by  sum of squares = sum over w of (squares_w + n_w (mean_w - mean)^2): a row far
+// from zero loses nothing, and one meeting is enough.
+template <int VPL>
+__device__ __forceinline__ void own_statistics(const float (&v)[VPL * 8], int norm, const Lane<VPL>& lane, float inv_n, float& mean, float& squares) {
+  mean = squares = 0.f;
+  if (norm == SVG_NORM_NONE) return;
+  if (norm == SVG_NORM_LAYER) {
+#pragma unroll
+    for (int i = 0; i < VPL * 8; ++i) mean += v[i];       // zeros where there is no channel
+    mean = wave_sum(mean) * inv_n;
+  }
+#pragma unroll
+  for (int i = 0; i < VPL * 8; ++i) {
+    const float d = lane.has(i) ? v[i] - mean : 0.f;
+    squares = __builtin_fmaf(d, d, squares);
+  }
+  squares = wave_sum(squares);
+}
+// mean_w and squares_w of wavefront w in lane w, n its channels there
+__device__ __forceinline__ void join_statistics(float& mean, float& squares, float n, float inv) {
+  const float all = wave_sum(n * mean) * inv, d = mean - all;
+  squares = wave_sum(__builtin_fmaf(n * d, d, squares));
+  mean = all;
+}
+template <int VPL>
+__device__ __forceinline__ float apply_statistics(float (&v)[VPL * 8], int norm, float mean, float squares, float inv, float eps, const Lane<VPL>& lane) {
+  if (norm == SVG_NORM_NONE) return 1.0f;
+  const float rho = 1.0f / sqrtf(squares * inv + eps);
+#pragma unroll
+  for (int i = 0; i < VPL * 8; ++i) v[i] = lane.has(i) ? (v[i] - mean) * rho : 0.f;
+  return rho;
+}
+
+// A workgroup's teams.
+template <int VPL>
+struct Team {
+  int wave, index, number;            // of this wavefront in its team; of the team in its workgroup and in the launch
+  Lane<VPL> lane;
+  Meeting meet;
+  float inv_n, n_of_lane, inv;        // 1 / channels of this wavefront; channels of the team's wavefront `lane`; 1 / C
+  __device__ __forceinline__ Team(const GateNormArgs& a, block_f32x4 (*places)[kMaxWaves])
+      : wave(__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6) % a.waves)),
+        index(__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6) / a.waves)),
+        number((int)blockIdx.x * ((int)blockDim.x / (a.waves * 64)) + index),
+        lane(a.C, a.waves, wave),
+        meet{places, 0, a.waves, wave, __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) - wave} {
+    auto channels = [&](int w) {
+      int n = 0;
+      for (int v = 0; v < VPL; ++v) n += min(max(a.C - (w + v * a.waves) * kSegment, 0), kSegment);
+      return (float)n;
+    };
+    inv_n = 1.0f / channels(wave);
+    n_of_lane = (int)(threadIdx.x & 63) < a.waves ? channels(threadIdx.x & 63) : 0.f;
+    inv = 1.0f / (float)a.C;
+  }
+  __device__ __forceinline__ float normalise(float (&v)[VPL * 8], int norm, float eps) {
+    if (norm == SVG_NORM_NONE) return 1.0f;
+    float mean, squares;
+    own_statistics<VPL>(v, norm, lane, inv_n, mean, squares);
+    const block_f32x4 all = meet.tell({mean, squares, 0.f, 0.f});
+    mean = all[0];
+    squares = all[1];
+    join_statistics(mean, squares, n_of_lane, inv);
+    return apply_statistics<VPL>(v, norm, mean, squares, inv, eps, lane);
+  }
+};
+
+// Waits until at most N of this wavefront's operations on memory are outstanding (they end in order).
+template <int N>
+__device__ __forceinline__ void wait_ring() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N < 63 ? N : 63) : "memory"); }
+
+// The forward pass.  The tables of a group stay in registers, folded with the norms' weights: r = alpha x + (G1 yhat + G0),
+// h = H1 rhat + H0.
+template <int TS, int TB, int VPL, int D, bool FP4>
+__global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_ring_kernel(GateNormArgs a) {
+  extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+  __shared__ block_f32x4 places[2][kMaxWaves];
+  Team<VPL> team(a, places);
+  constexpr int N = VPL * 8;
+  using X = Rows<TS, VPL>;
+  using Y = Rows<TB, VPL>;
+  const X xs{static_cast<const char*>(a.x), (size_t)a.ld_x * X::size};
+  const Y ys{static_cast<const char*>(a.y), (size_t)a.ld_y * Y::size};
+  constexpr int kSlot = X::bytes + Y::bytes, kLoads = X::loads + Y::loads;
+  // stores of a row at least, where r and h (or its 4-bit form) are wanted: only the first vector is sure to have a channel
+  constexpr int kStores = X::size / 2 + (FP4 ? 2 : 1);
+  unsigned char* const ring = lds + (threadIdx.x >> 6) * (D * kSlot);
+  const unsigned ring0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)ring);
+  const long long r0 = (long long)team.number * a.strip;
+  auto ask = [&](int k) {
+    const bool there = k < a.strip && r0 + k < a.rows;
+    const unsigned to = ring0 + (unsigned)(k % D) * kSlot;
+    xs.ask(r0 + k, there, a.C, a.waves, team.wave, to);
+    ys.ask(r0 + k, there, a.C, a.waves, team.wave, to + X::bytes);
+  };
+  const bool second = a.h || FP4, counted = a.r && (FP4 || a.h);
+  float g1[N], g0[N], h1[N], h0[N];
+  int group = -1;
+#pragma unroll
+  for (int k = 0; k < D; ++k) ask(k);
+  // all teams of a workgroup run as many turns: they meet
+  const int turns = (int)min((long long)a.strip, a.row_limit - (r0 - (long long)team.index * a.strip));
+  for (int k = 0; k < turns; ++k) {
+    const long long row = r0 + k;
+    const bool there = row < a.rows;
+    // the tables' loads run beside those of the first rows
+    if (there) {
+      const int now = group_of(a, row);
+      if (now != group) {
+        group = now;
+        const size_t mod = (size_t)now * a.ld_mod;
+        float t[N];
+        if (a.y) {
+          team.lane.table(a.gate, mod, 1.0f, g1);
+          team.lane.table(a.post == SVG_NORM_LAYER ? a.post_bias : nullptr, 0, 0.0f, g0);
+          team.lane.table(a.post != SVG_NORM_NONE ? a.post_weight : nullptr, 0, 1.0f, t);
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            g0[i] *= g1[i];
+            g1[i] *= t[i];
+          }
+        }
+        if (second) {
+          team.lane.table(a.scale, mod, 0.0f, t);
+          team.lane.table(a.pre != SVG_NORM_NONE ? a.weight : nullptr, 0, 1.0f, h1);
+          team.lane.table(a.pre == SVG_NORM_LAYER ? a.bias : nullptr, 0, 0.0f, h0);
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            h0[i] *= 1.0f + t[i];
+            h1[i] *= 1.0f + t[i];
+          }
+          team.lane.table(a.shift, mod, 0.0f, t);
+#pragma unroll
+          for (int i = 0; i < N; ++i) h0[i] += t[i];
+        }
+      }
+    }
+    // row k's loads are in front of those of D - 1 rows and, from row D on, of D rows' stores
+    if (counted && k >= D) wait_ring<(D - 1) * kLoads + D * kStores>();
+    else wait_ring<(D - 1) * kLoads>();
+    const unsigned char* const slot = ring + (unsigned)(k % D) * kSlot;
+    float v[N], y[N];
+    team.lane.template read<TS>(slot, v);
+    team.lane.template read<TB>(slot + X::bytes, y);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // the slot has been read
+    ask(k + D);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] *= a.alpha;
+    if (a.y) {
+      team.normalise(y, a.post, a.post_eps);
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] += __builtin_fmaf(g1[i], y[i], g0[i]);
+    }
+    if (a.r && there) team.lane.template store<TS>(a.r, (size_t)row * a.ld_r, v);
+    if (second) {
+      team.normalise(v, a.pre, a.eps);
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = __builtin_fmaf(v[i], h1[i], h0[i]);
+      if (a.h && there) team.lane.template store<TB>(a.h, (size_t)row * a.ld_h, v);
+    }
+    if constexpr (FP4) {
+      if (row >= a.row_limit) continue;
+      const long long rt = row / kFp4Rows;
+      const int i16 = (int)(row % kFp4Rows);
+#pragma unroll
+      for (int k8 = 0; k8 < VPL; ++k8) {
+        float t[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t[e] = there && team.lane.has(k8 * 8) ? v[k8 * 8 + e] : 0.f;      // the padding
+        const int c = team.lane.at(k8 * 8), ct = c / kFp4Cols, g = (c >> 5) & 3;
+        const unsigned s = fp4_scale(quad_max(magnitude8(t)));
+        if (ct < a.col_tiles) a.codes[((size_t)rt * a.col_tiles + ct) * 256 + g * 64 + i16 * 4 + ((c >> 3) & 3)] = fp4_codes8(t, s);
+        if ((c & 31) == 0 && ct < a.col_groups * kFp4Group)
+          a.scales[(((size_t)rt * a.col_groups + ct / kFp4Group) * 64 + g * 16 + i16) * 4 + ct % kFp4Group] = (unsigned char)s;
+      }
+    }
+  }
+  wait_ring<0>();                     // no load to LDS outlives the workgroup
+}
+
+// Gradients of the rows of a strip; the parameters' sums as in gate_norm_grad_kernel.
+template <int TS, int TB, int VPL, int D>
+__global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_grad_ring_kernel(GateNormArgs a) {
+  extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+  __shared__ block_f32x4 places[2][kMaxWaves];
+  Team<VPL> team(a, places);
+  constexpr int N = VPL * 8;
+  using S = Rows<TS, VPL>;
+  using B = Rows<TB, VPL>;
+  const S rs{static_cast<const char*>(a.r_in), (size_t)a.ld_r * S::size}, drs{static_cast<const char*>(a.dr), (size_t)a.ld_r * S::size};
+  const B ys{static_cast<const char*>(a.y), (size_t)a.ld_y * B::size}, dhs{static_cast<const char*>(a.dh), (size_t)a.ld_h * B::size};
+  constexpr int kSlot = 2 * (S::bytes + B::bytes), kLoads = 2 * (S::loads + B::loads), kStores = S::size / 2 + 1;
+  unsigned char* const ring = lds + (threadIdx.x >> 6) * (D * kSlot);
+  const unsigned ring0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)ring);
+  const long long r0 = (long long)team.number * a.strip;
+  auto ask = [&](int k) {
+    const bool there = k < a.strip && r0 + k < a.rows;
+    const unsigned to = ring0 + (unsigned)(k % D) * kSlot;
+    rs.ask(r0 + k, there, a.C, a.waves, team.wave, to);
+    drs.ask(r0 + k, there, a.C, a.waves, team.wave, to + S::bytes);
+    ys.ask(r0 + k, there, a.C, a.waves, team.wave, to + 2 * S::bytes);
+    dhs.ask(r0 + k, there, a.C, a.waves, team.wave, to + 2 * S::bytes + B::bytes);
+  };
+  float s1[N] = {}, s2[N] = {}, t1[N] = {}, t2[N] = {};
+  float e1[N], f1[N];                 // (1 + scale) weight, gate post_weight
+  int group = -1;
+  auto flush = [&] {
+    const size_t slot = (size_t)(team.number + group) * 4 * a.C;
+    team.lane.template store<SVG_F32>(a.partial, slot, s1);
+    team.lane.template store<SVG_F32>(a.partial, slot + a.C, s2);
+    team.lane.template store<SVG_F32>(a.partial, slot + 2 * (size_t)a.C, t1);
+    team.lane.template store<SVG_F32>(a.partial, slot + 3 * (size_t)a.C, t2);
+  };
+  const int pre = a.dh ? a.pre : SVG_NORM_NONE, post = a.y ? a.post : SVG_NORM_NONE;
+  const bool counted = a.dx && a.dy;
+#pragma unroll
+  for (int k = 0; k < D; ++k) ask(k);
+  const int turns = (int)min((long long)a.strip, a.rows - (r0 - (long long)team.index * a.strip));
+  for (int k = 0; k < turns; ++k) {
+    const long long row = r0 + k;
+    const bool there = row < a.rows;
+    if (there) {
+      const int now = group_of(a, row);
+      if (now != group) {
+        if (group >= 0) {
+          flush();
+#pragma unroll
+          for (int i = 0; i < N; ++i) s1[i] = s2[i] = t1[i] = t2[i] = 0.f;
+        }
+        group = now;
+        const size_t mod = (size_t)now * a.ld_mod;
+        float t[N];
+        team.lane.table(a.scale, mod, 0.0f, e1);
+        team.lane.table(a.pre != SVG_NORM_NONE ? a.weight : nullptr, 0, 1.0f, t);
+#pragma unroll
+        for (int i = 0; i < N; ++i) e1[i] = (1.0f + e1[i]) * t[i];
+        team.lane.table(a.gate, mod, 1.0f, f1);
+        team.lane.table(a.post != SVG_NORM_NONE ? a.post_weight : nullptr, 0, 1.0f, t);
+#pragma unroll
+        for (int i = 0; i < N; ++i) f1[i] *= t[i];
+      }
+    }
+    if (counted && k >= D) wait_ring<(D - 1) * kLoads + D * kStores>();
+    else wait_ring<(D - 1) * kLoads>();
+    const unsigned char* const slot = ring + (unsigned)(k % D) * kSlot;
+    float rhat[N], d[N], yhat[N], e[N];
+    team.lane.template read<TS>(slot, rhat);
+    team.lane.template read<TS>(slot + S::bytes, d);
+    team.lane.template read<TB>(slot + 2 * S::bytes, yhat);
+    team.lane.template read<TB>(slot + 2 * S::bytes + B::bytes, e);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    ask(k + D);
+    // both normalisations' statistics in one meeting; a row that does not exist is zeros
+    float rho = 1.0f, rho_y = 1.0f;
+    if (pre != SVG_NORM_NONE || post != SVG_NORM_NONE) {
+      float mr, sr, my, sy;
+      own_statistics<VPL>(rhat, pre, team.lane, team.inv_n, mr, sr);
+      own_statistics<VPL>(yhat, post, team.lane, team.inv_n, my, sy);
+      const block_f32x4 all = team.meet.tell({mr, sr, my, sy});
+      mr = all[0];
+      sr = all[1];
+      my = all[2];
+      sy = all[3];
+      if (pre != SVG_NORM_NONE) join_statistics(mr, sr, team.n_of_lane, team.inv);
+      if (post != SVG_NORM_NONE) join_statistics(my, sy, team.n_of_lane, team.inv);
+      rho = apply_statistics<VPL>(rhat, pre, mr, sr, team.inv, a.eps, team.lane);
+      rho_y = apply_statistics<VPL>(yhat, post, my, sy, team.inv, a.post_eps, team.lane);
+    }
+    if (a.dh) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        s1[i] += e[i];
+        s2[i] = __builtin_fmaf(e[i], rhat[i], s2[i]);
+        e[i] *= e1[i];
+      }
+      if (pre != SVG_NORM_NONE) {
+        float m1 = 0.f, m2 = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          m1 += e[i];
+          m2 = __builtin_fmaf(e[i], rhat[i], m2);
+        }
+        team.meet.sums(m1, m2);
+        m1 = pre == SVG_NORM_LAYER ? m1 * team.inv : 0.f;
+        m2 *= team.inv;
+        // places without a channel stay zero: they are part of the sums below
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          d[i] = team.lane.has(i) ? __builtin_fmaf(rho, __builtin_fmaf(-rhat[i], m2, e[i] - m1), d[i]) : 0.f;
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) d[i] += e[i];
+      }
+    }
+    if (a.dx && there) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) e[i] = a.alpha * d[i];
+      team.lane.template store<TS>(a.dx, (size_t)row * a.ld_x, e);
+    }
+    if (there) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        t1[i] += d[i];
+        t2[i] = __builtin_fmaf(d[i], yhat[i], t2[i]);
+      }
+    }
+    if (a.dy) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) d[i] *= f1[i];
+      if (post != SVG_NORM_NONE) {
+        float m1 = 0.f, m2 = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          m1 += d[i];
+          m2 = __builtin_fmaf(d[i], yhat[i], m2);
+        }
+        team.meet.sums(m1, m2);
+        m1 = post == SVG_NORM_LAYER ? m1 * team.inv : 0.f;
+        m2 *= team.inv;
+#pragma unroll
+        for (int i = 0; i < N; ++i) d[i] = rho_y * __builtin_fmaf(-yhat[i], m2, d[i] - m1);
+      }
+      if (there) team.lane.template store<TB>(a.dy, (size_t)row * a.ld_y, d);
+    }
+  }
+  wait_ring<0>();
+  if (group >= 0) flush();
+}
+
 struct GradSumArgs {
   long long rows;
-  int C, groups, rows_per_block;
+  int C, groups, strip, splits;
   const int32_t* group_ptr;
   long long group_rows;
   const float* partial;               // [slots][4][C]
-  float* total;                       // [groups][4][C], or null where no weight's gradient is wanted
+  float* split;                       // [splits][groups][4][C]: sums of parts of the strips, where there is more than one
+  float* total;                       // [groups][4][C], or null where no weight's gradient is wanted or there is one group
   const float *post_weight, *post_bias, *weight, *bias;
   const float *gate, *scale;          // the forward pass's tables, [groups] rows of ld_mod
   long long ld_mod, ld_grad;
   float *dgate, *dscale, *dshift, *dpost_weight, *dpost_bias, *dweight, *dbias;
 };
 
-constexpr int kSumLanes = 16;         // rows (slots, groups) that are summed side by side
+constexpr int kSumLanes = 16;         // rows (slots, splits, groups) that are summed side by side
 constexpr int kSumChannels = 64;
 
 // Adds up the four sums of 64 channels over the workgroup's rows of threads; the result is in the first row.
@@ -370,7 +815,25 @@ __device__ __forceinline__ void fold_rows(float (&s)[4]) {
   __syncthreads();
 }
 
-// The sums of a group from the slots of the strips that have rows of it.
+// The gradients of group g, channel c, from its sums.
+__device__ __forceinline__ void finish_group(const GradSumArgs& a, int g, int c, const float (&s)[4]) {
+  const size_t at = (size_t)g * a.ld_grad + c;
+  if (a.dshift) a.dshift[at] = s[0];
+  if (a.dscale) a.dscale[at] = (a.weight ? a.weight[c] : 1.f) * s[1] + (a.bias ? a.bias[c] : 0.f) * s[0];
+  if (a.dgate) a.dgate[at] = (a.post_weight ? a.post_weight[c] : 1.f) * s[3] + (a.post_bias ? a.post_bias[c] : 0.f) * s[2];
+  if (a.groups == 1) {
+    const float scale = a.scale ? 1.0f + a.scale[c] : 1.0f, gate = a.gate ? a.gate[c] : 1.0f;
+    if (a.dbias) a.dbias[c] = scale * s[0];
+    if (a.dweight) a.dweight[c] = scale * s[1];
+    if (a.dpost_bias) a.dpost_bias[c] = gate * s[2];
+    if (a.dpost_weight) a.dpost_weight[c] = gate * s[3];
+  } else if (a.total) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) a.total[((size_t)g * 4 + j) * a.C + c] = s[j];
+  }
+}
+
+// The sums of a group from the slots of the strips that have rows of it; blockIdx.z: a part of the strips.
 __global__ __launch_bounds__(kSumLanes* kSumChannels) void grad_groups_kernel(GradSumArgs a) {
   const int c = blockIdx.x * kSumChannels + threadIdx.x % kSumChannels, k = threadIdx.x / kSumChannels;
   for (int g = blockIdx.y; g < a.groups; g += gridDim.y) {
@@ -385,27 +848,43 @@ __global__ __launch_bounds__(kSumLanes* kSumChannels) void grad_groups_kernel(Gr
       }
     }
     float s[4] = {};
-    if (lo < hi && c < a.C)
-      for (long long b = lo / a.rows_per_block + k; b <= (hi - 1) / a.rows_per_block; b += kSumLanes) {
+    if (lo < hi && c < a.C) {
+      const long long first = lo / a.strip, end = (hi - 1) / a.strip + 1, part = (end - first + a.splits - 1) / a.splits;
+      const long long b1 = min(end, first + ((long long)blockIdx.z + 1) * part);
+#pragma unroll 4
+      for (long long b = first + blockIdx.z * part + k; b < b1; b += kSumLanes) {
         const float* p = a.partial + (size_t)(b + g) * 4 * a.C + c;
 #pragma unroll
         for (int j = 0; j < 4; ++j) s[j] += p[(size_t)j * a.C];
       }
+    }
     fold_rows(s);
     if (k == 0 && c < a.C) {
-      const size_t at = (size_t)g * a.ld_grad + c;
-      if (a.dshift) a.dshift[at] = s[0];
-      if (a.dscale) a.dscale[at] = (a.weight ? a.weight[c] : 1.f) * s[1] + (a.bias ? a.bias[c] : 0.f) * s[0];
-      if (a.dgate) a.dgate[at] = (a.post_weight ? a.post_weight[c] : 1.f) * s[3] + (a.post_bias ? a.post_bias[c] : 0.f) * s[2];
-      if (a.total) {
+      if (a.splits == 1) {
+        finish_group(a, g, c, s);
+      } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) a.total[((size_t)g * 4 + j) * a.C + c] = s[j];
+        for (int j = 0; j < 4; ++j) a.split[(((size_t)blockIdx.z * a.groups + g) * 4 + j) * a.C + c] = s[j];
       }
     }
   }
 }
 
-// The weights' gradients: the groups' sums under their modulation.
+// The parts' sums, and the gradients of the groups.
+__global__ __launch_bounds__(kSumLanes* kSumChannels) void grad_splits_kernel(GradSumArgs a) {
+  const int c = blockIdx.x * kSumChannels + threadIdx.x % kSumChannels, k = threadIdx.x / kSumChannels;
+  for (int g = blockIdx.y; g < a.groups; g += gridDim.y) {
+    float s[4] = {};
+    if (c < a.C)
+      for (int z = k; z < a.splits; z += kSumLanes)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[j] += a.split[(((size_t)z * a.groups + g) * 4 + j) * a.C + c];
+    fold_rows(s);
+    if (k == 0 && c < a.C) finish_group(a, g, c, s);
+  }
+}
+
+// The weights' gradients of several groups: the groups' sums under their modulation.
 __global__ __launch_bounds__(kSumLanes* kSumChannels) void grad_weights_kernel(GradSumArgs a) {
   const int c = blockIdx.x * kSumChannels + threadIdx.x % kSumChannels, k = threadIdx.x / kSumChannels;
   float s[4] = {};
@@ -428,12 +907,22 @@ __global__ __launch_bounds__(kSumLanes* kSumChannels) void grad_weights_kernel(G
   }
 }
 
-// Wavefronts that share a row and vectors of a lane, 512 channels each: one vector up to 512 channels, two up to 8192, four up to 16384.
-struct RowShape { int waves, vpl; };
+// Wavefronts that share a row, vectors of a lane (512 channels a wavefront and vector: one up to 8192 channels, two up to
+// 16384), and teams of a workgroup: as many as give it about ten wavefronts.
+struct RowShape { int waves, vpl, teams; };
 RowShape row_shape(int C) {
-  const int vectors = (C + 511) / 512;
-  const int vpl = vectors == 1 ? 1 : vectors <= 2 * kMaxWaves ? 2 : 4;
-  return {(vectors + vpl - 1) / vpl, vpl};
+  const int vectors = (C + 511) / 512, vpl = vectors <= kMaxWaves ? 1 : 2, waves = (vectors + vpl - 1) / vpl;
+  return {waves, vpl, waves >= 6 ? 1 : 10 / waves};
+}
+
+// Rows that a workgroup of so many wavefronts has on their way, at `slot` bytes a wavefront and row: three, or what LDS holds; 0: not one.
+constexpr int kRingBytes = 155 << 10;
+int ring_depth(int waves, int slot) { return std::min(3, kRingBytes / (waves * slot)); }
+
+// Rows of a strip, so that `per_unit` workgroups' teams to a compute unit take them all.
+int strip_rows(long long rows, int teams, int per_unit) {
+  const long long strips = 256ll * per_unit * teams;
+  return (int)std::max(1ll, (rows + strips - 1) / strips);
 }
 
 GateNormArgs gate_norm_args(const svg_gate_norm_t& d) {
@@ -460,41 +949,75 @@ bool aligned(const GateNormArgs& a) {
   return (a.C | a.ld_x | a.ld_y | a.ld_r | a.ld_h | a.ld_mod) % 8 == 0;
 }
 
-// f(stream type, branch type, vectors of a lane, whole vectors?) as integral constants
+// f(stream type, branch type, vectors of a lane) as integral constants
 template <class F>
-void dispatch(const svg_gate_norm_t& d, int vpl, bool vec, F f) {
-  auto with_types = [&](auto v, auto whole) {
+void dispatch(const svg_gate_norm_t& d, int vpl, F f) {
+  auto with_types = [&](auto v) {
     using BF = std::integral_constant<int, SVG_BF16>;
     using HF = std::integral_constant<int, SVG_F16>;
     using SF = std::integral_constant<int, SVG_F32>;
     if (d.stream_type == SVG_F32) {
-      if (d.branch_type == SVG_F16) f(SF{}, HF{}, v, whole);
-      else f(SF{}, BF{}, v, whole);
+      if (d.branch_type == SVG_F16) f(SF{}, HF{}, v);
+      else f(SF{}, BF{}, v);
     } else {
-      if (d.branch_type == SVG_F16) f(BF{}, HF{}, v, whole);
-      else f(BF{}, BF{}, v, whole);
+      if (d.branch_type == SVG_F16) f(BF{}, HF{}, v);
+      else f(BF{}, BF{}, v);
     }
   };
-  auto with_vectors = [&](auto whole) {
-    if (vpl == 1) with_types(std::integral_constant<int, 1>{}, whole);
-    else if (vpl == 2) with_types(std::integral_constant<int, 2>{}, whole);
-    else with_types(std::integral_constant<int, 4>{}, whole);
-  };
-  if (vec) with_vectors(std::true_type{});
-  else with_vectors(std::false_type{});
+  if (vpl == 1) with_types(std::integral_constant<int, 1>{});
+  else with_types(std::integral_constant<int, 2>{});
+}
+// f(depth) as an integral constant
+template <class F>
+void with_depth(int depth, F f) {
+  if (depth == 1) f(std::integral_constant<int, 1>{});
+  else if (depth == 2) f(std::integral_constant<int, 2>{});
+  else f(std::integral_constant<int, 3>{});
 }
 
-constexpr int kGradBlocks = 1024;     // strips of the backward pass
-int grad_rows_per_block(long long rows) { return (int)((rows + kGradBlocks - 1) / kGradBlocks); }
-long long grad_blocks(long long rows) {
-  const long long r = grad_rows_per_block(rows);
-  return r ? (rows + r - 1) / r : 0;
+// Launches a kernel with `bytes` of dynamic LDS; more than 64 KB has to be allowed, once for each GPU, because the call costs a microsecond.
+hipError_t launch_with_lds(void (*kernel)(GateNormArgs), std::atomic<unsigned long long>& allowed, dim3 grid, dim3 block, int bytes, hipStream_t stream,
+                           const GateNormArgs& a) {
+  if (bytes > 65536) {
+    int device = 0;
+    hipError_t e = hipGetDevice(&device);
+    if (e != hipSuccess) return e;
+    const unsigned long long bit = device < 64 ? 1ull << device : 0;
+    if (!(allowed.load(std::memory_order_relaxed) & bit)) {
+      e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kRingBytes);
+      if (e != hipSuccess) return e;
+      allowed.fetch_or(bit, std::memory_order_relaxed);
+    }
+  }
+  hipLaunchKernelGGL(kernel, grid, block, (unsigned)bytes, stream, a);
+  return hipGetLastError();
+}
+
+constexpr int kGradLeast = 2;         // rows of a strip of the backward pass: its sums cost the traffic of two
+struct GradShape {
+  RowShape row;
+  int strip, splits, slot, depth;     // depth 0: the general kernel
+  long long strips;
+};
+GradShape grad_shape(const svg_gate_norm_t& d) {
+  GradShape g;
+  g.row = row_shape(d.C);
+  g.slot = g.row.vpl * kSegment * 2 * (type_bytes(d.stream_type) + 2);
+  g.depth = ring_depth(g.row.waves * g.row.teams, g.slot);
+  g.strip = std::max(strip_rows(d.rows, g.row.teams, 1), kGradLeast);
+  g.strips = (d.rows + g.strip - 1) / g.strip;
+  // parts of the strips that are added up side by side: enough workgroups for the chip, at least 64 strips each
+  const long long chunks = (d.C + 63) / 64 * (long long)std::min(d.groups, 4096);
+  const long long most = std::min<long long>(32, g.strips / std::max(1, std::min(d.groups, 64)) / 64);
+  g.splits = (int)std::max<long long>(1, std::min<long long>(most, (512 + chunks - 1) / chunks));
+  return g;
 }
 
 }  // namespace
 
 size_t gate_norm_workspace_bytes(const svg_gate_norm_t& d) {
-  return (size_t)(grad_blocks(d.rows) + 2 * (long long)d.groups) * 4 * d.C * sizeof(float);
+  const GradShape g = grad_shape(d);
+  return (size_t)(g.strips + (long long)d.groups * (2 + (g.splits > 1 ? g.splits : 0))) * 4 * d.C * sizeof(float);
 }
 
 int launch_gate_norm(const svg_gate_norm_t& d, const void* x, const void* y, void* r, void* h, void* codes, void* scales,
@@ -508,23 +1031,31 @@ int launch_gate_norm(const svg_gate_norm_t& d, const void* x, const void* y, voi
   const bool vec = aligned(a);
   if (codes && (!vec || d.C % 32)) return SVG_ERR_UNSUPPORTED;
   if (codes) a.row_limit = fp4_row_tiles(d.rows) * kFp4Rows;
-  a.rows_per_block = codes ? 4 : 1;
-  while ((a.row_limit + a.rows_per_block - 1) / a.rows_per_block > 1 << 22) a.rows_per_block *= 2;      // a launch has fewer than 2^32 threads
-  const RowShape s = row_shape(d.C);
-  const long long blocks = (a.row_limit + a.rows_per_block - 1) / a.rows_per_block;
+  RowShape s = row_shape(d.C);
+  const int slot = s.vpl * kSegment * (type_bytes(d.stream_type) + 2), depth = ring_depth(s.waves * s.teams, slot);
+  const bool general = !vec;
+  if (general) s.teams = 1;
+  a.waves = s.waves;
+  a.strip = strip_rows(a.row_limit, general ? 8 : s.teams, 2);
+  const long long strips = (a.row_limit + a.strip - 1) / a.strip, blocks = (strips + s.teams - 1) / s.teams;
+  const dim3 grid((unsigned)blocks), block((unsigned)(64 * s.waves * s.teams));
+  hipError_t e = hipSuccess;
   (void)hipGetLastError();
-  dispatch(d, s.vpl, vec, [&](auto ts, auto tb, auto vpl, auto whole) {
+  dispatch(d, s.vpl, [&](auto ts, auto tb, auto vpl) {
     constexpr int TS = decltype(ts)::value, TB = decltype(tb)::value, VPL = decltype(vpl)::value;
-    constexpr bool VEC = decltype(whole)::value;
-    if constexpr (VEC) {
-      if (codes) {
-        hipLaunchKernelGGL((gate_norm_kernel<TS, TB, VPL, true, true>), dim3((unsigned)blocks), dim3(64 * s.waves), 0, stream, a);
-        return;
-      }
+    if (general) {
+      hipLaunchKernelGGL((gate_norm_kernel<TS, TB, VPL>), grid, block, 0, stream, a);
+      e = hipGetLastError();
+      return;
     }
-    hipLaunchKernelGGL((gate_norm_kernel<TS, TB, VPL, VEC, false>), dim3((unsigned)blocks), dim3(64 * s.waves), 0, stream, a);
+    with_depth(depth, [&](auto dc) {
+      constexpr int D = decltype(dc)::value;
+      static std::atomic<unsigned long long> allowed[2];
+      e = launch_with_lds(codes ? gate_norm_ring_kernel<TS, TB, VPL, D, true> : gate_norm_ring_kernel<TS, TB, VPL, D, false>, allowed[codes != nullptr],
+                          grid, block, s.waves * s.teams * D * slot, stream, a);
+    });
   });
-  return hip_status(hipGetLastError());
+  return hip_status(e);
 }
 
 int launch_gate_norm_grad(const svg_gate_norm_t& d, const void* r, const void* y, const void* dr, const void* dh, void* dx, void* dy,
@@ -532,25 +1063,39 @@ int launch_gate_norm_grad(const svg_gate_norm_t& d, const void* r, const void* y
   GateNormArgs a = gate_norm_args(d);
   a.r_in = r; a.y = y; a.dr = dr; a.dh = dh; a.dx = dx; a.dy = dy;
   a.partial = workspace;
-  const bool vec = aligned(a);
-  a.rows_per_block = grad_rows_per_block(d.rows);
-  const RowShape s = row_shape(d.C);
-  const long long blocks = grad_blocks(d.rows);
+  const GradShape g = grad_shape(d);
+  const bool general = !aligned(a) || !g.depth;
+  const int teams = general ? 1 : g.row.teams;
+  a.waves = g.row.waves;
+  a.strip = g.strip;
   (void)hipGetLastError();
-  if (d.rows)
-    dispatch(d, s.vpl, vec, [&](auto ts, auto tb, auto vpl, auto whole) {
-      hipLaunchKernelGGL((gate_norm_grad_kernel<decltype(ts)::value, decltype(tb)::value, decltype(vpl)::value, decltype(whole)::value>),
-                         dim3((unsigned)blocks), dim3(64 * s.waves), 0, stream, a);
+  if (d.rows) {
+    const dim3 grid((unsigned)((g.strips + teams - 1) / teams)), block((unsigned)(64 * g.row.waves * teams));
+    hipError_t e = hipSuccess;
+    dispatch(d, g.row.vpl, [&](auto ts, auto tb, auto vpl) {
+      constexpr int TS = decltype(ts)::value, TB = decltype(tb)::value, VPL = decltype(vpl)::value;
+      if (general) {
+        hipLaunchKernelGGL((gate_norm_grad_kernel<TS, TB, VPL>), grid, block, 0, stream, a);
+        e = hipGetLastError();
+        return;
+      }
+      with_depth(g.depth, [&](auto dc) {
+        constexpr int D = decltype(dc)::value;
+        static std::atomic<unsigned long long> allowed;
+        e = launch_with_lds(gate_norm_grad_ring_kernel<TS, TB, VPL, D>, allowed, grid, block, g.row.waves * teams * D * g.slot, stream, a);
+      });
     });
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return hip_status(e);
+    if (e != hipSuccess) return hip_status(e);
+  }
   GradSumArgs p = {};
   p.rows = d.rows; p.C = d.C; p.groups = d.groups;
-  p.rows_per_block = a.rows_per_block ? a.rows_per_block : 1;
+  p.strip = g.strip; p.splits = g.splits;
   p.group_ptr = d.group_ptr; p.group_rows = a.group_rows;
   p.partial = workspace;
   const bool weights = grads.post_weight || grads.post_bias || grads.weight || grads.bias;
-  p.total = weights ? workspace + (size_t)(blocks + d.groups) * 4 * d.C : nullptr;
+  float* const behind = workspace + (size_t)(g.strips + d.groups) * 4 * d.C;
+  p.total = weights && d.groups > 1 ? behind : nullptr;
+  p.split = behind + (size_t)d.groups * 4 * d.C;
   // a missing norm's weight and bias take no part
   p.post_weight = d.post_norm != SVG_NORM_NONE ? d.post_weight : nullptr;
   p.post_bias = d.post_norm == SVG_NORM_LAYER ? d.post_bias : nullptr;
@@ -561,11 +1106,12 @@ int launch_gate_norm_grad(const svg_gate_norm_t& d, const void* r, const void* y
   p.ld_grad = grads.ld_mod ? grads.ld_mod : d.C;
   p.dgate = grads.gate; p.dscale = grads.scale; p.dshift = grads.shift;
   p.dpost_weight = grads.post_weight; p.dpost_bias = grads.post_bias; p.dweight = grads.weight; p.dbias = grads.bias;
-  const unsigned chunks = (unsigned)((d.C + kSumChannels - 1) / kSumChannels);
-  if (weights || p.dgate || p.dscale || p.dshift)
-    hipLaunchKernelGGL(grad_groups_kernel, dim3(chunks, (unsigned)(d.groups < 4096 ? d.groups : 4096)), dim3(kSumLanes * kSumChannels), 0,
-                       stream, p);
-  if (weights) hipLaunchKernelGGL(grad_weights_kernel, dim3(chunks), dim3(kSumLanes * kSumChannels), 0, stream, p);
+  if (!weights && !p.dgate && !p.dscale && !p.dshift) return SVG_OK;
+  const unsigned chunks = (unsigned)((d.C + kSumChannels - 1) / kSumChannels), gy = (unsigned)std::min(d.groups, 4096);
+  const dim3 threads(kSumLanes * kSumChannels);
+  hipLaunchKernelGGL(grad_groups_kernel, dim3(chunks, gy, (unsigned)p.splits), threads, 0, stream, p);
+  if (p.splits > 1) hipLaunchKernelGGL(grad_splits_kernel, dim3(chunks, gy), threads, 0, stream, p);
+  if (p.total) hipLaunchKernelGGL(grad_weights_kernel, dim3(chunks), threads, 0, stream, p);
   return hip_status(hipGetLastError());
 }
 
