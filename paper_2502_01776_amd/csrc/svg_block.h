@@ -128,6 +128,44 @@ __device__ __forceinline__ void store8(void* base, size_t element, const float (
     *reinterpret_cast<block_f16x8*>(static_cast<unsigned short*>(base) + element) = __builtin_convertvector(f, block_f16x8);
   }
 }
+// The same at any element's address: the vector unit's loads and stores of 16 bytes need no alignment of their own.
+typedef unsigned block_u32x4_of2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef unsigned block_u32x4_of4 __attribute__((ext_vector_type(4), aligned(4)));
+template <int TYPE>
+__device__ __forceinline__ void load8_any(const void* base, size_t element, float (&v)[8]) {
+  if constexpr (TYPE == SVG_F32) {
+    const block_u32x4_of4* p = reinterpret_cast<const block_u32x4_of4*>(static_cast<const float*>(base) + element);
+    const block_u32x4 a = p[0], b = p[1];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { v[e] = __uint_as_float(a[e]); v[4 + e] = __uint_as_float(b[e]); }
+  } else {
+    const block_u32x4 a = *reinterpret_cast<const block_u32x4_of2*>(static_cast<const unsigned short*>(base) + element);
+    if constexpr (TYPE == SVG_BF16) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[2 * e] = __uint_as_float(a[e] << 16);
+        v[2 * e + 1] = __uint_as_float(a[e] & 0xffff0000u);
+      }
+    } else {
+      const block_f16x8 h = __builtin_bit_cast(block_f16x8, a);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = (float)h[e];
+    }
+  }
+}
+template <int TYPE>
+__device__ __forceinline__ void store8_any(void* base, size_t element, const float (&v)[8]) {
+  const block_f32x8 f = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
+  if constexpr (TYPE == SVG_F32) {
+    block_u32x4_of4* p = reinterpret_cast<block_u32x4_of4*>(static_cast<float*>(base) + element);
+    p[0] = __builtin_bit_cast(block_u32x4, block_f32x4{v[0], v[1], v[2], v[3]});
+    p[1] = __builtin_bit_cast(block_u32x4, block_f32x4{v[4], v[5], v[6], v[7]});
+  } else {
+    *reinterpret_cast<block_u32x4_of2*>(static_cast<unsigned short*>(base) + element) =
+        TYPE == SVG_BF16 ? __builtin_bit_cast(block_u32x4, __builtin_convertvector(f, block_bf16x8))
+                         : __builtin_bit_cast(block_u32x4, __builtin_convertvector(f, block_f16x8));
+  }
+}
 template <int TYPE>
 __device__ __forceinline__ float load1(const void* base, size_t element) {
   if constexpr (TYPE == SVG_F32) return static_cast<const float*>(base)[element];
