@@ -56,286 +56,12 @@ __device__ __forceinline__ int group_of(const GateNormArgs& a, long long row, lo
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
-// Rows of any alignment: a workgroup holds a row, neighbouring channels in neighbouring lanes, VPL times eight a lane, one element an access.
-template <int VPL>
-struct Channels {
-  int first, step, C;
-  __device__ __forceinline__ Channels(int C_) : C(C_) {
-    first = (int)threadIdx.x;
-    step = (int)blockDim.x;
-  }
-  __device__ __forceinline__ int at(int v, int e) const { return first + (v * 8 + e) * step; }
-  __device__ __forceinline__ bool has(int v, int e) const { return at(v, e) < C; }
-
-  // the row is the same for all lanes: its address stays in scalar registers
-  template <int TYPE>
-  static __device__ __forceinline__ const void* from(const void* base, size_t row) {
-    return static_cast<const char*>(base) + row * (TYPE == SVG_F32 ? 4 : 2);
-  }
-  template <int TYPE>
-  __device__ __forceinline__ void load(const void* base, size_t row, float (&x)[VPL * 8]) const {
-#pragma unroll
-    for (int v = 0; v < VPL; ++v) {
-      float t[8] = {};
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (has(v, e)) t[e] = load1<TYPE>(from<TYPE>(base, row), (unsigned)at(v, e));
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[v * 8 + e] = t[e];
-    }
-  }
-  template <int TYPE>
-  __device__ __forceinline__ void store(void* base, size_t row, const float (&x)[VPL * 8]) const {
-#pragma unroll
-    for (int v = 0; v < VPL; ++v) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (has(v, e)) store1<TYPE>(const_cast<void*>(from<TYPE>(base, row)), (unsigned)at(v, e), x[v * 8 + e]);
-    }
-  }
-  // a parameter vector, or `otherwise` where there is none
-  __device__ __forceinline__ void table(const float* base, size_t row, float otherwise, float (&x)[VPL * 8]) const {
-    if (base) {
-      load<SVG_F32>(base, row, x);
-    } else {
-#pragma unroll
-      for (int i = 0; i < VPL * 8; ++i) x[i] = otherwise;
-    }
-  }
-};
-
-// Sums over the row: over the wavefront, then over the wavefronts of the workgroup through LDS.  Two sets of places in
-// turn, so that one barrier a sum is enough: a wavefront writes a place again only behind the next barrier.
-struct RowSum {
-  float (*place)[kMaxWaves][2];
-  int turn, waves;
-  __device__ __forceinline__ void operator()(float& p, float& q) {
-    p = wave_sum(p);
-    q = wave_sum(q);
-    if (waves == 1) return;
-    if ((threadIdx.x & 63) == 0) {
-      place[turn][threadIdx.x >> 6][0] = p;
-      place[turn][threadIdx.x >> 6][1] = q;
-    }
-    __syncthreads();
-    p = q = 0.f;
-    for (int w = 0; w < waves; ++w) {
-      p += place[turn][w][0];
-      q += place[turn][w][1];
-    }
-    turn ^= 1;
-  }
-  __device__ __forceinline__ void operator()(float& p) {
-    float none = 0.f;
-    (*this)(p, none);
-  }
-};
-
-// v -> (v - mean) * rho, returns rho.  The mean first and the squares of what is left then: a row far from zero loses nothing.
-template <int VPL>
-__device__ __forceinline__ float normalise(float (&v)[VPL * 8], int norm, float eps, const Channels<VPL>& ch, RowSum& sum) {
-  if (norm == SVG_NORM_NONE) return 1.0f;
-  const float inv = 1.0f / (float)ch.C;
-  if (norm == SVG_NORM_LAYER) {
-    float m = 0.f;
-#pragma unroll
-    for (int i = 0; i < VPL * 8; ++i) m += v[i];
-    sum(m);
-    m *= inv;
-#pragma unroll
-    for (int i = 0; i < VPL * 8; ++i) v[i] = ch.has(i / 8, i % 8) ? v[i] - m : 0.f;
-  }
-  float s = 0.f;
-#pragma unroll
-  for (int i = 0; i < VPL * 8; ++i) s = __builtin_fmaf(v[i], v[i], s);
-  sum(s);
-  const float rho = 1.0f / sqrtf(s * inv + eps);
-#pragma unroll
-  for (int i = 0; i < VPL * 8; ++i) v[i] *= rho;
-  return rho;
-}
-
-template <int TS, int TB, int VPL>
-__global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_kernel(GateNormArgs a) {
-  __shared__ float places[2][kMaxWaves][2];
-  const Channels<VPL> ch(a.C);
-  RowSum sum{places, 0, (int)(blockDim.x >> 6)};
-  const long long r0 = (long long)blockIdx.x * a.strip;
-  const long long r1 = min(r0 + a.strip, a.rows);
-  int group = 0;
-  long long group_end = 0;
-  for (long long row = r0; row < r1; ++row) {
-    float v[VPL * 8] = {};
-    if (row < a.rows) {
-      if (row >= group_end) group = group_of(a, row, group_end);
-      const size_t mod = (size_t)group * a.ld_mod;
-      float t[VPL * 8];
-      ch.template load<TS>(a.x, (size_t)row * a.ld_x, v);
-#pragma unroll
-      for (int i = 0; i < VPL * 8; ++i) v[i] *= a.alpha;
-      if (a.y) {
-        float y[VPL * 8];
-        ch.template load<TB>(a.y, (size_t)row * a.ld_y, y);
-        normalise(y, a.post, a.post_eps, ch, sum);
-        if (a.post != SVG_NORM_NONE) {
-          ch.table(a.post_weight, 0, 1.0f, t);
-#pragma unroll
-          for (int i = 0; i < VPL * 8; ++i) y[i] *= t[i];
-          if (a.post == SVG_NORM_LAYER) {
-            ch.table(a.post_bias, 0, 0.0f, t);
-#pragma unroll
-            for (int i = 0; i < VPL * 8; ++i) y[i] += t[i];
-          }
-        }
-        ch.table(a.gate, mod, 1.0f, t);
-#pragma unroll
-        for (int i = 0; i < VPL * 8; ++i) v[i] = __builtin_fmaf(t[i], y[i], v[i]);
-      }
-      if (a.r) ch.template store<TS>(a.r, (size_t)row * a.ld_r, v);
-      if (a.h) {
-        normalise(v, a.pre, a.eps, ch, sum);
-        if (a.pre != SVG_NORM_NONE) {
-          ch.table(a.weight, 0, 1.0f, t);
-#pragma unroll
-          for (int i = 0; i < VPL * 8; ++i) v[i] *= t[i];
-          if (a.pre == SVG_NORM_LAYER) {
-            ch.table(a.bias, 0, 0.0f, t);
-#pragma unroll
-            for (int i = 0; i < VPL * 8; ++i) v[i] += t[i];
-          }
-        }
-        float u[VPL * 8];
-        ch.table(a.scale, mod, 0.0f, t);
-        ch.table(a.shift, mod, 0.0f, u);
-#pragma unroll
-        for (int i = 0; i < VPL * 8; ++i) v[i] = __builtin_fmaf(v[i], 1.0f + t[i], u[i]);
-        if (a.h) ch.template store<TB>(a.h, (size_t)row * a.ld_h, v);
-      }
-    }
-  }
-}
-
-// Gradients of a strip of rows.  What the parameters get are four sums over the rows of a group and channel:
-//   S1 = sum dh, S2 = sum dh rhat, T1 = sum dR, T2 = sum dR yhat   (dR: gradient of r)
-//   dshift = S1, dscale = weight S2 + bias S1, dgate = post_weight T2 + post_bias T1,
-//   dweight = sum over g of (1 + scale) S2, dbias the same of S1, dpost_weight = sum over g of gate T2, dpost_bias of T1.
-// They stay in registers while the strip is in one group and go to slot (workgroup + group), of which every pair that has
-// rows has one of its own, because neither number ever falls along the rows.
-template <int TS, int TB, int VPL>
-__global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_grad_kernel(GateNormArgs a) {
-  __shared__ float places[2][kMaxWaves][2];
-  const Channels<VPL> ch(a.C);
-  RowSum sum{places, 0, (int)(blockDim.x >> 6)};
-  constexpr int NC = VPL * 8;
-  float s1[NC] = {}, s2[NC] = {}, t1[NC] = {}, t2[NC] = {};
-  const float inv = 1.0f / (float)a.C;
-  const long long r0 = (long long)blockIdx.x * a.strip;
-  const long long r1 = min(r0 + a.strip, a.rows);
-  long long group_end;
-  int g = group_of(a, r0, group_end);
-  auto flush = [&] {
-    const size_t slot = (size_t)(blockIdx.x + (unsigned)g) * 4 * a.C;
-    ch.template store<SVG_F32>(a.partial, slot, s1);
-    ch.template store<SVG_F32>(a.partial, slot + a.C, s2);
-    ch.template store<SVG_F32>(a.partial, slot + 2 * (size_t)a.C, t1);
-    ch.template store<SVG_F32>(a.partial, slot + 3 * (size_t)a.C, t2);
-  };
-  for (long long row = r0; row < r1; ++row) {
-    const int now = row < group_end ? g : group_of(a, row, group_end);
-    if (now != g) {
-      flush();
-      g = now;
-#pragma unroll
-      for (int i = 0; i < NC; ++i) s1[i] = s2[i] = t1[i] = t2[i] = 0.f;
-    }
-    const size_t mod = (size_t)g * a.ld_mod;
-    float d[NC] = {}, t[NC];
-    if (a.dr) ch.template load<TS>(a.dr, (size_t)row * a.ld_r, d);
-    if (a.dh) {
-      float hat[NC], e[NC];
-      ch.template load<TS>(a.r_in, (size_t)row * a.ld_r, hat);
-      ch.template load<TB>(a.dh, (size_t)row * a.ld_h, e);
-      const float rho = normalise(hat, a.pre, a.eps, ch, sum);
-#pragma unroll
-      for (int i = 0; i < NC; ++i) {
-        s1[i] += e[i];
-        s2[i] = __builtin_fmaf(e[i], hat[i], s2[i]);
-      }
-      ch.table(a.scale, mod, 0.0f, t);
-#pragma unroll
-      for (int i = 0; i < NC; ++i) e[i] *= 1.0f + t[i];
-      if (a.pre != SVG_NORM_NONE) {
-        ch.table(a.weight, 0, 1.0f, t);
-        float m1 = 0.f, m2 = 0.f;
-#pragma unroll
-        for (int i = 0; i < NC; ++i) {
-          e[i] *= t[i];
-          m1 += e[i];
-          m2 = __builtin_fmaf(e[i], hat[i], m2);
-        }
-        sum(m1, m2);
-        m1 = a.pre == SVG_NORM_LAYER ? m1 * inv : 0.f;
-        m2 *= inv;
-#pragma unroll
-        for (int i = 0; i < NC; ++i) d[i] = __builtin_fmaf(rho, __builtin_fmaf(-hat[i], m2, e[i] - m1), d[i]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < NC; ++i) d[i] += e[i];
-      }
-    }
-    if (a.dx) {
-#pragma unroll
-      for (int i = 0; i < NC; ++i) t[i] = a.alpha * d[i];
-      ch.template store<TS>(a.dx, (size_t)row * a.ld_x, t);
-    }
-    if (a.y || a.dy) {
-      float hat[NC] = {}, rho = 1.0f;
-      if (a.y) {
-        ch.template load<TB>(a.y, (size_t)row * a.ld_y, hat);
-        rho = normalise(hat, a.post, a.post_eps, ch, sum);
-      }
-      // the padding's d is not zero under a layer form of Pre, so it is kept out of the sums
-#pragma unroll
-      for (int i = 0; i < NC; ++i) d[i] = ch.has(i / 8, i % 8) ? d[i] : 0.f;
-#pragma unroll
-      for (int i = 0; i < NC; ++i) {
-        t1[i] += d[i];
-        t2[i] = __builtin_fmaf(d[i], hat[i], t2[i]);
-      }
-      if (a.dy) {
-        ch.table(a.gate, mod, 1.0f, t);
-#pragma unroll
-        for (int i = 0; i < NC; ++i) d[i] *= t[i];
-        if (a.post != SVG_NORM_NONE) {
-          ch.table(a.post_weight, 0, 1.0f, t);
-          float m1 = 0.f, m2 = 0.f;
-#pragma unroll
-          for (int i = 0; i < NC; ++i) {
-            d[i] *= t[i];
-            m1 += d[i];
-            m2 = __builtin_fmaf(d[i], hat[i], m2);
-          }
-          sum(m1, m2);
-          m1 = a.post == SVG_NORM_LAYER ? m1 * inv : 0.f;
-          m2 *= inv;
-#pragma unroll
-          for (int i = 0; i < NC; ++i) d[i] = rho * __builtin_fmaf(-hat[i], m2, d[i] - m1);
-        }
-        ch.template store<TB>(a.dy, (size_t)row * a.ld_y, d);
-      }
-    }
-  }
-  flush();
-}
-
-// ---------------------------------------------------------------------------------------------------------------------
-// Rows that are 16-byte aligned.
-//
 // A workgroup holds a row, eight neighbouring channels a lane and 512 a wavefront (VPL times), and takes the rows of a
-// strip in turn.  Rows come through LDS: every wavefront asks
+// strip in turn.  Rows that are 16-byte aligned come through LDS: every wavefront asks
 // for its part of the row D rows ahead, straight from memory into a ring of its own, so that 80 to 120 KB are on their way to a
-// compute unit whatever registers the row in work needs.  (One row ahead in registers: 32760 x 5120 forward 538 us, backward 992.)
+// compute unit whatever registers the row in work needs.
 // A ring is written and read by its own wavefront alone: no barrier, a count of its outstanding operations is enough.
+// Rows of any other alignment (D = 0) come in registers, one row ahead, in loads of eight elements at any address.
 constexpr int kSegment = 512;         // channels of a wavefront and vector
 
 // The lane's eight channels of one tensor in the ring.
@@ -381,13 +107,15 @@ struct Rows {
   }
 };
 
-template <int VPL>
+// ANY: rows of any alignment and number of channels; otherwise whole, 16-byte aligned runs of eight.
+template <int VPL, bool ANY>
 struct Lane {
   static constexpr int N = VPL * 8;
   int first, step, C;                 // channel of vector v, element e: first + v step + e
   __device__ __forceinline__ Lane(int C_, int waves, int wave) : first((wave * 64 + (int)(threadIdx.x & 63)) * 8), step(waves * kSegment), C(C_) {}
   __device__ __forceinline__ int at(int i) const { return first + i / 8 * step + i % 8; }
-  __device__ __forceinline__ bool has(int i) const { return first + i / 8 * step < C; }
+  __device__ __forceinline__ bool has(int i) const { return (ANY ? at(i) : at(i / 8 * 8)) < C; }
+  __device__ __forceinline__ bool whole(int v) const { return at(v * 8) + (ANY ? 7 : 0) < C; }
   template <int TYPE>
   __device__ __forceinline__ void read(const unsigned char* ring, float (&x)[N]) const {
 #pragma unroll
@@ -398,22 +126,34 @@ struct Lane {
       for (int e = 0; e < 8; ++e) x[v * 8 + e] = t[e];
     }
   }
-  // Results are not kept in L2: a tensor of this size leaves it before it is read again.
+  // Results are not kept in L2: a tensor of this size leaves it before it is read again.  (Where they cross its lines L2 has to join them.)
   template <int TYPE>
   __device__ __forceinline__ void store(void* base, size_t row, const float (&x)[N]) const {
     char* const p = static_cast<char*>(base) + row * type_bytes(TYPE);
 #pragma unroll
     for (int v = 0; v < VPL; ++v) {
-      if (!has(v * 8)) continue;
-      block_u32x4* const q = reinterpret_cast<block_u32x4*>(p + (unsigned)at(v * 8) * (unsigned)type_bytes(TYPE));
-      const block_f32x8 f = {x[v * 8], x[v * 8 + 1], x[v * 8 + 2], x[v * 8 + 3], x[v * 8 + 4], x[v * 8 + 5], x[v * 8 + 6], x[v * 8 + 7]};
-      if constexpr (TYPE == SVG_F32) {
-        __builtin_nontemporal_store(__builtin_bit_cast(block_u32x4, block_f32x4{f[0], f[1], f[2], f[3]}), q);
-        __builtin_nontemporal_store(__builtin_bit_cast(block_u32x4, block_f32x4{f[4], f[5], f[6], f[7]}), q + 1);
-      } else if constexpr (TYPE == SVG_BF16) {
-        __builtin_nontemporal_store(__builtin_bit_cast(block_u32x4, __builtin_convertvector(f, block_bf16x8)), q);
+      const unsigned c = (unsigned)at(v * 8);
+      const float t[8] = {x[v * 8], x[v * 8 + 1], x[v * 8 + 2], x[v * 8 + 3], x[v * 8 + 4], x[v * 8 + 5], x[v * 8 + 6], x[v * 8 + 7]};
+      if constexpr (ANY) {
+        if (whole(v)) {
+          store8_any<TYPE>(p, c, t);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 7; ++e)
+            if (has(v * 8 + e)) store1<TYPE>(p, c + e, t[e]);
+        }
       } else {
-        __builtin_nontemporal_store(__builtin_bit_cast(block_u32x4, __builtin_convertvector(f, block_f16x8)), q);
+        if (!whole(v)) continue;
+        block_u32x4* const q = reinterpret_cast<block_u32x4*>(p + c * (unsigned)type_bytes(TYPE));
+        const block_f32x8 f = {t[0], t[1], t[2], t[3], t[4], t[5], t[6], t[7]};
+        if constexpr (TYPE == SVG_F32) {
+          __builtin_nontemporal_store(__builtin_bit_cast(block_u32x4, block_f32x4{f[0], f[1], f[2], f[3]}), q);
+          __builtin_nontemporal_store(__builtin_bit_cast(block_u32x4, block_f32x4{f[4], f[5], f[6], f[7]}), q + 1);
+        } else if constexpr (TYPE == SVG_BF16) {
+          __builtin_nontemporal_store(__builtin_bit_cast(block_u32x4, __builtin_convertvector(f, block_bf16x8)), q);
+        } else {
+          __builtin_nontemporal_store(__builtin_bit_cast(block_u32x4, __builtin_convertvector(f, block_f16x8)), q);
+        }
       }
     }
   }
@@ -422,13 +162,75 @@ struct Lane {
 #pragma unroll
     for (int v = 0; v < VPL; ++v) {
       float t[8] = {};
-      if (has(v * 8)) {
-        if (base) {
-          load8<SVG_F32>(base + row, (unsigned)at(v * 8), t);
+      const unsigned c = (unsigned)at(v * 8);
+      if (!base) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t[e] = has(v * 8 + e) ? otherwise : 0.f;
+      } else if (whole(v)) {
+        if constexpr (ANY) load8_any<SVG_F32>(base + row, c, t);
+        else load8<SVG_F32>(base + row, c, t);
+      } else if constexpr (ANY) {
+#pragma unroll
+        for (int e = 0; e < 7; ++e)
+          if (has(v * 8 + e)) t[e] = base[row + c + e];
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[v * 8 + e] = t[e];
+    }
+  }
+};
+
+// A lane's part of a row of any alignment, on its way into registers.  The lane that holds the row's end reads the row's last eight
+// elements and moves them to their places when they are used: loads of single elements would have to be waited for at once.  Where
+// some of the eight are another wavefront's, which may be writing the row in place, it takes its own one by one.
+template <int TYPE, int VPL>
+struct Coming {
+  using Word = std::conditional_t<TYPE == SVG_F32, block_u32x4_of4, block_u32x4_of2>;
+  static constexpr int kWords = TYPE == SVG_F32 ? 2 : 1;
+  block_u32x4 w[VPL][kWords];
+  __device__ __forceinline__ void ask(const void* base, size_t row, const Lane<VPL, true>& lane) {
+    const char* const p = static_cast<const char*>(base) + row * type_bytes(TYPE);
+#pragma unroll
+    for (int v = 0; v < VPL; ++v) {
+      const int c = lane.at(v * 8);
+#pragma unroll
+      for (int k = 0; k < kWords; ++k) w[v][k] = block_u32x4{};
+      if (base && c < lane.C) {
+        if (c + 8 <= lane.C || c % kSegment) {
+          const Word* const q = reinterpret_cast<const Word*>(p + (unsigned)min(c, lane.C - 8) * (unsigned)type_bytes(TYPE));
+#pragma unroll
+          for (int k = 0; k < kWords; ++k) w[v][k] = q[k];
         } else {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) t[e] = otherwise;
+          for (int e = 0; e < 7; ++e) {
+            if (c + e >= lane.C) continue;
+            if constexpr (TYPE == SVG_F32) w[v][e / 4][e % 4] = reinterpret_cast<const unsigned*>(p)[c + e];
+            else w[v][0][e / 2] |= (unsigned)reinterpret_cast<const unsigned short*>(p)[c + e] << (e % 2 * 16);
+          }
         }
+      }
+    }
+  }
+  __device__ __forceinline__ void read(const Lane<VPL, true>& lane, float (&x)[VPL * 8]) const {
+#pragma unroll
+    for (int v = 0; v < VPL; ++v) {
+      float t[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if constexpr (TYPE == SVG_F32) {
+          t[e] = __uint_as_float(w[v][e / 4][e % 4]);
+        } else {
+          const unsigned bits = w[v][0][e / 2];
+          if constexpr (TYPE == SVG_BF16) t[e] = __uint_as_float(e % 2 ? bits & 0xffff0000u : bits << 16);
+          else t[e] = (float)__builtin_bit_cast(_Float16, (unsigned short)(e % 2 ? bits >> 16 : bits));
+        }
+      }
+      if (lane.C % 8) {
+        const int c = lane.at(v * 8), past = c < lane.C && c % kSegment ? max(c + 8 - lane.C, 0) : 0;
+#pragma unroll
+        for (int by = 4; by; by /= 2)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) t[e] = past & by ? (e + by < 8 ? t[(e + by) & 7] : 0.f) : t[e];
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[v * 8 + e] = t[e];
@@ -467,8 +269,8 @@ struct Meeting {
 // A row's normalisation, v -> (v - mean) rho.  A wavefront takes the mean of its own n channels first and the squares of what is left
 // then, and the wavefronts' pairs are joined by  sum of squares = sum over w of (squares_w + n_w (mean_w - mean)^2): a row far
 // from zero loses nothing, and one meeting is enough.
-template <int VPL>
-__device__ __forceinline__ void own_statistics(const float (&v)[VPL * 8], int norm, const Lane<VPL>& lane, float inv_n, float& mean, float& squares) {
+template <int VPL, bool ANY>
+__device__ __forceinline__ void own_statistics(const float (&v)[VPL * 8], int norm, const Lane<VPL, ANY>& lane, float inv_n, float& mean, float& squares) {
   mean = squares = 0.f;
   if (norm == SVG_NORM_NONE) return;
   if (norm == SVG_NORM_LAYER) {
@@ -489,8 +291,8 @@ __device__ __forceinline__ void join_statistics(float& mean, float& squares, flo
   squares = wave_sum(__builtin_fmaf(n * d, d, squares));
   mean = all;
 }
-template <int VPL>
-__device__ __forceinline__ float apply_statistics(float (&v)[VPL * 8], int norm, float mean, float squares, float inv, float eps, const Lane<VPL>& lane) {
+template <int VPL, bool ANY>
+__device__ __forceinline__ float apply_statistics(float (&v)[VPL * 8], int norm, float mean, float squares, float inv, float eps, const Lane<VPL, ANY>& lane) {
   if (norm == SVG_NORM_NONE) return 1.0f;
   const float rho = 1.0f / sqrtf(squares * inv + eps);
 #pragma unroll
@@ -498,10 +300,10 @@ __device__ __forceinline__ float apply_statistics(float (&v)[VPL * 8], int norm,
   return rho;
 }
 
-template <int VPL>
+template <int VPL, bool ANY>
 struct Team {
   int wave;
-  Lane<VPL> lane;
+  Lane<VPL, ANY> lane;
   Meeting meet;
   float inv_n, n_of_lane, inv;        // 1 / channels of this wavefront; channels of wavefront `lane`; 1 / C
   __device__ __forceinline__ Team(const GateNormArgs& a, block_f32x4 (*places)[kMaxWaves])
@@ -518,12 +320,12 @@ struct Team {
   __device__ __forceinline__ float normalise(float (&v)[VPL * 8], int norm, float eps) {
     if (norm == SVG_NORM_NONE) return 1.0f;
     float mean, squares;
-    own_statistics<VPL>(v, norm, lane, inv_n, mean, squares);
+    own_statistics<VPL, ANY>(v, norm, lane, inv_n, mean, squares);
     const block_f32x4 all = meet.tell({mean, squares, 0.f, 0.f});
     mean = all[0];
     squares = all[1];
     join_statistics(mean, squares, n_of_lane, inv);
-    return apply_statistics<VPL>(v, norm, mean, squares, inv, eps, lane);
+    return apply_statistics<VPL, ANY>(v, norm, mean, squares, inv, eps, lane);
   }
 };
 
@@ -534,10 +336,11 @@ __device__ __forceinline__ void wait_ring() { asm volatile("s_waitcnt vmcnt(%0)"
 // The forward pass.  The tables of a group stay in registers, folded with the norms' weights: r = alpha x + (G1 yhat + G0),
 // h = H1 rhat + H0.
 template <int TS, int TB, int VPL, int D, bool FP4>
-__global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_ring_kernel(GateNormArgs a) {
+__global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_kernel(GateNormArgs a) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   __shared__ block_f32x4 places[2][kMaxWaves];
-  Team<VPL> team(a, places);
+  constexpr bool ANY = D == 0;
+  Team<VPL, ANY> team(a, places);
   constexpr int N = VPL * 8;
   using X = Rows<TS, VPL>;
   using Y = Rows<TB, VPL>;
@@ -549,9 +352,17 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_ring_kernel(GateNorm
   unsigned char* const ring = lds + (threadIdx.x >> 6) * (D * kSlot);
   const unsigned ring0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)ring);
   const long long r0 = (long long)blockIdx.x * a.strip;
+  Coming<TS, VPL> next_x;
+  Coming<TB, VPL> next_y;
   auto ask = [&](int k) {
     const bool there = k < a.strip && r0 + k < a.rows;
-    const unsigned to = ring0 + (unsigned)(k % D) * kSlot;
+    if constexpr (ANY) {
+      if (!there) return;
+      next_x.ask(a.x, (size_t)(r0 + k) * a.ld_x, team.lane);
+      next_y.ask(a.y, (size_t)(r0 + k) * a.ld_y, team.lane);
+      return;
+    }
+    const unsigned to = ring0 + (unsigned)(k % (ANY ? 1 : D)) * kSlot;
     xs.ask(r0 + k, there, a.C, a.waves, team.wave, to);
     ys.ask(r0 + k, there, a.C, a.waves, team.wave, to + X::bytes);
   };
@@ -560,7 +371,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_ring_kernel(GateNorm
   int group = -1;
   long long group_end = 0;
 #pragma unroll
-  for (int k = 0; k < D; ++k) ask(k);
+  for (int k = 0; k < (ANY ? 1 : D); ++k) ask(k);
   const int turns = (int)min((long long)a.strip, a.row_limit - r0);
   for (int k = 0; k < turns; ++k) {
     const long long row = r0 + k;
@@ -597,15 +408,21 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_ring_kernel(GateNorm
         }
       }
     }
-    // row k's loads are in front of those of D - 1 rows and, from row D on, of D rows' stores
-    if (counted && k >= D) wait_ring<(D - 1) * kLoads + D * kStores>();
-    else wait_ring<(D - 1) * kLoads>();
-    const unsigned char* const slot = ring + (unsigned)(k % D) * kSlot;
     float v[N], y[N];
-    team.lane.template read<TS>(slot, v);
-    team.lane.template read<TB>(slot + X::bytes, y);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // the slot has been read
-    ask(k + D);
+    if constexpr (ANY) {
+      next_x.read(team.lane, v);
+      next_y.read(team.lane, y);
+      ask(k + 1);
+    } else {
+      // row k's loads are in front of those of D - 1 rows and, from row D on, of D rows' stores
+      if (counted && k >= D) wait_ring<(D - 1) * kLoads + D * kStores>();
+      else wait_ring<(D - 1) * kLoads>();
+      const unsigned char* const slot = ring + (unsigned)(k % D) * kSlot;
+      team.lane.template read<TS>(slot, v);
+      team.lane.template read<TB>(slot + X::bytes, y);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the slot has been read
+      ask(k + D);
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] *= a.alpha;
     if (a.y) {
@@ -637,15 +454,21 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_ring_kernel(GateNorm
       }
     }
   }
-  wait_ring<0>();                     // no load to LDS outlives the workgroup
+  if constexpr (!ANY) wait_ring<0>();           // no load to LDS outlives the workgroup
 }
 
-// Gradients of the rows of a strip; the parameters' sums as in gate_norm_grad_kernel.
+// Gradients of a strip of rows.  What the parameters get are four sums over the rows of a group and channel:
+//   S1 = sum dh, S2 = sum dh rhat, T1 = sum dR, T2 = sum dR yhat   (dR: gradient of r)
+//   dshift = S1, dscale = weight S2 + bias S1, dgate = post_weight T2 + post_bias T1,
+//   dweight = sum over g of (1 + scale) S2, dbias the same of S1, dpost_weight = sum over g of gate T2, dpost_bias of T1.
+// They stay in registers while the strip is in one group and go to slot (workgroup + group), of which every pair that has
+// rows has one of its own, because neither number ever falls along the rows.
 template <int TS, int TB, int VPL, int D>
-__global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_grad_ring_kernel(GateNormArgs a) {
+__global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_grad_kernel(GateNormArgs a) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   __shared__ block_f32x4 places[2][kMaxWaves];
-  Team<VPL> team(a, places);
+  constexpr bool ANY = D == 0;
+  Team<VPL, ANY> team(a, places);
   constexpr int N = VPL * 8;
   using S = Rows<TS, VPL>;
   using B = Rows<TB, VPL>;
@@ -655,9 +478,19 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_grad_ring_kernel(Gat
   unsigned char* const ring = lds + (threadIdx.x >> 6) * (D * kSlot);
   const unsigned ring0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)ring);
   const long long r0 = (long long)blockIdx.x * a.strip;
+  Coming<TS, VPL> next_r, next_dr;
+  Coming<TB, VPL> next_y, next_dh;
   auto ask = [&](int k) {
     const bool there = k < a.strip && r0 + k < a.rows;
-    const unsigned to = ring0 + (unsigned)(k % D) * kSlot;
+    if constexpr (ANY) {
+      if (!there) return;
+      next_r.ask(a.r_in, (size_t)(r0 + k) * a.ld_r, team.lane);
+      next_dr.ask(a.dr, (size_t)(r0 + k) * a.ld_r, team.lane);
+      next_y.ask(a.y, (size_t)(r0 + k) * a.ld_y, team.lane);
+      next_dh.ask(a.dh, (size_t)(r0 + k) * a.ld_h, team.lane);
+      return;
+    }
+    const unsigned to = ring0 + (unsigned)(k % (ANY ? 1 : D)) * kSlot;
     rs.ask(r0 + k, there, a.C, a.waves, team.wave, to);
     drs.ask(r0 + k, there, a.C, a.waves, team.wave, to + S::bytes);
     ys.ask(r0 + k, there, a.C, a.waves, team.wave, to + 2 * S::bytes);
@@ -677,7 +510,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_grad_ring_kernel(Gat
   const int pre = a.dh ? a.pre : SVG_NORM_NONE, post = a.y ? a.post : SVG_NORM_NONE;
   const bool counted = a.dx && a.dy;
 #pragma unroll
-  for (int k = 0; k < D; ++k) ask(k);
+  for (int k = 0; k < (ANY ? 1 : D); ++k) ask(k);
   const int turns = (int)min((long long)a.strip, a.rows - r0);
   for (int k = 0; k < turns; ++k) {
     const long long row = r0 + k;
@@ -703,22 +536,30 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_grad_ring_kernel(Gat
         for (int i = 0; i < N; ++i) f1[i] *= t[i];
       }
     }
-    if (counted && k >= D) wait_ring<(D - 1) * kLoads + D * kStores>();
-    else wait_ring<(D - 1) * kLoads>();
-    const unsigned char* const slot = ring + (unsigned)(k % D) * kSlot;
     float rhat[N], d[N], yhat[N], e[N];
-    team.lane.template read<TS>(slot, rhat);
-    team.lane.template read<TS>(slot + S::bytes, d);
-    team.lane.template read<TB>(slot + 2 * S::bytes, yhat);
-    team.lane.template read<TB>(slot + 2 * S::bytes + B::bytes, e);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    ask(k + D);
+    if constexpr (ANY) {
+      next_r.read(team.lane, rhat);
+      next_dr.read(team.lane, d);
+      next_y.read(team.lane, yhat);
+      next_dh.read(team.lane, e);
+      ask(k + 1);
+    } else {
+      if (counted && k >= D) wait_ring<(D - 1) * kLoads + D * kStores>();
+      else wait_ring<(D - 1) * kLoads>();
+      const unsigned char* const slot = ring + (unsigned)(k % D) * kSlot;
+      team.lane.template read<TS>(slot, rhat);
+      team.lane.template read<TS>(slot + S::bytes, d);
+      team.lane.template read<TB>(slot + 2 * S::bytes, yhat);
+      team.lane.template read<TB>(slot + 2 * S::bytes + B::bytes, e);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      ask(k + D);
+    }
     // both normalisations' statistics in one meeting; a row that does not exist is zeros
     float rho = 1.0f, rho_y = 1.0f;
     if (pre != SVG_NORM_NONE || post != SVG_NORM_NONE) {
       float mr, sr, my, sy;
-      own_statistics<VPL>(rhat, pre, team.lane, team.inv_n, mr, sr);
-      own_statistics<VPL>(yhat, post, team.lane, team.inv_n, my, sy);
+      own_statistics<VPL, ANY>(rhat, pre, team.lane, team.inv_n, mr, sr);
+      own_statistics<VPL, ANY>(yhat, post, team.lane, team.inv_n, my, sy);
       const block_f32x4 all = team.meet.tell({mr, sr, my, sy});
       mr = all[0];
       sr = all[1];
@@ -726,8 +567,8 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_grad_ring_kernel(Gat
       sy = all[3];
       if (pre != SVG_NORM_NONE) join_statistics(mr, sr, team.n_of_lane, team.inv);
       if (post != SVG_NORM_NONE) join_statistics(my, sy, team.n_of_lane, team.inv);
-      rho = apply_statistics<VPL>(rhat, pre, mr, sr, team.inv, a.eps, team.lane);
-      rho_y = apply_statistics<VPL>(yhat, post, my, sy, team.inv, a.post_eps, team.lane);
+      rho = apply_statistics<VPL, ANY>(rhat, pre, mr, sr, team.inv, a.eps, team.lane);
+      rho_y = apply_statistics<VPL, ANY>(yhat, post, my, sy, team.inv, a.post_eps, team.lane);
     }
     if (a.dh) {
 #pragma unroll
@@ -786,7 +627,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_grad_ring_kernel(Gat
       if (there) team.lane.template store<TB>(a.dy, (size_t)row * a.ld_y, d);
     }
   }
-  wait_ring<0>();
+  if constexpr (!ANY) wait_ring<0>();
   if (group >= 0) flush();
 }
 
@@ -988,7 +829,8 @@ void dispatch(const svg_gate_norm_t& d, int vpl, F f) {
 // f(depth) as an integral constant
 template <class F>
 void with_depth(int depth, F f) {
-  if (depth == 1) f(std::integral_constant<int, 1>{});
+  if (depth == 0) f(std::integral_constant<int, 0>{});
+  else if (depth == 1) f(std::integral_constant<int, 1>{});
   else if (depth == 2) f(std::integral_constant<int, 2>{});
   else f(std::integral_constant<int, 3>{});
 }
@@ -1014,7 +856,7 @@ hipError_t launch_with_lds(void (*kernel)(GateNormArgs), std::atomic<unsigned lo
 constexpr int kGradLeast = 2;         // rows of a strip of the backward pass: its sums cost the traffic of two
 struct GradShape {
   RowShape row;
-  int strip, splits, slot, depth;     // depth 0: the general kernel
+  int strip, splits, slot, depth;     // depth 0: rows through registers
   long long strips;
 };
 GradShape grad_shape(const svg_gate_norm_t& d) {
@@ -1050,28 +892,22 @@ int launch_gate_norm(const svg_gate_norm_t& d, const void* x, const void* y, voi
   if (codes && (!vec || d.C % 32)) return SVG_ERR_UNSUPPORTED;
   if (codes) a.row_limit = fp4_row_tiles(d.rows) * kFp4Rows;
   const RowShape s = row_shape(d.C);
-  const int slot = s.vpl * kSegment * (type_bytes(d.stream_type) + 2), depth = ring_depth(s.waves, slot);
-  const bool general = !vec;
+  const int slot = s.vpl * kSegment * (type_bytes(d.stream_type) + 2), depth = vec ? ring_depth(s.waves, slot) : 0;
   a.waves = s.waves;
   // Rows few enough for three generations of workgroups are taken one each (1573 x 1536 11.4 us instead of 14.9, 6000 x 2048
   // 22.2 instead of 20.6).
-  a.strip = strip_rows(a.row_limit, s.waves, 20, general ? 0 : s.waves * depth * slot);
+  a.strip = strip_rows(a.row_limit, s.waves, 20, s.waves * depth * slot);
   if (a.strip <= 3) a.strip = 1;
   const dim3 grid((unsigned)((a.row_limit + a.strip - 1) / a.strip)), block((unsigned)(64 * s.waves));
   hipError_t e = hipSuccess;
   (void)hipGetLastError();
   dispatch(d, s.vpl, [&](auto ts, auto tb, auto vpl) {
     constexpr int TS = decltype(ts)::value, TB = decltype(tb)::value, VPL = decltype(vpl)::value;
-    if (general) {
-      hipLaunchKernelGGL((gate_norm_kernel<TS, TB, VPL>), grid, block, 0, stream, a);
-      e = hipGetLastError();
-      return;
-    }
     with_depth(depth, [&](auto dc) {
       constexpr int D = decltype(dc)::value;
       static std::atomic<unsigned long long> allowed[2];
-      e = launch_with_lds(codes ? gate_norm_ring_kernel<TS, TB, VPL, D, true> : gate_norm_ring_kernel<TS, TB, VPL, D, false>, allowed[codes != nullptr],
-                          grid, block, s.waves * D * slot, stream, a);
+      constexpr bool F = D > 0;        // a 4-bit output only where rows are aligned
+      e = launch_with_lds(codes ? gate_norm_kernel<TS, TB, VPL, D, F> : gate_norm_kernel<TS, TB, VPL, D, false>, allowed[codes != nullptr], grid, block, s.waves * D * slot, stream, a);
     });
   });
   return hip_status(e);
@@ -1083,7 +919,6 @@ int launch_gate_norm_grad(const svg_gate_norm_t& d, const void* r, const void* y
   a.r_in = r; a.y = y; a.dr = dr; a.dh = dh; a.dx = dx; a.dy = dy;
   a.partial = workspace;
   const GradShape g = grad_shape(d);
-  const bool general = !aligned(a) || !g.depth;
   a.waves = g.row.waves;
   a.strip = g.strip;
   (void)hipGetLastError();
@@ -1092,15 +927,10 @@ int launch_gate_norm_grad(const svg_gate_norm_t& d, const void* r, const void* y
     hipError_t e = hipSuccess;
     dispatch(d, g.row.vpl, [&](auto ts, auto tb, auto vpl) {
       constexpr int TS = decltype(ts)::value, TB = decltype(tb)::value, VPL = decltype(vpl)::value;
-      if (general) {
-        hipLaunchKernelGGL((gate_norm_grad_kernel<TS, TB, VPL>), grid, block, 0, stream, a);
-        e = hipGetLastError();
-        return;
-      }
-      with_depth(g.depth, [&](auto dc) {
+      with_depth(aligned(a) ? g.depth : 0, [&](auto dc) {
         constexpr int D = decltype(dc)::value;
         static std::atomic<unsigned long long> allowed;
-        e = launch_with_lds(gate_norm_grad_ring_kernel<TS, TB, VPL, D>, allowed, grid, block, g.row.waves * D * g.slot, stream, a);
+        e = launch_with_lds(gate_norm_grad_kernel<TS, TB, VPL, D>, allowed, grid, block, g.row.waves * D * g.slot, stream, a);
       });
     });
     if (e != hipSuccess) return hip_status(e);
