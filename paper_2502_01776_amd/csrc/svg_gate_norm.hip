@@ -13,6 +13,7 @@ namespace svg {
 namespace {
 
 constexpr int kMaxWaves = 16;         // wavefronts of a workgroup
+constexpr int kMaxChannels = 16384;
 
 struct GateNormArgs {
   long long rows;
@@ -61,14 +62,21 @@ __device__ __forceinline__ int group_of(const GateNormArgs& a, long long row, lo
 // for its part of the row D rows ahead, straight from memory into a ring of its own, so that 80 to 120 KB are on their way to a
 // compute unit whatever registers the row in work needs.
 // A ring is written and read by its own wavefront alone: no barrier, a count of its outstanding operations is enough.
-// Rows of any other alignment (D = 0) come in registers, one row ahead, in loads of eight elements at any address.
+// Rows of any other alignment come from the 16-byte granules that they touch: the granules of 504 channels fill the same 1 or 2 KB
+// wherever the row begins, and are read out of LDS from its first byte on.  Rows that LDS has no place for, or of more channels than 16
+// wavefronts of two such vectors hold, come in registers, one row ahead, in loads of eight elements at any address.
+// (In registers, 32760 x 5119 takes 377 us forward and 1024 backward.)
 constexpr int kSegment = 512;         // channels of a wavefront and vector
+enum Form { kWhole, kShifted, kSingle };                  // aligned rows; granules in LDS; in registers
+__host__ __device__ constexpr int segment(Form form) { return form == kShifted ? 504 : kSegment; }
 
 // The lane's eight channels of one tensor in the ring.
-template <int TYPE>
+template <int TYPE, bool ANY>
 __device__ __forceinline__ void read_ring(const unsigned char* at, float (&x)[8]) {
   const int lane = threadIdx.x & 63;
-  if constexpr (TYPE == SVG_F32) {
+  if constexpr (ANY) {                // lane 63 has none
+    load8_any<TYPE>(at, (unsigned)min(lane, 62) * 8, x);
+  } else if constexpr (TYPE == SVG_F32) {
     const block_f32x4* p = reinterpret_cast<const block_f32x4*>(at + lane * 32);
     const block_f32x4 lo = p[0], hi = p[1];
 #pragma unroll
@@ -89,30 +97,39 @@ __device__ __forceinline__ void read_ring(const unsigned char* at, float (&x)[8]
 
 // A tensor's rows: the wavefront's part of one goes to the ring in loads of 1 KB; what is behind the last channel, or of a
 // row that does not exist, arrives as zeros.
-template <int TYPE, int VPL>
+template <int TYPE, int VPL, Form FORM>
 struct Rows {
   static constexpr int size = type_bytes(TYPE);
   static constexpr int loads = VPL * kSegment * 2 / 1024 * (size / 2);
   static constexpr int bytes = VPL * kSegment * size;
   const char* base;
   size_t step;                        // bytes of a row
+  // bytes from the row's first granule to its first element
+  __device__ __forceinline__ unsigned shift(long long row) const {
+    return FORM == kShifted ? (unsigned)(reinterpret_cast<uintptr_t>(base) + (size_t)row * step) & 15u : 0u;
+  }
   __device__ __forceinline__ void ask(long long row, bool there, int C, int waves, int wave, unsigned to) const {
-    const auto rsrc = attn::buffer_words(base + (there ? (size_t)row * step : 0), there && base ? (unsigned)C * size : 0u);
+    const unsigned past = there ? shift(row) : 0;         // granules lie in the allocation that their elements lie in
+    const auto rsrc = attn::buffer_words(base + (there ? (size_t)row * step - past : 0),
+                                         there && base ? (past + (unsigned)C * size + 3u) & ~3u : 0u);
     const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int v = 0; v < VPL; ++v)
 #pragma unroll
       for (int l = 0; l < loads / VPL; ++l)
-        load_one_to_lds(rsrc, lane * 16, (wave + v * waves) * kSegment * size + l * 1024, to + v * kSegment * size + l * 1024);
+        load_one_to_lds(rsrc, lane * 16, (wave + v * waves) * segment(FORM) * size + l * 1024, to + v * kSegment * size + l * 1024);
   }
 };
 
-// ANY: rows of any alignment and number of channels; otherwise whole, 16-byte aligned runs of eight.
-template <int VPL, bool ANY>
+template <int VPL, Form FORM>
 struct Lane {
   static constexpr int N = VPL * 8;
+  static constexpr bool ANY = FORM != kWhole;
   int first, step, C;                 // channel of vector v, element e: first + v step + e
-  __device__ __forceinline__ Lane(int C_, int waves, int wave) : first((wave * 64 + (int)(threadIdx.x & 63)) * 8), step(waves * kSegment), C(C_) {}
+  __device__ __forceinline__ Lane(int C_, int waves, int wave) : step(waves * segment(FORM)), C(C_) {
+    const int lane = threadIdx.x & 63;
+    first = lane * 8 < segment(FORM) ? wave * segment(FORM) + lane * 8 : kMaxChannels;
+  }
   __device__ __forceinline__ int at(int i) const { return first + i / 8 * step + i % 8; }
   __device__ __forceinline__ bool has(int i) const { return (ANY ? at(i) : at(i / 8 * 8)) < C; }
   __device__ __forceinline__ bool whole(int v) const { return at(v * 8) + (ANY ? 7 : 0) < C; }
@@ -121,12 +138,13 @@ struct Lane {
 #pragma unroll
     for (int v = 0; v < VPL; ++v) {
       float t[8];
-      read_ring<TYPE>(ring + v * kSegment * type_bytes(TYPE), t);
+      read_ring<TYPE, ANY>(ring + v * kSegment * type_bytes(TYPE), t);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[v * 8 + e] = t[e];
+      for (int e = 0; e < 8; ++e) x[v * 8 + e] = !ANY || has(v * 8 + e) ? t[e] : 0.f;
     }
   }
-  // Results are not kept in L2: a tensor of this size leaves it before it is read again.  (Where they cross its lines L2 has to join them.)
+  // Results of 16 bits are not kept in L2: a tensor of this size leaves it before it is read again.  Where a line is
+  // written in parts (fp32: half of it by each store; rows off its borders), L2 has to join them.
   template <int TYPE>
   __device__ __forceinline__ void store(void* base, size_t row, const float (&x)[N]) const {
     char* const p = static_cast<char*>(base) + row * type_bytes(TYPE);
@@ -147,8 +165,8 @@ struct Lane {
         block_u32x4* const q = reinterpret_cast<block_u32x4*>(p + c * (unsigned)type_bytes(TYPE));
         const block_f32x8 f = {t[0], t[1], t[2], t[3], t[4], t[5], t[6], t[7]};
         if constexpr (TYPE == SVG_F32) {
-          __builtin_nontemporal_store(__builtin_bit_cast(block_u32x4, block_f32x4{f[0], f[1], f[2], f[3]}), q);
-          __builtin_nontemporal_store(__builtin_bit_cast(block_u32x4, block_f32x4{f[4], f[5], f[6], f[7]}), q + 1);
+          q[0] = __builtin_bit_cast(block_u32x4, block_f32x4{f[0], f[1], f[2], f[3]});
+          q[1] = __builtin_bit_cast(block_u32x4, block_f32x4{f[4], f[5], f[6], f[7]});
         } else if constexpr (TYPE == SVG_BF16) {
           __builtin_nontemporal_store(__builtin_bit_cast(block_u32x4, __builtin_convertvector(f, block_bf16x8)), q);
         } else {
@@ -188,7 +206,7 @@ struct Coming {
   using Word = std::conditional_t<TYPE == SVG_F32, block_u32x4_of4, block_u32x4_of2>;
   static constexpr int kWords = TYPE == SVG_F32 ? 2 : 1;
   block_u32x4 w[VPL][kWords];
-  __device__ __forceinline__ void ask(const void* base, size_t row, const Lane<VPL, true>& lane) {
+  __device__ __forceinline__ void ask(const void* base, size_t row, const Lane<VPL, kSingle>& lane) {
     const char* const p = static_cast<const char*>(base) + row * type_bytes(TYPE);
 #pragma unroll
     for (int v = 0; v < VPL; ++v) {
@@ -211,7 +229,7 @@ struct Coming {
       }
     }
   }
-  __device__ __forceinline__ void read(const Lane<VPL, true>& lane, float (&x)[VPL * 8]) const {
+  __device__ __forceinline__ void read(const Lane<VPL, kSingle>& lane, float (&x)[VPL * 8]) const {
 #pragma unroll
     for (int v = 0; v < VPL; ++v) {
       float t[8];
@@ -269,8 +287,8 @@ struct Meeting {
 // A row's normalisation, v -> (v - mean) rho.  A wavefront takes the mean of its own n channels first and the squares of what is left
 // then, and the wavefronts' pairs are joined by  sum of squares = sum over w of (squares_w + n_w (mean_w - mean)^2): a row far
 // from zero loses nothing, and one meeting is enough.
-template <int VPL, bool ANY>
-__device__ __forceinline__ void own_statistics(const float (&v)[VPL * 8], int norm, const Lane<VPL, ANY>& lane, float inv_n, float& mean, float& squares) {
+template <int VPL, Form FORM>
+__device__ __forceinline__ void own_statistics(const float (&v)[VPL * 8], int norm, const Lane<VPL, FORM>& lane, float inv_n, float& mean, float& squares) {
   mean = squares = 0.f;
   if (norm == SVG_NORM_NONE) return;
   if (norm == SVG_NORM_LAYER) {
@@ -291,8 +309,8 @@ __device__ __forceinline__ void join_statistics(float& mean, float& squares, flo
   squares = wave_sum(__builtin_fmaf(n * d, d, squares));
   mean = all;
 }
-template <int VPL, bool ANY>
-__device__ __forceinline__ float apply_statistics(float (&v)[VPL * 8], int norm, float mean, float squares, float inv, float eps, const Lane<VPL, ANY>& lane) {
+template <int VPL, Form FORM>
+__device__ __forceinline__ float apply_statistics(float (&v)[VPL * 8], int norm, float mean, float squares, float inv, float eps, const Lane<VPL, FORM>& lane) {
   if (norm == SVG_NORM_NONE) return 1.0f;
   const float rho = 1.0f / sqrtf(squares * inv + eps);
 #pragma unroll
@@ -300,17 +318,17 @@ __device__ __forceinline__ float apply_statistics(float (&v)[VPL * 8], int norm,
   return rho;
 }
 
-template <int VPL, bool ANY>
+template <int VPL, Form FORM>
 struct Team {
   int wave;
-  Lane<VPL, ANY> lane;
+  Lane<VPL, FORM> lane;
   Meeting meet;
   float inv_n, n_of_lane, inv;        // 1 / channels of this wavefront; channels of wavefront `lane`; 1 / C
   __device__ __forceinline__ Team(const GateNormArgs& a, block_f32x4 (*places)[kMaxWaves])
       : wave(__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6))), lane(a.C, a.waves, wave), meet{places, 0, a.waves, wave} {
     auto channels = [&](int w) {
       int n = 0;
-      for (int v = 0; v < VPL; ++v) n += min(max(a.C - (w + v * a.waves) * kSegment, 0), kSegment);
+      for (int v = 0; v < VPL; ++v) n += min(max(a.C - (w + v * a.waves) * segment(FORM), 0), segment(FORM));
       return (float)n;
     };
     inv_n = 1.0f / channels(wave);
@@ -320,12 +338,12 @@ struct Team {
   __device__ __forceinline__ float normalise(float (&v)[VPL * 8], int norm, float eps) {
     if (norm == SVG_NORM_NONE) return 1.0f;
     float mean, squares;
-    own_statistics<VPL, ANY>(v, norm, lane, inv_n, mean, squares);
+    own_statistics<VPL, FORM>(v, norm, lane, inv_n, mean, squares);
     const block_f32x4 all = meet.tell({mean, squares, 0.f, 0.f});
     mean = all[0];
     squares = all[1];
     join_statistics(mean, squares, n_of_lane, inv);
-    return apply_statistics<VPL, ANY>(v, norm, mean, squares, inv, eps, lane);
+    return apply_statistics<VPL, FORM>(v, norm, mean, squares, inv, eps, lane);
   }
 };
 
@@ -335,20 +353,20 @@ __device__ __forceinline__ void wait_ring() { asm volatile("s_waitcnt vmcnt(%0)"
 
 // The forward pass.  The tables of a group stay in registers, folded with the norms' weights: r = alpha x + (G1 yhat + G0),
 // h = H1 rhat + H0.
-template <int TS, int TB, int VPL, int D, bool FP4>
+template <int TS, int TB, int VPL, int D, Form FORM, bool FP4>
 __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_kernel(GateNormArgs a) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   __shared__ block_f32x4 places[2][kMaxWaves];
-  constexpr bool ANY = D == 0;
-  Team<VPL, ANY> team(a, places);
+  constexpr bool SINGLE = FORM == kSingle;
+  Team<VPL, FORM> team(a, places);
   constexpr int N = VPL * 8;
-  using X = Rows<TS, VPL>;
-  using Y = Rows<TB, VPL>;
+  using X = Rows<TS, VPL, FORM>;
+  using Y = Rows<TB, VPL, FORM>;
   const X xs{static_cast<const char*>(a.x), (size_t)a.ld_x * X::size};
   const Y ys{static_cast<const char*>(a.y), (size_t)a.ld_y * Y::size};
   constexpr int kSlot = X::bytes + Y::bytes, kLoads = X::loads + Y::loads;
   // stores of a row at least, where r and h (or its 4-bit form) are wanted: only the first vector is sure to have a channel
-  constexpr int kStores = X::size / 2 + (FP4 ? 2 : 1);
+  constexpr int kStores = FORM == kWhole ? X::size / 2 + (FP4 ? 2 : 1) : 2;
   unsigned char* const ring = lds + (threadIdx.x >> 6) * (D * kSlot);
   const unsigned ring0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)ring);
   const long long r0 = (long long)blockIdx.x * a.strip;
@@ -356,13 +374,13 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_kernel(GateNormArgs 
   Coming<TB, VPL> next_y;
   auto ask = [&](int k) {
     const bool there = k < a.strip && r0 + k < a.rows;
-    if constexpr (ANY) {
+    if constexpr (SINGLE) {
       if (!there) return;
       next_x.ask(a.x, (size_t)(r0 + k) * a.ld_x, team.lane);
       next_y.ask(a.y, (size_t)(r0 + k) * a.ld_y, team.lane);
       return;
     }
-    const unsigned to = ring0 + (unsigned)(k % (ANY ? 1 : D)) * kSlot;
+    const unsigned to = ring0 + (unsigned)(k % (SINGLE ? 1 : D)) * kSlot;
     xs.ask(r0 + k, there, a.C, a.waves, team.wave, to);
     ys.ask(r0 + k, there, a.C, a.waves, team.wave, to + X::bytes);
   };
@@ -371,7 +389,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_kernel(GateNormArgs 
   int group = -1;
   long long group_end = 0;
 #pragma unroll
-  for (int k = 0; k < (ANY ? 1 : D); ++k) ask(k);
+  for (int k = 0; k < (SINGLE ? 1 : D); ++k) ask(k);
   const int turns = (int)min((long long)a.strip, a.row_limit - r0);
   for (int k = 0; k < turns; ++k) {
     const long long row = r0 + k;
@@ -409,7 +427,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_kernel(GateNormArgs 
       }
     }
     float v[N], y[N];
-    if constexpr (ANY) {
+    if constexpr (SINGLE) {
       next_x.read(team.lane, v);
       next_y.read(team.lane, y);
       ask(k + 1);
@@ -418,8 +436,8 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_kernel(GateNormArgs 
       if (counted && k >= D) wait_ring<(D - 1) * kLoads + D * kStores>();
       else wait_ring<(D - 1) * kLoads>();
       const unsigned char* const slot = ring + (unsigned)(k % D) * kSlot;
-      team.lane.template read<TS>(slot, v);
-      team.lane.template read<TB>(slot + X::bytes, y);
+      team.lane.template read<TS>(slot + xs.shift(row), v);
+      team.lane.template read<TB>(slot + X::bytes + ys.shift(row), y);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the slot has been read
       ask(k + D);
     }
@@ -454,7 +472,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_kernel(GateNormArgs 
       }
     }
   }
-  if constexpr (!ANY) wait_ring<0>();           // no load to LDS outlives the workgroup
+  if constexpr (!SINGLE) wait_ring<0>();           // no load to LDS outlives the workgroup
 }
 
 // Gradients of a strip of rows.  What the parameters get are four sums over the rows of a group and channel:
@@ -463,18 +481,18 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_kernel(GateNormArgs 
 //   dweight = sum over g of (1 + scale) S2, dbias the same of S1, dpost_weight = sum over g of gate T2, dpost_bias of T1.
 // They stay in registers while the strip is in one group and go to slot (workgroup + group), of which every pair that has
 // rows has one of its own, because neither number ever falls along the rows.
-template <int TS, int TB, int VPL, int D>
+template <int TS, int TB, int VPL, int D, Form FORM>
 __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_grad_kernel(GateNormArgs a) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   __shared__ block_f32x4 places[2][kMaxWaves];
-  constexpr bool ANY = D == 0;
-  Team<VPL, ANY> team(a, places);
+  constexpr bool SINGLE = FORM == kSingle;
+  Team<VPL, FORM> team(a, places);
   constexpr int N = VPL * 8;
-  using S = Rows<TS, VPL>;
-  using B = Rows<TB, VPL>;
+  using S = Rows<TS, VPL, FORM>;
+  using B = Rows<TB, VPL, FORM>;
   const S rs{static_cast<const char*>(a.r_in), (size_t)a.ld_r * S::size}, drs{static_cast<const char*>(a.dr), (size_t)a.ld_r * S::size};
   const B ys{static_cast<const char*>(a.y), (size_t)a.ld_y * B::size}, dhs{static_cast<const char*>(a.dh), (size_t)a.ld_h * B::size};
-  constexpr int kSlot = 2 * (S::bytes + B::bytes), kLoads = 2 * (S::loads + B::loads), kStores = S::size / 2 + 1;
+  constexpr int kSlot = 2 * (S::bytes + B::bytes), kLoads = 2 * (S::loads + B::loads), kStores = FORM == kWhole ? S::size / 2 + 1 : 2;
   unsigned char* const ring = lds + (threadIdx.x >> 6) * (D * kSlot);
   const unsigned ring0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)ring);
   const long long r0 = (long long)blockIdx.x * a.strip;
@@ -482,7 +500,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_grad_kernel(GateNorm
   Coming<TB, VPL> next_y, next_dh;
   auto ask = [&](int k) {
     const bool there = k < a.strip && r0 + k < a.rows;
-    if constexpr (ANY) {
+    if constexpr (SINGLE) {
       if (!there) return;
       next_r.ask(a.r_in, (size_t)(r0 + k) * a.ld_r, team.lane);
       next_dr.ask(a.dr, (size_t)(r0 + k) * a.ld_r, team.lane);
@@ -490,7 +508,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_grad_kernel(GateNorm
       next_dh.ask(a.dh, (size_t)(r0 + k) * a.ld_h, team.lane);
       return;
     }
-    const unsigned to = ring0 + (unsigned)(k % (ANY ? 1 : D)) * kSlot;
+    const unsigned to = ring0 + (unsigned)(k % (SINGLE ? 1 : D)) * kSlot;
     rs.ask(r0 + k, there, a.C, a.waves, team.wave, to);
     drs.ask(r0 + k, there, a.C, a.waves, team.wave, to + S::bytes);
     ys.ask(r0 + k, there, a.C, a.waves, team.wave, to + 2 * S::bytes);
@@ -510,7 +528,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_grad_kernel(GateNorm
   const int pre = a.dh ? a.pre : SVG_NORM_NONE, post = a.y ? a.post : SVG_NORM_NONE;
   const bool counted = a.dx && a.dy;
 #pragma unroll
-  for (int k = 0; k < (ANY ? 1 : D); ++k) ask(k);
+  for (int k = 0; k < (SINGLE ? 1 : D); ++k) ask(k);
   const int turns = (int)min((long long)a.strip, a.rows - r0);
   for (int k = 0; k < turns; ++k) {
     const long long row = r0 + k;
@@ -537,7 +555,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_grad_kernel(GateNorm
       }
     }
     float rhat[N], d[N], yhat[N], e[N];
-    if constexpr (ANY) {
+    if constexpr (SINGLE) {
       next_r.read(team.lane, rhat);
       next_dr.read(team.lane, d);
       next_y.read(team.lane, yhat);
@@ -547,10 +565,10 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_grad_kernel(GateNorm
       if (counted && k >= D) wait_ring<(D - 1) * kLoads + D * kStores>();
       else wait_ring<(D - 1) * kLoads>();
       const unsigned char* const slot = ring + (unsigned)(k % D) * kSlot;
-      team.lane.template read<TS>(slot, rhat);
-      team.lane.template read<TS>(slot + S::bytes, d);
-      team.lane.template read<TB>(slot + 2 * S::bytes, yhat);
-      team.lane.template read<TB>(slot + 2 * S::bytes + B::bytes, e);
+      team.lane.template read<TS>(slot + rs.shift(row), rhat);
+      team.lane.template read<TS>(slot + S::bytes + drs.shift(row), d);
+      team.lane.template read<TB>(slot + 2 * S::bytes + ys.shift(row), yhat);
+      team.lane.template read<TB>(slot + 2 * S::bytes + B::bytes + dhs.shift(row), e);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       ask(k + D);
     }
@@ -558,8 +576,8 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_grad_kernel(GateNorm
     float rho = 1.0f, rho_y = 1.0f;
     if (pre != SVG_NORM_NONE || post != SVG_NORM_NONE) {
       float mr, sr, my, sy;
-      own_statistics<VPL, ANY>(rhat, pre, team.lane, team.inv_n, mr, sr);
-      own_statistics<VPL, ANY>(yhat, post, team.lane, team.inv_n, my, sy);
+      own_statistics<VPL, FORM>(rhat, pre, team.lane, team.inv_n, mr, sr);
+      own_statistics<VPL, FORM>(yhat, post, team.lane, team.inv_n, my, sy);
       const block_f32x4 all = team.meet.tell({mr, sr, my, sy});
       mr = all[0];
       sr = all[1];
@@ -567,8 +585,8 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_grad_kernel(GateNorm
       sy = all[3];
       if (pre != SVG_NORM_NONE) join_statistics(mr, sr, team.n_of_lane, team.inv);
       if (post != SVG_NORM_NONE) join_statistics(my, sy, team.n_of_lane, team.inv);
-      rho = apply_statistics<VPL, ANY>(rhat, pre, mr, sr, team.inv, a.eps, team.lane);
-      rho_y = apply_statistics<VPL, ANY>(yhat, post, my, sy, team.inv, a.post_eps, team.lane);
+      rho = apply_statistics<VPL, FORM>(rhat, pre, mr, sr, team.inv, a.eps, team.lane);
+      rho_y = apply_statistics<VPL, FORM>(yhat, post, my, sy, team.inv, a.post_eps, team.lane);
     }
     if (a.dh) {
 #pragma unroll
@@ -627,7 +645,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_grad_kernel(GateNorm
       if (there) team.lane.template store<TB>(a.dy, (size_t)row * a.ld_y, d);
     }
   }
-  if constexpr (!ANY) wait_ring<0>();
+  if constexpr (!SINGLE) wait_ring<0>();
   if (group >= 0) flush();
 }
 
@@ -768,8 +786,8 @@ __global__ __launch_bounds__(kSumLanes* kSumChannels) void grad_weights_kernel(G
 
 // Wavefronts of a workgroup, vectors of a lane: 512 channels a wavefront and vector, one vector up to 8192 channels, two up to 16384.
 struct RowShape { int waves, vpl; };
-RowShape row_shape(int C) {
-  const int vectors = (C + 511) / 512, vpl = vectors <= kMaxWaves ? 1 : 2;
+RowShape row_shape(int C, Form form = kWhole) {
+  const int vectors = (C + segment(form) - 1) / segment(form), vpl = vectors <= kMaxWaves ? 1 : 2;
   return {(vectors + vpl - 1) / vpl, vpl};
 }
 
@@ -826,13 +844,31 @@ void dispatch(const svg_gate_norm_t& d, int vpl, F f) {
   if (vpl == 1) with_types(std::integral_constant<int, 1>{});
   else with_types(std::integral_constant<int, 2>{});
 }
-// f(depth) as an integral constant
+// How a call's rows come: form, wavefronts, rows ahead.
+struct Way {
+  Form form;
+  RowShape row;
+  int depth;
+  int bytes(int element) const { return row.waves * depth * row.vpl * kSegment * element; }      // LDS of a workgroup
+};
+Way way(int C, bool whole, int bytes) {                  // bytes of an element of all tensors that are read
+  auto depth = [&](const RowShape& r) { return ring_depth(r.waves, r.vpl * kSegment * bytes); };
+  const Form form = whole ? kWhole : kShifted;
+  const RowShape row = row_shape(C, form);
+  if (row.waves <= kMaxWaves && depth(row)) return {form, row, depth(row)};
+  return {kSingle, row_shape(C), 0};
+}
+// f(form, depth) as integral constants
 template <class F>
-void with_depth(int depth, F f) {
-  if (depth == 0) f(std::integral_constant<int, 0>{});
-  else if (depth == 1) f(std::integral_constant<int, 1>{});
-  else if (depth == 2) f(std::integral_constant<int, 2>{});
-  else f(std::integral_constant<int, 3>{});
+void with_way(const Way& w, F f) {
+  auto with_form = [&](auto form) {
+    if (w.depth == 1) f(form, std::integral_constant<int, 1>{});
+    else if (w.depth == 2) f(form, std::integral_constant<int, 2>{});
+    else f(form, std::integral_constant<int, 3>{});
+  };
+  if (w.form == kWhole) with_form(std::integral_constant<Form, kWhole>{});
+  else if (w.form == kShifted) with_form(std::integral_constant<Form, kShifted>{});
+  else f(std::integral_constant<Form, kSingle>{}, std::integral_constant<int, 0>{});
 }
 
 // Launches a kernel with `bytes` of dynamic LDS; more than 64 KB has to be allowed, once for each GPU, because the call costs a microsecond.
@@ -854,17 +890,15 @@ hipError_t launch_with_lds(void (*kernel)(GateNormArgs), std::atomic<unsigned lo
 }
 
 constexpr int kGradLeast = 2;         // rows of a strip of the backward pass: its sums cost the traffic of two
-struct GradShape {
-  RowShape row;
-  int strip, splits, slot, depth;     // depth 0: rows through registers
+struct GradShape {                    // by the descriptor alone: the workspace depends on it
+  int strip, splits;
   long long strips;
 };
 GradShape grad_shape(const svg_gate_norm_t& d) {
   GradShape g;
-  g.row = row_shape(d.C);
-  g.slot = g.row.vpl * kSegment * 2 * (type_bytes(d.stream_type) + 2);
-  g.depth = ring_depth(g.row.waves, g.slot);
-  g.strip = std::max(strip_rows(d.rows, g.row.waves, 16, g.row.waves * g.depth * g.slot), kGradLeast);
+  const int bytes = 2 * (type_bytes(d.stream_type) + 2);
+  const Way w = way(d.C, true, bytes);
+  g.strip = std::max(strip_rows(d.rows, w.row.waves, 16, w.bytes(bytes)), kGradLeast);
   g.strips = (d.rows + g.strip - 1) / g.strip;
   // parts of the strips that are added up side by side: enough workgroups for the chip, at least 128 strips each
   const long long chunks = (d.C + kSumChannels - 1) / kSumChannels * (long long)std::min(d.groups, 4096);
@@ -891,23 +925,25 @@ int launch_gate_norm(const svg_gate_norm_t& d, const void* x, const void* y, voi
   const bool vec = aligned(a);
   if (codes && (!vec || d.C % 32)) return SVG_ERR_UNSUPPORTED;
   if (codes) a.row_limit = fp4_row_tiles(d.rows) * kFp4Rows;
-  const RowShape s = row_shape(d.C);
-  const int slot = s.vpl * kSegment * (type_bytes(d.stream_type) + 2), depth = vec ? ring_depth(s.waves, slot) : 0;
-  a.waves = s.waves;
+  const int bytes = type_bytes(d.stream_type) + 2;
+  const Way w = way(d.C, vec, bytes);
+  a.waves = w.row.waves;
   // Rows few enough for three generations of workgroups are taken one each (1573 x 1536 11.4 us instead of 14.9, 6000 x 2048
   // 22.2 instead of 20.6).
-  a.strip = strip_rows(a.row_limit, s.waves, 20, s.waves * depth * slot);
+  a.strip = strip_rows(a.row_limit, w.row.waves, 20, w.bytes(bytes));
   if (a.strip <= 3) a.strip = 1;
-  const dim3 grid((unsigned)((a.row_limit + a.strip - 1) / a.strip)), block((unsigned)(64 * s.waves));
+  const dim3 grid((unsigned)((a.row_limit + a.strip - 1) / a.strip)), block((unsigned)(64 * w.row.waves));
   hipError_t e = hipSuccess;
   (void)hipGetLastError();
-  dispatch(d, s.vpl, [&](auto ts, auto tb, auto vpl) {
+  dispatch(d, w.row.vpl, [&](auto ts, auto tb, auto vpl) {
     constexpr int TS = decltype(ts)::value, TB = decltype(tb)::value, VPL = decltype(vpl)::value;
-    with_depth(depth, [&](auto dc) {
-      constexpr int D = decltype(dc)::value;
+    with_way(w, [&](auto form, auto depth) {
+      constexpr Form FORM = decltype(form)::value;
+      constexpr int D = decltype(depth)::value;
       static std::atomic<unsigned long long> allowed[2];
-      constexpr bool F = D > 0;        // a 4-bit output only where rows are aligned
-      e = launch_with_lds(codes ? gate_norm_kernel<TS, TB, VPL, D, F> : gate_norm_kernel<TS, TB, VPL, D, false>, allowed[codes != nullptr], grid, block, s.waves * D * slot, stream, a);
+      constexpr bool F = FORM == kWhole;
+      e = launch_with_lds(codes ? gate_norm_kernel<TS, TB, VPL, D, FORM, F> : gate_norm_kernel<TS, TB, VPL, D, FORM, false>, allowed[codes != nullptr],
+                          grid, block, w.bytes(bytes), stream, a);
     });
   });
   return hip_status(e);
@@ -919,18 +955,21 @@ int launch_gate_norm_grad(const svg_gate_norm_t& d, const void* r, const void* y
   a.r_in = r; a.y = y; a.dr = dr; a.dh = dh; a.dx = dx; a.dy = dy;
   a.partial = workspace;
   const GradShape g = grad_shape(d);
-  a.waves = g.row.waves;
+  const int bytes = 2 * (type_bytes(d.stream_type) + 2);
+  const Way w = way(d.C, aligned(a), bytes);
+  a.waves = w.row.waves;
   a.strip = g.strip;
   (void)hipGetLastError();
   if (d.rows) {
-    const dim3 grid((unsigned)g.strips), block((unsigned)(64 * g.row.waves));
+    const dim3 grid((unsigned)g.strips), block((unsigned)(64 * w.row.waves));
     hipError_t e = hipSuccess;
-    dispatch(d, g.row.vpl, [&](auto ts, auto tb, auto vpl) {
+    dispatch(d, w.row.vpl, [&](auto ts, auto tb, auto vpl) {
       constexpr int TS = decltype(ts)::value, TB = decltype(tb)::value, VPL = decltype(vpl)::value;
-      with_depth(aligned(a) ? g.depth : 0, [&](auto dc) {
-        constexpr int D = decltype(dc)::value;
+      with_way(w, [&](auto form, auto depth) {
+        constexpr Form FORM = decltype(form)::value;
+        constexpr int D = decltype(depth)::value;
         static std::atomic<unsigned long long> allowed;
-        e = launch_with_lds(gate_norm_grad_kernel<TS, TB, VPL, D>, allowed, grid, block, g.row.waves * D * g.slot, stream, a);
+        e = launch_with_lds(gate_norm_grad_kernel<TS, TB, VPL, D, FORM>, allowed, grid, block, w.bytes(bytes), stream, a);
       });
     });
     if (e != hipSuccess) return hip_status(e);
