@@ -179,11 +179,13 @@ __device__ __forceinline__ void store1(void* base, size_t element, float v) {
   else static_cast<_Float16*>(base)[element] = (_Float16)v;
 }
 
-// silu(v) = v / (1 + e^-v);  the tanh form of GELU is v sigmoid(2 sqrt(2/pi) (v + 0.044715 v^3)).
+// silu(v) = v / (1 + e^-v);  the tanh form of GELU is v sigmoid(2 sqrt(2/pi) (v + 0.044715 v^3)).  The result is rounded next: base-2
+// exponential and reciprocal of the vector unit, a few units in the last place of fp32.
 __device__ __forceinline__ float activate(float v, int activation) {
-  if (activation == SVG_ACT_SILU) return v / (1.0f + expf(-v));
-  if (activation == SVG_ACT_GELU_TANH) return v / (1.0f + expf(-1.5957691216057308f * (v + 0.044715f * v * v * v)));
-  return v;
+  if (activation == SVG_ACT_NONE) return v;
+  constexpr float kLog2e = 1.4426950408889634f;
+  const float u = activation == SVG_ACT_SILU ? -kLog2e * v : -1.5957691216057308f * kLog2e * __builtin_fmaf(0.044715f * v * v, v, v);
+  return v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u));
 }
 
 // The bits of the largest magnitude of eight values; infinities and NaNs are above every finite value's.

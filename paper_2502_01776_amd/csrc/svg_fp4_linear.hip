@@ -68,14 +68,6 @@ constexpr long long kComputeUnits = 256;
 // a 4-bit operand.
 enum Output { kAny, kVectors, kOperand };
 
-// The activations where the result is rounded next: base-2 exponential and reciprocal of the vector unit, a few units in the last place of fp32.
-__device__ __forceinline__ float activate_fast(float v, int activation) {
-  if (activation == SVG_ACT_NONE) return v;
-  constexpr float kLog2e = 1.4426950408889634f;
-  const float u = activation == SVG_ACT_SILU ? -kLog2e * v : -1.5957691216057308f * kLog2e * __builtin_fmaf(0.044715f * v * v, v, v);
-  return v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u));
-}
-
 // The bias of the columns n to n + 3.
 __device__ __forceinline__ f32x4 bias_of(const LinearArgs& A, int n) {
   f32x4 b;
@@ -135,7 +127,7 @@ struct Writer {
     for (int e = 0; e < 8; ++e) v[e] = e < 4 ? lo[e & 3] : hi[e & 3];
     if (A.activation != SVG_ACT_NONE) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = activate_fast(v[e], A.activation);
+      for (int e = 0; e < 8; ++e) v[e] = activate(v[e], A.activation);
     }
     const int n = n0 + Y * 32 + 8 * q;
     if constexpr (OUT == kOperand) {
