@@ -180,12 +180,18 @@ __device__ __forceinline__ void store1(void* base, size_t element, float v) {
 }
 
 // silu(v) = v / (1 + e^-v);  the tanh form of GELU is v sigmoid(2 sqrt(2/pi) (v + 0.044715 v^3)).  The result is rounded next: base-2
-// exponential and reciprocal of the vector unit, a few units in the last place of fp32.
-__device__ __forceinline__ float activate(float v, int activation) {
-  if (activation == SVG_ACT_NONE) return v;
-  constexpr float kLog2e = 1.4426950408889634f;
-  const float u = activation == SVG_ACT_SILU ? -kLog2e * v : -1.5957691216057308f * kLog2e * __builtin_fmaf(0.044715f * v * v, v, v);
-  return v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u));
+// exponential and reciprocal of the vector unit, a few units in the last place of fp32.  The choice is made once for eight
+// values: taken for each, its branches cost more than the arithmetic.
+__device__ __forceinline__ void activate8(float (&v)[8], int activation) {
+  constexpr float kLog2e = 1.4426950408889634f, kGelu = -1.5957691216057308f * kLog2e;
+  auto gate = [](float x, float u) { return x * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u)); };
+  if (activation == SVG_ACT_GELU_TANH) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = gate(v[e], v[e] * __builtin_fmaf(0.044715f * kGelu, v[e] * v[e], kGelu));
+  } else if (activation == SVG_ACT_SILU) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = gate(v[e], -kLog2e * v[e]);
+  }
 }
 
 // The bits of the largest magnitude of eight values; infinities and NaNs are above every finite value's.

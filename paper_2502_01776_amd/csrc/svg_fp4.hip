@@ -103,8 +103,7 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantArgs a) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       if (at.row(k) >= a.rows) break;                    // act(0) = 0: the padding stays zero
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[k][e] = activate(v[k][e], a.activation);
+      activate8(v[k], a.activation);
     }
   }
   unsigned code[4], scale = 0;

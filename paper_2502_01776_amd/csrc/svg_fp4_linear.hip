@@ -125,10 +125,7 @@ struct Writer {
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = e < 4 ? lo[e & 3] : hi[e & 3];
-    if (A.activation != SVG_ACT_NONE) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = activate(v[e], A.activation);
-    }
+    if (A.activation != SVG_ACT_NONE) activate8(v, A.activation);
     const int n = n0 + Y * 32 + 8 * q;
     if constexpr (OUT == kOperand) {
       if (!inner) {                                     // the padding
