@@ -656,7 +656,7 @@ struct GradSumArgs {
   long long group_rows;
   const float* partial;               // [slots][4][C]
   float* split;                       // [splits][groups][4][C]: sums of parts of the strips, where there is more than one
-  float* total;                       // [groups][4][C], or null where no weight's gradient is wanted or there is one group
+  float* total;                       // [groups][4][C], or null where no weight's gradient is wanted or the groups are few
   const float *post_weight, *post_bias, *weight, *bias;
   const float *gate, *scale;          // the forward pass's tables, [groups] rows of ld_mod
   long long ld_mod, ld_grad;
@@ -665,11 +665,13 @@ struct GradSumArgs {
 
 constexpr int kSumLanes = 64;         // rows (slots, splits, groups) that are summed side by side
 constexpr int kSumChannels = 16;
+constexpr int kFewGroups = 8;
 
-// Adds up the four sums of 16 channels over the workgroup's 64 rows of threads; the result is in the first row.
-__device__ __forceinline__ void fold_rows(float (&s)[4]) {
+// Adds up the four sums of 16 channels over the workgroup's 64 rows of threads, in parts of `rows` of them (a multiple of 4):
+// part p's result is in row p.
+__device__ __forceinline__ void fold_rows(float (&s)[4], int rows = kSumLanes) {
   __shared__ float lds[kSumLanes / 4][4][kSumChannels];
-  const int c = threadIdx.x % kSumChannels, wave = threadIdx.x >> 6;
+  const int c = threadIdx.x % kSumChannels, wave = threadIdx.x >> 6, part = threadIdx.x / kSumChannels;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {       // the four rows of a wavefront
     const unsigned u = __float_as_uint(s[j]);
@@ -682,12 +684,11 @@ __device__ __forceinline__ void fold_rows(float (&s)[4]) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) lds[wave][j][c] = s[j];
   __syncthreads();
-  if (threadIdx.x < kSumChannels)
+  if (part * rows < kSumLanes)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      s[j] = lds[0][j][c];
-#pragma unroll
-      for (int q = 1; q < kSumLanes / 4; ++q) s[j] += lds[q][j][c];
+      s[j] = lds[part * rows / 4][j][c];
+      for (int q = 1; q < rows / 4; ++q) s[j] += lds[part * rows / 4 + q][j][c];
     }
   __syncthreads();
 }
@@ -698,15 +699,76 @@ __device__ __forceinline__ void finish_group(const GradSumArgs& a, int g, int c,
   if (a.dshift) a.dshift[at] = s[0];
   if (a.dscale) a.dscale[at] = (a.weight ? a.weight[c] : 1.f) * s[1] + (a.bias ? a.bias[c] : 0.f) * s[0];
   if (a.dgate) a.dgate[at] = (a.post_weight ? a.post_weight[c] : 1.f) * s[3] + (a.post_bias ? a.post_bias[c] : 0.f) * s[2];
-  if (a.groups == 1) {
-    const float scale = a.scale ? 1.0f + a.scale[c] : 1.0f, gate = a.gate ? a.gate[c] : 1.0f;
-    if (a.dbias) a.dbias[c] = scale * s[0];
-    if (a.dweight) a.dweight[c] = scale * s[1];
-    if (a.dpost_bias) a.dpost_bias[c] = gate * s[2];
-    if (a.dpost_weight) a.dpost_weight[c] = gate * s[3];
-  } else if (a.total) {
+  if (a.total) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) a.total[((size_t)g * 4 + j) * a.C + c] = s[j];
+  }
+}
+
+// Adds a group's sums under its modulation to those of the weights' gradients.
+__device__ __forceinline__ void add_weights(const GradSumArgs& a, int g, int c, const float (&p)[4], float (&s)[4]) {
+  const float scale = a.scale ? 1.0f + a.scale[(size_t)g * a.ld_mod + c] : 1.0f;
+  const float gate = a.gate ? a.gate[(size_t)g * a.ld_mod + c] : 1.0f;
+  s[0] = __builtin_fmaf(scale, p[0], s[0]);
+  s[1] = __builtin_fmaf(scale, p[1], s[1]);
+  s[2] = __builtin_fmaf(gate, p[2], s[2]);
+  s[3] = __builtin_fmaf(gate, p[3], s[3]);
+}
+__device__ __forceinline__ void write_weights(const GradSumArgs& a, int c, const float (&s)[4]) {
+  if (a.dbias) a.dbias[c] = s[0];
+  if (a.dweight) a.dweight[c] = s[1];
+  if (a.dpost_bias) a.dpost_bias[c] = s[2];
+  if (a.dpost_weight) a.dpost_weight[c] = s[3];
+}
+
+// The strips that have rows of group g: first to end - 1.
+__device__ __forceinline__ void group_strips(const GradSumArgs& a, int g, long long& first, long long& end) {
+  long long lo = 0, hi = a.rows;
+  if (a.groups > 1) {
+    if (a.group_ptr) {
+      if (g > 0) lo = min(max((long long)a.group_ptr[g], 0ll), a.rows);
+      if (g + 1 < a.groups) hi = min(max((long long)a.group_ptr[g + 1], 0ll), a.rows);
+    } else {
+      lo = g * a.group_rows;
+      hi = lo + a.group_rows;
+    }
+  }
+  first = lo < hi ? lo / a.strip : 0;
+  end = lo < hi ? (hi - 1) / a.strip + 1 : 0;
+}
+
+// Few groups: their sums side by side, each by `lanes` rows of threads, from the strips' (or from the parts' where SPLIT), and all
+// gradients from them.  One launch instead of two: 2971 x 1536 in four groups BEFORE -> AFTER us.
+template <bool SPLIT>
+__global__ __launch_bounds__(kSumLanes* kSumChannels) void grad_few_kernel(GradSumArgs a, int lanes) {
+  __shared__ float lds[kFewGroups][4][kSumChannels];
+  const int i = threadIdx.x % kSumChannels, c = blockIdx.x * kSumChannels + i, k = threadIdx.x / kSumChannels, g = k / lanes;
+  float s[4] = {};
+  if (g < a.groups && c < a.C) {
+    long long b = 0, end = a.splits;
+    if constexpr (!SPLIT) group_strips(a, g, b, end);
+#pragma unroll 4
+    for (b += k % lanes; b < end; b += lanes) {
+      const float* p = SPLIT ? a.split + ((size_t)b * a.groups + g) * 4 * a.C + c : a.partial + (size_t)(b + g) * 4 * a.C + c;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[j] += p[(size_t)j * a.C];
+    }
+  }
+  fold_rows(s, lanes);
+  if (k < a.groups && c < a.C) {
+    finish_group(a, k, c, s);
+    float w[4] = {};
+    add_weights(a, k, c, s, w);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) lds[k][j][i] = w[j];
+  }
+  __syncthreads();
+  if (k == 0 && c < a.C) {
+    for (int j = 0; j < 4; ++j) s[j] = lds[0][j][i];
+    for (int h = 1; h < a.groups; ++h)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[j] += lds[h][j][i];
+    write_weights(a, c, s);
   }
 }
 
@@ -714,19 +776,11 @@ __device__ __forceinline__ void finish_group(const GradSumArgs& a, int g, int c,
 __global__ __launch_bounds__(kSumLanes* kSumChannels) void grad_groups_kernel(GradSumArgs a) {
   const int c = blockIdx.x * kSumChannels + threadIdx.x % kSumChannels, k = threadIdx.x / kSumChannels;
   for (int g = blockIdx.y; g < a.groups; g += gridDim.y) {
-    long long lo = 0, hi = a.rows;
-    if (a.groups > 1) {
-      if (a.group_ptr) {
-        if (g > 0) lo = min(max((long long)a.group_ptr[g], 0ll), a.rows);
-        if (g + 1 < a.groups) hi = min(max((long long)a.group_ptr[g + 1], 0ll), a.rows);
-      } else {
-        lo = g * a.group_rows;
-        hi = lo + a.group_rows;
-      }
-    }
+    long long first, end;
+    group_strips(a, g, first, end);
     float s[4] = {};
-    if (lo < hi && c < a.C) {
-      const long long first = lo / a.strip, end = (hi - 1) / a.strip + 1, part = (end - first + a.splits - 1) / a.splits;
+    if (c < a.C) {
+      const long long part = (end - first + a.splits - 1) / a.splits;
       const long long b1 = min(end, first + ((long long)blockIdx.z + 1) * part);
 #pragma unroll 4
       for (long long b = first + blockIdx.z * part + k; b < b1; b += kSumLanes) {
@@ -767,21 +821,12 @@ __global__ __launch_bounds__(kSumLanes* kSumChannels) void grad_weights_kernel(G
   float s[4] = {};
   if (c < a.C)
     for (int g = k; g < a.groups; g += kSumLanes) {
-      const float* p = a.total + (size_t)g * 4 * a.C + c;
-      const float scale = a.scale ? 1.0f + a.scale[(size_t)g * a.ld_mod + c] : 1.0f;
-      const float gate = a.gate ? a.gate[(size_t)g * a.ld_mod + c] : 1.0f;
-      s[0] = __builtin_fmaf(scale, p[0], s[0]);
-      s[1] = __builtin_fmaf(scale, p[a.C], s[1]);
-      s[2] = __builtin_fmaf(gate, p[2 * (size_t)a.C], s[2]);
-      s[3] = __builtin_fmaf(gate, p[3 * (size_t)a.C], s[3]);
+      const float* t = a.total + (size_t)g * 4 * a.C + c;
+      const float p[4] = {t[0], t[a.C], t[2 * (size_t)a.C], t[3 * (size_t)a.C]};
+      add_weights(a, g, c, p, s);
     }
   fold_rows(s);
-  if (k == 0 && c < a.C) {
-    if (a.dbias) a.dbias[c] = s[0];
-    if (a.dweight) a.dweight[c] = s[1];
-    if (a.dpost_bias) a.dpost_bias[c] = s[2];
-    if (a.dpost_weight) a.dpost_weight[c] = s[3];
-  }
+  if (k == 0 && c < a.C) write_weights(a, c, s);
 }
 
 // Wavefronts of a workgroup, vectors of a lane: 512 channels a wavefront and vector, one vector up to 8192 channels, two up to 16384.
@@ -901,7 +946,7 @@ GradShape grad_shape(const svg_gate_norm_t& d) {
   g.strip = std::max(strip_rows(d.rows, w.row.waves, 16, w.bytes(bytes)), kGradLeast);
   g.strips = (d.rows + g.strip - 1) / g.strip;
   // parts of the strips that are added up side by side: enough workgroups for the chip, at least 128 strips each
-  const long long chunks = (d.C + kSumChannels - 1) / kSumChannels * (long long)std::min(d.groups, 4096);
+  const long long chunks = (d.C + kSumChannels - 1) / kSumChannels * (long long)(d.groups <= kFewGroups ? 1 : std::min(d.groups, 4096));
   const long long most = std::min<long long>(32, g.strips / std::max(1, std::min(d.groups, 64)) / 128);
   g.splits = (int)std::max<long long>(1, std::min<long long>(most, (256 + chunks - 1) / chunks));
   return g;
@@ -981,7 +1026,7 @@ int launch_gate_norm_grad(const svg_gate_norm_t& d, const void* r, const void* y
   p.partial = workspace;
   const bool weights = grads.post_weight || grads.post_bias || grads.weight || grads.bias;
   float* const behind = workspace + (size_t)(g.strips + d.groups) * 4 * d.C;
-  p.total = weights && d.groups > 1 ? behind : nullptr;
+  p.total = weights && d.groups > kFewGroups ? behind : nullptr;
   p.split = behind + (size_t)d.groups * 4 * d.C;
   // a missing norm's weight and bias take no part
   p.post_weight = d.post_norm != SVG_NORM_NONE ? d.post_weight : nullptr;
@@ -996,9 +1041,20 @@ int launch_gate_norm_grad(const svg_gate_norm_t& d, const void* r, const void* y
   if (!weights && !p.dgate && !p.dscale && !p.dshift) return SVG_OK;
   const unsigned chunks = (unsigned)((d.C + kSumChannels - 1) / kSumChannels), gy = (unsigned)std::min(d.groups, 4096);
   const dim3 threads(kSumLanes * kSumChannels);
-  hipLaunchKernelGGL(grad_groups_kernel, dim3(chunks, gy, (unsigned)p.splits), threads, 0, stream, p);
-  if (p.splits > 1) hipLaunchKernelGGL(grad_splits_kernel, dim3(chunks, gy), threads, 0, stream, p);
-  if (p.total) hipLaunchKernelGGL(grad_weights_kernel, dim3(chunks), threads, 0, stream, p);
+  if (d.groups <= kFewGroups) {
+    int lanes = kSumLanes;            // a power of two: whole wavefronts
+    while (lanes * d.groups > kSumLanes) lanes /= 2;
+    if (p.splits > 1) {
+      hipLaunchKernelGGL(grad_groups_kernel, dim3(chunks, gy, (unsigned)p.splits), threads, 0, stream, p);
+      hipLaunchKernelGGL(grad_few_kernel<true>, dim3(chunks), threads, 0, stream, p, lanes);
+    } else {
+      hipLaunchKernelGGL(grad_few_kernel<false>, dim3(chunks), threads, 0, stream, p, lanes);
+    }
+  } else {
+    hipLaunchKernelGGL(grad_groups_kernel, dim3(chunks, gy, (unsigned)p.splits), threads, 0, stream, p);
+    if (p.splits > 1) hipLaunchKernelGGL(grad_splits_kernel, dim3(chunks, gy), threads, 0, stream, p);
+    if (p.total) hipLaunchKernelGGL(grad_weights_kernel, dim3(chunks), threads, 0, stream, p);
+  }
   return hip_status(hipGetLastError());
 }
 
