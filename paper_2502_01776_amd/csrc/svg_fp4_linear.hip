@@ -763,15 +763,19 @@ int launch_rows(const LinearArgs& a, Output out, hipStream_t stream) {
 }
 
 
-// Which form a product takes, by estimates of its time in units of what a compute unit needs for a 256 x 256 tile.  A launch's
-// workgroups of 256 x 256 run one to a compute unit, the smaller ones two, and one that has its compute unit to itself is faster.
-//   256 x 256: 1 a round of 256;  128 x 256: 1.05 a round of 512, 0.62 for a last one of up to 256;  64 x 128: 0.48, 0.41.
+// Which form a product takes, by estimates of its time: what a round of workgroups needs is a part for its beginning and end, more of it
+// with an activation, and one that grows with K.  A launch's workgroups of 256 x 256 run one to a compute unit, the smaller ones
+// two, and one that has its compute unit to itself is faster.  In us, K in thousands:
+//   256 x 256: 9 + 5.1 K a round of 256;  128 x 256: 9 + 5.35 K a round of 512, 6.1 + 3.44 K for a last one of up to 256;
+//   64 x 128: 3.6 + 1.9 K, 85 % of it;  an activation: + 3.5, 3.5, 2.6, 0.5.
 // Up to 64 tokens, or up to 400 workgroups of 64 tokens and 32 columns, operands straight from memory (K split over the wavefronts).
 // us, 256 x 256 | 128 x 256 | 64 x 128 | straight (M x N x K):
 //   64 x 5120 x 5120 30.3 22.9 12.5 9.3;  226 x 5120 x 4096 27.1 19.5 10.9 13.3;  226 x 1536 x 1536 15.8 11.3 6.9 6.4;
-//   226 x 20480 x 1536 16.8 12.6 13.6 20.2;  1573 x 512 x 512 11.3 8.6 6.0 5.9;  1573 x 1536 x 6144 36.3 26.2 18.5 28.2;
-//   4096 x 1536 x 1536 17.0 12.4 13.5 17.5;  2048 x 5120 x 5120 35.6 37.1 42.0 62.5;  4096 x 5120 x 5120 73.4 60.2 77.8 117;
+//   1573 x 512 x 512 11.3 8.6 6.0 5.9;  1573 x 1536 x 6144 34.3 25.4 16.8 26.7;  1573 x 6144 x 1536 17.3 17.2 18.0 26.6;
+//   4096 x 1536 x 1536 17.0 12.4 13.5 17.5;  2048 x 5120 x 5120 33.3 34.5 36.6 63.3;  4096 x 5120 x 5120 73.4 60.2 77.8 117;
 //   17776 x 512 x 8192 47.9 52.1 58.6 174;  32760 x 5120 x 20480 1376 1465 2246
+// and behind GELU 500 x 10240 x 2560 22.9 17.2 15.2 25.2;  226 x 20480 x 5120 33.7 25.7 24.7 40.2;  1573 x 6144 x 1536 20.4 20.4 18.7 27.0;
+//   8000 x 4096 x 1024 35.1 33.5 46.3 86.1;  32760 x 20480 x 5120 1569 1558 2212
 // Straight, one token tile (K over 8 wavefronts), two (4, or 8 where there are fewer workgroups than compute units) and four (4):
 //   16 x 5120 x 5120 7.1 7.8 (8: 7.5) 8.9;  32 x 5120 x 5120 9.6 7.9 (7.5) 8.9;  32 x 20480 x 5120 22.8 15.7 (19.5) 17.6
 int launch(const LinearArgs& a, Output form, hipStream_t stream) {
@@ -784,8 +788,10 @@ int launch(const LinearArgs& a, Output form, hipStream_t stream) {
     const long long rest = tiles % (2 * kComputeUnits);
     return (double)(tiles / (2 * kComputeUnits)) * whole + (rest > kComputeUnits ? whole : rest ? alone : 0.0);
   };
-  const double square = (double)((tiles(16, 8) + kComputeUnits - 1) / kComputeUnits);
-  const double large = rounds(tiles(8, 8), 1.05, 0.62), small = rounds(tiles(4, 4), 0.48, 0.41);
+  const double k = a.kt * 0.128, act = a.activation != SVG_ACT_NONE ? 1.0 : 0.0;
+  const double square = (double)((tiles(16, 8) + kComputeUnits - 1) / kComputeUnits) * (9.0 + 3.5 * act + 5.1 * k);
+  const double large = rounds(tiles(8, 8), 9.0 + 3.5 * act + 5.35 * k, 6.1 + 2.6 * act + 3.44 * k);
+  const double one = 3.6 + 0.5 * act + 1.9 * k, small = rounds(tiles(4, 4), one, 0.85 * one);
   if (square <= large && square <= small) return launch_square<8, 2, 2, 4>(a, form, stream);
   return large <= small ? launch_tiles<8, 2, 1, 4>(a, form, stream) : launch_tiles<4, 1, 1, 4>(a, form, stream);
 }
