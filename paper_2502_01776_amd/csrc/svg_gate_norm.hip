@@ -14,6 +14,7 @@ namespace {
 
 constexpr int kMaxWaves = 16;         // wavefronts of a workgroup
 constexpr int kMaxChannels = 16384;
+constexpr int kFewGroups = 8;
 
 struct GateNormArgs {
   long long rows;
@@ -45,6 +46,18 @@ __device__ __forceinline__ int group_of(const GateNormArgs& a, long long row, lo
     const unsigned g = (unsigned)row / (unsigned)a.group_rows;
     end = (long long)(g + 1) * a.group_rows;
     return (int)g;
+  }
+  if (a.groups <= kFewGroups) {       // all ends at once instead of one load behind another
+    int ends[kFewGroups], g = 0;
+#pragma unroll
+    for (int j = 1; j < kFewGroups; ++j) ends[j] = a.group_ptr[min(j, a.groups)];
+#pragma unroll
+    for (int j = 1; j < kFewGroups; ++j) {
+      if (j >= a.groups) continue;
+      if (ends[j] <= row) ++g;
+      else end = min(end, (long long)ends[j]);
+    }
+    return g;
   }
   int lo = 0, hi = a.groups - 1;
   while (lo < hi) {
@@ -665,7 +678,6 @@ struct GradSumArgs {
 
 constexpr int kSumLanes = 64;         // rows (slots, splits, groups) that are summed side by side
 constexpr int kSumChannels = 16;
-constexpr int kFewGroups = 8;
 
 // Adds up the four sums of 16 channels over the workgroup's 64 rows of threads, in parts of `rows` of them (a multiple of 4):
 // part p's result is in row p.
