@@ -262,3 +262,42 @@ def test_matrices_past_32_bit_offsets():
     v = f64(heads[0, :, [0, 449_999]]).transpose(1, 0, 2).reshape(2, 5120)
     assert np.array_equal(f64(back[[0, 449_999]]), O.mx_values(*O.mx_quantise(v)))
     assert not back[1].any() and not back[449_998].any()
+
+
+@pytest.mark.parametrize("rows", [1, 3, 4, 5, 13, 17])
+@pytest.mark.parametrize("first", [0, 1, 2, 5])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_quantise_rows_that_begin_anywhere(rows, first, dtype):
+    """Rows of an odd stride and width at every offset; what lies around a matrix that is read back stays."""
+    wide = data(rows, 1049, dtype, rows + first)
+    x = wide[:, first:first + 1031]
+    codes, scales = check_exact(x)
+    back = torch.full((rows + 2, 1049), 7.0, dtype=dtype, device="cuda")
+    part = back[1:1 + rows, first:first + 1031]
+    S.svg_fp4_dequantize(S.tokens_of(part), codes, scales, part)
+    torch.cuda.synchronize()
+    assert np.array_equal(f64(part), O.mx_values(*O.mx_quantise(f64(x))))
+    part.fill_(7.0)
+    assert (back == 7).all()
+
+
+@pytest.mark.parametrize("M,N,K", [(500, 1280, 2560), (230, 2560, 5120), (1573, 1536, 1536), (600, 4100, 700)])
+@pytest.mark.parametrize("act", [S.SVG_ACT_NONE, S.SVG_ACT_SILU, S.SVG_ACT_GELU_TANH])
+def test_products_where_the_activation_decides_the_form(M, N, K, act):
+    p = Product(M, N, K, M)
+    ref, noise = p.expected(act)
+    close(p.linear(torch.full((M, N), float("nan"), dtype=torch.bfloat16, device="cuda"), act), ref, HALF[torch.bfloat16], noise, "out")
+
+
+def test_activations_far_from_zero():
+    """Their exponentials overflow or vanish: silu and GELU are v on one side and zero on the other."""
+    x = torch.tensor([[1e30, -1e30, 300.0, -300.0, 88.0, -88.0, 3e19, -3e19] * 4], device="cuda")
+    w = torch.eye(32, device="cuda")
+    for act in (S.SVG_ACT_SILU, S.SVG_ACT_GELU_TANH):
+        for k in range(8):                                          # one magnitude at a time: a block of its own
+            v = torch.zeros_like(x)
+            v[0, k] = x[0, k]
+            out = torch.full((1, 32), float("nan"), device="cuda")
+            S.svg_fp4_linear(1, 32, 32, *quantise(v), *quantise(w), None, act, S.tokens_of(out), out)
+            value = O.mx_values(*O.mx_quantise(f64(v)))[0, k]
+            assert out[0, k].item() == (pytest.approx(value, rel=1e-6) if value > 0 else pytest.approx(0.0, abs=1e-30))

@@ -394,3 +394,46 @@ def test_tensors_past_32_bit_offsets():
     close(h[sample], ref["dy"], 2.0 ** -8, 1e-4, "dy")
     close(gate, ref["gate"], U, 1e-3, "gate")
     assert not x[2].any() and not h[rows - 3].any()
+
+
+# ---- rows of any alignment, and sums over many strips ------------------------------------------------
+
+@pytest.mark.parametrize("C", [503, 504, 505, 509, 511, 513, 1007, 1009, 8063, 8065, 16127, 16129, 16383])
+@pytest.mark.parametrize("stream,branch", [("bf16", "f16"), ("f32", "bf16")])
+def test_widths_at_the_edges_of_a_wavefront(C, stream, branch):
+    c = Case(3, C, 2, [0, 1, 3], stream, branch, post=2, pre=1, seed=C)
+    check_forward(c)
+    check_backward(c)
+
+
+@pytest.mark.parametrize("rows,C", [(4100, 37), (3100, 513), (3100, 333), (2600, 1001), (4100, 504)])
+def test_long_strips_of_odd_rows(rows, C):
+    """More rows of a workgroup than are on their way at a time; the rows begin at every offset in a granule."""
+    c = Case(rows, C, 3, [0, rows // 5, rows // 2, rows], "f32" if C == 333 else "bf16", "f16", post=1, pre=2, seed=rows)
+    check_forward(c)
+    check_backward(c)
+
+
+@pytest.mark.parametrize("C", [5, 513, 516, 1001, 1017])
+@pytest.mark.parametrize("ld", [0, 1031])
+def test_odd_rows_in_place(C, ld):
+    """No norm, so wavefronts never wait for each other: none may read what another one has written."""
+    for pre, post in ((0, 0), (2, 1)):
+        c = Case(2500, C, post=post, pre=pre, ld=ld, seed=C)
+        r, h = run_forward(c)
+        got = run_backward(c)
+        x, dr, dh = (t._base.clone()[:, :C] if t._base is not None else t.clone() for t in (c.x, c.dr, c.dh))
+        h2 = c.empty(c.tb)
+        S.svg_gate_norm_fwd(c.desc, x, c.y, x, h2)
+        assert torch.equal(x, r) and torch.equal(h2, h)
+        n = S.svg_gate_norm_workspace_bytes(c.desc)
+        S.svg_gate_norm_bwd(c.desc, c.x, c.y, dr, dh, dr, dh, None, torch.empty(n, dtype=torch.uint8, device="cuda"), n)
+        assert torch.equal(dr, got["dx"]) and torch.equal(dh, got["dy"])
+
+
+@pytest.mark.parametrize("groups", [1, 2, 7, 8, 9, 17])
+@pytest.mark.parametrize("rows,C", [(65000, 16), (900, 24)])
+def test_sums_of_few_and_of_many_groups(rows, C, groups):
+    """Up to eight groups are summed in one launch; the sums of many strips are added up in parts first."""
+    ends = sorted(np.random.default_rng(groups).integers(0, rows + 1, groups - 1).tolist())
+    check_backward(Case(rows, C, groups, [0] + ends + [rows] if groups > 1 else None, stream="f32", post=2, pre=2, seed=groups))
