@@ -47,18 +47,6 @@ __device__ __forceinline__ int group_of(const GateNormArgs& a, long long row, lo
     end = (long long)(g + 1) * a.group_rows;
     return (int)g;
   }
-  if (a.groups <= kFewGroups) {       // all ends at once instead of one load behind another
-    int ends[kFewGroups], g = 0;
-#pragma unroll
-    for (int j = 1; j < kFewGroups; ++j) ends[j] = a.group_ptr[min(j, a.groups)];
-#pragma unroll
-    for (int j = 1; j < kFewGroups; ++j) {
-      if (j >= a.groups) continue;
-      if (ends[j] <= row) ++g;
-      else end = min(end, (long long)ends[j]);
-    }
-    return g;
-  }
   int lo = 0, hi = a.groups - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -360,14 +348,20 @@ struct Team {
   }
 };
 
+// Ends every load that the compiler knows of where a group begins.  It would wait for them, and with them for all rows on their way, where
+// the paths with and without a new group meet, once a row.
+__device__ __forceinline__ void wait_tables() { __builtin_amdgcn_s_waitcnt(0x0f70); }      // vmcnt(0)
+
 // Waits until at most N of this wavefront's operations on memory are outstanding (they end in order).
 template <int N>
 __device__ __forceinline__ void wait_ring() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N < 63 ? N : 63) : "memory"); }
 
 // The forward pass.  The tables of a group stay in registers, folded with the norms' weights: r = alpha x + (G1 yhat + G0),
-// h = H1 rhat + H0.
+// h = H1 rhat + H0.  With a 4-bit output five wavefronts a SIMD are asked for: the 101 registers that it takes otherwise leave a compute
+// unit to one row of ten wavefronts (32760 x 5120 299 -> 245 us).  A spilt register in the loop would cost more: its reload waits for
+// the rows on their way.
 template <int TS, int TB, int VPL, int D, Form FORM, bool FP4>
-__global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_kernel(GateNormArgs a) {
+__global__ __launch_bounds__(64 * kMaxWaves, FP4 && VPL == 1 ? 5 : 4) void gate_norm_kernel(GateNormArgs a) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   __shared__ block_f32x4 places[2][kMaxWaves];
   constexpr bool SINGLE = FORM == kSingle;
@@ -438,6 +432,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_kernel(GateNormArgs 
           for (int i = 0; i < N; ++i) h0[i] += t[i];
         }
       }
+      wait_tables();
     }
     float v[N], y[N];
     if constexpr (SINGLE) {
@@ -566,6 +561,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_grad_kernel(GateNorm
 #pragma unroll
         for (int i = 0; i < N; ++i) f1[i] *= t[i];
       }
+      wait_tables();
     }
     float rhat[N], d[N], yhat[N], e[N];
     if constexpr (SINGLE) {
@@ -750,7 +746,7 @@ __device__ __forceinline__ void group_strips(const GradSumArgs& a, int g, long l
 }
 
 // Few groups: their sums side by side, each by `lanes` rows of threads, from the strips' (or from the parts' where SPLIT), and all
-// gradients from them.  One launch instead of two: 2971 x 1536 in four groups BEFORE -> AFTER us.
+// gradients from them.  One launch instead of two: 2971 x 1536 in four groups 15.6 -> 10.8 us.
 template <bool SPLIT>
 __global__ __launch_bounds__(kSumLanes* kSumChannels) void grad_few_kernel(GradSumArgs a, int lanes) {
   __shared__ float lds[kFewGroups][4][kSumChannels];
