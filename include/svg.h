@@ -438,7 +438,7 @@ typedef struct svg_gate_norm_grads {
  *   dr  stream [rows, C]: gradient of r from what follows, or NULL (zero)
  *   dh  branch [rows, C]: gradient of h, or NULL (the forward pass had no h)
  *   dx, dy  written, or NULL.  dx == dr and dy == y or dy == dh (same stride) are allowed.
- * Sums over rows are fp32, their order depends on rows, C and groups only: results repeat bit for bit.
+ * Sums are fp32 in an order that depends on the descriptor and the tensors' alignment only: results repeat bit for bit.
  * workspace: >= svg_gate_norm_workspace_bytes(desc), 16-byte aligned.
  */
 size_t svg_gate_norm_workspace_bytes(const svg_gate_norm_t* desc);
@@ -492,7 +492,8 @@ int svg_fp4_dequantize(const svg_tokens_t* tokens, const void* codes, const void
  * with fp32 accumulation; a is an operand [M, K], w an operand [N, K], bias device fp32 [N] or
  * NULL.  svg_fp4_linear writes the token matrix `out` (out_desc: B*N rows = M, H*D columns = N), so a projection
  * can write [B,H,N,D] heads directly; svg_fp4_linear_quantize writes the operand [M, N] of the
- * next product, rounded from fp32.  K >= 1, N >= 1; results repeat bit for bit.
+ * next product, rounded from fp32.  The activations are taken on the vector unit's exponential and reciprocal (a few
+ * units in the last place of fp32).  K >= 1, N >= 1; results repeat bit for bit.
  * workspace: >= svg_fp4_linear_workspace_bytes(M, N, K), 16-byte aligned; NULL where that is 0.
  */
 size_t svg_fp4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);

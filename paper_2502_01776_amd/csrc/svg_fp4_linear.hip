@@ -543,8 +543,13 @@ int launch_tiles(const LinearArgs& a, Output out, hipStream_t stream) {
   return hip_status(hipGetLastError());
 }
 
+// Output tiles of 256 x 256 for large products: eight wavefronts of 8 token tiles x 2 pairs, both operands through LDS in four stages of a
+// step each, asked for four steps ahead; one barrier a step, in front of its last pair of products, behind which the loads of the
+// stage that is free are issued between products.  The 128 x 64 outputs of a wavefront take 12 KB of LDS reads for 32 products.
+// 32760 x 5120 x 20480: 1340 us, 5.1 PFLOP/s; the matrix units are busy 69 % of the cycles at 1.78 GHz (a loop of the same products from
+// registers alone reaches 6.4 to 6.8 PFLOP/s on random operands, 9.5 on zeros: power).  32760 x 20480 x 5120 behind GELU: 1560 us, 50 of them
+// the activation.
 constexpr int kStages = 4;
-
 
 template <int TM, int TP, int WM, int WN>
 struct SquareShape {
