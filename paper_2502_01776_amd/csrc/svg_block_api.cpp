@@ -1,4 +1,6 @@
 // C-ABI entry points of the operators around the attention: argument checks, then the launchers.
+#include <algorithm>
+
 #include "svg_block.h"
 
 namespace {
@@ -30,6 +32,9 @@ int check_gate_norm(const svg_gate_norm_t* d) {
   for (const void* p : words)
     if (misaligned(p, 4)) return SVG_ERR_INVALID_ARG;
   if (d->C > 16384 || d->rows > svg::kMaxTokenRows) return SVG_ERR_UNSUPPORTED;
+  // the furthest element of every tensor, as in check_tokens
+  for (int64_t ld : lds)
+    if ((__int128)std::max<int64_t>(d->rows, d->groups) * ld >= ((__int128)1 << 60)) return SVG_ERR_UNSUPPORTED;
   return SVG_OK;
 }
 
@@ -131,6 +136,7 @@ int svg_gate_norm_bwd(const svg_gate_norm_t* desc, const void* r, const void* y,
   svg_gate_norm_grads_t none = {};
   const svg_gate_norm_grads_t& gr = grads ? *grads : none;
   if (gr.ld_mod && (gr.ld_mod < d.C || gr.ld_mod > kMaxStride)) return SVG_ERR_INVALID_ARG;
+  if ((__int128)d.groups * gr.ld_mod >= ((__int128)1 << 60)) return SVG_ERR_UNSUPPORTED;
   float* const out_grads[7] = {gr.gate, gr.scale, gr.shift, gr.post_weight, gr.post_bias, gr.weight, gr.bias};
   bool any = dx || dy;
   for (const float* p : out_grads) {

@@ -147,3 +147,13 @@ def test_tokens_of_tensors():
         with pytest.raises(ValueError):
             S.tokens_of(bad)
     assert binding.EXPORTS.count("svg_fp4_linear") == 1
+
+
+@pytest.mark.parametrize("strides", [dict(ld_x=2 ** 40), dict(ld_h=2 ** 39), dict(ld_mod=2 ** 40, groups=2 ** 20)])
+def test_tensors_whose_extent_passes_64_bits_are_refused(strides):
+    """2^30 rows of 2^40 elements each: their last byte has no address, and their overlaps could not be told."""
+    d = desc(**{**dict(rows=2 ** 30, groups=1), **strides})
+    assert fwd(d) == -2 and S.svg_gate_norm_workspace_bytes(d) == 0
+    grads = S.gate_norm_grads(gate=A, ld_mod=2 ** 40)
+    big = desc(rows=2 ** 20, groups=2 ** 20)
+    assert S.lib().svg_gate_norm_bwd(C.byref(big), X, Y, Z, W, A, B_, C.byref(grads), None, 0, None) == -2
