@@ -361,15 +361,14 @@ def gate_norm_grads(gate=None, scale=None, shift=None, post_weight=None, post_bi
 
 def tokens_of(x) -> SvgTokens:
     """The token matrix of a tensor [rows, columns] or [B, H, N, D] with neighbouring last elements."""
-    if x.stride(-1) != 1 and x.shape[-1] > 1:
-        raise ValueError("the elements of a row (of a head) have to be neighbours")
-    if x.dim() == 2:
-        return SvgTokens(1, x.shape[0], 1, x.shape[1], 0, x.stride(0), 0, _TYPE_OF[x.dtype], 0)
-    if x.dim() != 4:
+    shape, stride = x.shape, x.stride()
+    if len(shape) not in (2, 4):
         raise ValueError("a token matrix is [rows, columns] or [B, H, N, D]")
-    B, H, N, D = x.shape
-    sb, sh, sn, _ = x.stride()
-    return SvgTokens(B, N, H, D, sb, sn, sh, _TYPE_OF[x.dtype], 0)
+    if stride[-1] != 1 and shape[-1] > 1:
+        raise ValueError("the elements of a row (of a head) have to be neighbours")
+    if len(shape) == 2:
+        return SvgTokens(1, shape[0], 1, shape[1], 0, stride[0], 0, _TYPE_OF[x.dtype])
+    return SvgTokens(shape[0], shape[2], shape[1], shape[3], stride[0], stride[2], stride[1], _TYPE_OF[x.dtype])
 
 
 def svg_gate_norm_fwd(desc, x, y, r, h, codes=None, scales=None, stream=None):
