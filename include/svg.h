@@ -428,7 +428,7 @@ int svg_gate_norm_fwd(const svg_gate_norm_t* desc, const void* x, const void* y,
 typedef struct svg_gate_norm_grads {
   int64_t ld_mod;                               /* row stride of gate, scale and shift (0: C) */
   float *gate, *scale, *shift;                  /* [groups, C]; an empty group's rows are zero */
-  float *post_weight, *post_bias, *weight, *bias;   /* [C] */
+  float *post_weight, *post_bias, *weight, *bias;   /* [C]; zero where the norm has none (see svg_gate_norm_t) */
 } svg_gate_norm_grads_t;
 
 /*

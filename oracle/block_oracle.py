@@ -55,7 +55,8 @@ def _norm_grad(g, hat, rho, norm):
 
 def gate_norm_grad(r, y, dr, dh, group, groups, gate, scale, alpha, post, pre, post_eps, eps, post_weight=None, post_bias=None,
                    weight=None, bias=None):
-    """Gradients of sum(dr * r + dh * h) by name; r is the stream that the forward pass gave."""
+    """Gradients of sum(dr * r + dh * h) by name; r is the stream that the forward pass gave.
+    A weight or bias that a norm does not have (bias: layer form only) takes no part in it: its gradient is zero."""
     rows, C = r.shape
     one = np.ones((groups, C))
     gate = one if gate is None else gate
@@ -69,7 +70,7 @@ def gate_norm_grad(r, y, dr, dh, group, groups, gate, scale, alpha, post, pre, p
     hat, rho = normalise(r, pre, eps)
     dn = dh * (1.0 + scale[group])
     out["shift"], out["scale"] = sums(dh), sums(dh * affine(hat, pre, weight, bias))
-    out["weight"], out["bias"] = (dn * hat).sum(0), dn.sum(0)
+    out["weight"], out["bias"] = ((dn * hat).sum(0) if pre != NORM_NONE else np.zeros(C)), (dn.sum(0) if pre == NORM_LAYER else np.zeros(C))
     d = d + _norm_grad(dn * w, hat, rho, pre)
     out["dx"] = alpha * d
     if y is None:
@@ -78,7 +79,8 @@ def gate_norm_grad(r, y, dr, dh, group, groups, gate, scale, alpha, post, pre, p
     hat, rho = normalise(y, post, post_eps)
     out["gate"] = sums(d * affine(hat, post, post_weight, post_bias))
     f = d * gate[group]
-    out["post_weight"], out["post_bias"] = (f * hat).sum(0), f.sum(0)
+    out["post_weight"] = (f * hat).sum(0) if post != NORM_NONE else np.zeros(C)
+    out["post_bias"] = f.sum(0) if post == NORM_LAYER else np.zeros(C)
     out["dy"] = _norm_grad(f * wp, hat, rho, post)
     return out
 

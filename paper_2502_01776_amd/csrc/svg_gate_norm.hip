@@ -670,6 +670,7 @@ struct GradSumArgs {
   const float *gate, *scale;          // the forward pass's tables, [groups] rows of ld_mod
   long long ld_mod, ld_grad;
   float *dgate, *dscale, *dshift, *dpost_weight, *dpost_bias, *dweight, *dbias;
+  bool has_post_weight, has_post_bias, has_weight, has_bias;        // does the norm have it?
 };
 
 constexpr int kSumLanes = 64;         // rows (slots, splits, groups) that are summed side by side
@@ -722,11 +723,12 @@ __device__ __forceinline__ void add_weights(const GradSumArgs& a, int g, int c, 
   s[2] = __builtin_fmaf(gate, p[2], s[2]);
   s[3] = __builtin_fmaf(gate, p[3], s[3]);
 }
+// What a norm does not have takes no part in the forward pass: its gradient is zero, whatever the sums hold.
 __device__ __forceinline__ void write_weights(const GradSumArgs& a, int c, const float (&s)[4]) {
-  if (a.dbias) a.dbias[c] = s[0];
-  if (a.dweight) a.dweight[c] = s[1];
-  if (a.dpost_bias) a.dpost_bias[c] = s[2];
-  if (a.dpost_weight) a.dpost_weight[c] = s[3];
+  if (a.dbias) a.dbias[c] = a.has_bias ? s[0] : 0.f;
+  if (a.dweight) a.dweight[c] = a.has_weight ? s[1] : 0.f;
+  if (a.dpost_bias) a.dpost_bias[c] = a.has_post_bias ? s[2] : 0.f;
+  if (a.dpost_weight) a.dpost_weight[c] = a.has_post_weight ? s[3] : 0.f;
 }
 
 // The strips that have rows of group g: first to end - 1.
@@ -1037,10 +1039,14 @@ int launch_gate_norm_grad(const svg_gate_norm_t& d, const void* r, const void* y
   p.total = weights && d.groups > kFewGroups ? behind : nullptr;
   p.split = behind + (size_t)d.groups * 4 * d.C;
   // a missing norm's weight and bias take no part
-  p.post_weight = d.post_norm != SVG_NORM_NONE ? d.post_weight : nullptr;
-  p.post_bias = d.post_norm == SVG_NORM_LAYER ? d.post_bias : nullptr;
-  p.weight = d.pre_norm != SVG_NORM_NONE ? d.weight : nullptr;
-  p.bias = d.pre_norm == SVG_NORM_LAYER ? d.bias : nullptr;
+  p.has_post_weight = d.post_norm != SVG_NORM_NONE;
+  p.has_post_bias = d.post_norm == SVG_NORM_LAYER;
+  p.has_weight = d.pre_norm != SVG_NORM_NONE;
+  p.has_bias = d.pre_norm == SVG_NORM_LAYER;
+  p.post_weight = p.has_post_weight ? d.post_weight : nullptr;
+  p.post_bias = p.has_post_bias ? d.post_bias : nullptr;
+  p.weight = p.has_weight ? d.weight : nullptr;
+  p.bias = p.has_bias ? d.bias : nullptr;
   p.gate = d.gate; p.scale = d.scale;
   p.ld_mod = a.ld_mod;
   p.ld_grad = grads.ld_mod ? grads.ld_mod : d.C;

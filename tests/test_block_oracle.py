@@ -114,3 +114,32 @@ def test_gradients_are_those_of_autograd_and_of_differences(post, pre):
         (torch.from_numpy(dr) * rt + torch.from_numpy(dh) * ht).sum().backward()
         for name in used:
             assert np.allclose(t[name].grad.numpy(), g[name], rtol=1e-9, atol=1e-10), name
+
+
+@pytest.mark.parametrize("post", [0, 1, 2])
+@pytest.mark.parametrize("pre", [0, 1, 2])
+def test_gradients_of_every_parameter_are_those_of_differences(post, pre):
+    """Also of the weights and biases that a norm does not have: the forward pass takes no notice of them, so they have none.  Central
+    differences in 64 bits: r and h are linear in what stands behind the second norm (a step of 1e-3 leaves 1e-13 of rounding); of what stands in
+    front of it the third derivative's part is the square of a step of 1e-5.  1e-6 of the terms' size is allowed."""
+    rng = np.random.default_rng(100 + 10 * post + pre)
+    rows, C, G = 9, 16, 2
+    group = O.group_of_rows(rows, G, [0, 5, 9])
+    p = {k: rng.normal(size=(G, C)) for k in ("gate", "scale", "shift")}
+    p.update({k: 1 + 0.3 * rng.normal(size=C) for k in ("post_weight", "post_bias", "weight", "bias")})
+    x, y, dr, dh = (rng.normal(size=(rows, C)) + 0.3 for _ in range(4))
+
+    def forward(**changed):
+        q = {**p, **changed}
+        return O.gate_norm(x, y, group, q["gate"], q["scale"], q["shift"], 0.8, post, pre, 1e-3, 1e-2, q["post_weight"], q["post_bias"],
+                           q["weight"], q["bias"])
+    g = O.gate_norm_grad(forward()[0], y, dr, dh, group, G, p["gate"], p["scale"], alpha=0.8, post=post, pre=pre, post_eps=1e-3, eps=1e-2,
+                         post_weight=p["post_weight"], post_bias=p["post_bias"], weight=p["weight"], bias=p["bias"])
+    there = {"weight": pre != 0, "bias": pre == 2, "post_weight": post != 0, "post_bias": post == 2}
+    for name in ("weight", "bias", "post_weight", "post_bias", "gate", "scale", "shift"):
+        direction = rng.normal(size=p[name].shape)
+        step = 1e-3 if name in ("weight", "bias", "scale", "shift") else 1e-5
+        (ra, ha), (rb, hb) = forward(**{name: p[name] + step * direction}), forward(**{name: p[name] - step * direction})
+        slope = ((dr * (ra - rb)).sum() + (dh * (ha - hb)).sum()) / (2 * step)
+        assert abs(slope - (g[name] * direction).sum()) <= 1e-6 * (np.abs(dr).sum() + np.abs(dh).sum()), name
+        assert there.get(name, True) or (slope == 0 and not g[name].any()), name

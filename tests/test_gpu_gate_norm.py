@@ -437,3 +437,18 @@ def test_sums_of_few_and_of_many_groups(rows, C, groups):
     """Up to eight groups are summed in one launch; the sums of many strips are added up in parts first."""
     ends = sorted(np.random.default_rng(groups).integers(0, rows + 1, groups - 1).tolist())
     check_backward(Case(rows, C, groups, [0] + ends + [rows] if groups > 1 else None, stream="f32", post=2, pre=2, seed=groups))
+
+
+@pytest.mark.parametrize("groups", [1, 3, 17])
+@pytest.mark.parametrize("post,pre", list(itertools.product(range(3), range(3))))
+def test_parameters_that_a_norm_does_not_have_get_zero_gradients(post, pre, groups):
+    """The forward pass takes no notice of them, whether the descriptor holds them or not; NaNs in the rows change nothing."""
+    ends = sorted(np.random.default_rng(groups).integers(0, 41, groups - 1).tolist())
+    for affine in (True, False):
+        c = Case(40, 72, groups, [0] + ends + [40], post=post, pre=pre, affine=affine)
+        check_backward(c)
+        c.dh[3, 5], c.dr[7, 9] = float("nan"), float("inf")
+        got = run_backward(c)
+        there = {"weight": pre != 0, "bias": pre == 2, "post_weight": post != 0, "post_bias": post == 2}
+        for name, has in there.items():
+            assert has or not got[name].any(), name
