@@ -5,11 +5,27 @@
 
 namespace {
 
+// `rows` runs of `width` bytes, `step` apart (width <= step).
 struct Span {
-  uintptr_t first, last;              // [first, last)
+  uintptr_t first;
+  size_t rows, width, step;
+  uintptr_t last() const { return first + (rows - 1) * step + width; }
 };
-Span span(const void* p, size_t bytes) { return {reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes}; }
-bool overlap(const Span& a, const Span& b) { return a.first < b.last && b.first < a.last; }
+Span span(const void* p, size_t bytes) { return {reinterpret_cast<uintptr_t>(p), p && bytes ? size_t{1} : size_t{0}, bytes, bytes}; }
+Span row_span(const void* p, int64_t rows, int64_t C, int64_t ld, int type) {
+  const size_t size = svg::type_bytes(type);
+  return {reinterpret_cast<uintptr_t>(p), p ? (size_t)rows : 0, (size_t)C * size, (size_t)(ld ? ld : C) * size};
+}
+// Column slices of one tensor lie in each other's gaps: with one step, runs whose places modulo the step differ never meet.  Runs of
+// different steps are taken to meet wherever the places between their first and last byte do.
+bool overlap(const Span& a, const Span& b) {
+  if (!a.rows || !b.rows || a.first >= b.last() || b.first >= a.last()) return false;
+  if (a.rows > 1 && b.rows > 1 && a.step != b.step) return true;
+  if (a.rows == 1 && b.rows == 1) return true;
+  const size_t step = a.rows > 1 ? a.step : b.step;
+  const size_t behind = b.first >= a.first ? (b.first - a.first) % step : (step - (a.first - b.first) % step) % step;
+  return behind < a.width || behind + b.width > step;
+}
 
 bool float_type(int t) { return t == SVG_BF16 || t == SVG_F16 || t == SVG_F32; }
 bool norm_kind(int n) { return n == SVG_NORM_NONE || n == SVG_NORM_RMS || n == SVG_NORM_LAYER; }
@@ -36,10 +52,6 @@ int check_gate_norm(const svg_gate_norm_t* d) {
   for (int64_t ld : lds)
     if ((__int128)std::max<int64_t>(d->rows, d->groups) * ld >= ((__int128)1 << 60)) return SVG_ERR_UNSUPPORTED;
   return SVG_OK;
-}
-
-size_t extent(int64_t rows, int64_t C, int64_t ld, int type) {
-  return rows ? ((size_t)(rows - 1) * (size_t)(ld ? ld : C) + (size_t)C) * svg::type_bytes(type) : 0;
 }
 
 // Checks a token matrix; fills t, its rows and columns and the bytes it spans.  An output's elements must not share places.
@@ -107,12 +119,9 @@ int svg_gate_norm_fwd(const svg_gate_norm_t* desc, const void* x, const void* y,
   const int sb = svg::type_bytes(d.stream_type), bb = svg::type_bytes(d.branch_type);
   if (misaligned(x, sb) || misaligned(r, sb) || misaligned(y, bb) || misaligned(h, bb)) return SVG_ERR_INVALID_ARG;
   if (svg::misaligned16(codes) || svg::misaligned16(scales)) return SVG_ERR_INVALID_ARG;
-  const Span in[2] = {span(x, extent(d.rows, d.C, d.ld_x, d.stream_type)),
-                      span(y, y ? extent(d.rows, d.C, d.ld_y, d.branch_type) : 0)};
-  const Span out[4] = {span(r, r ? extent(d.rows, d.C, d.ld_r, d.stream_type) : 0),
-                       span(h, h ? extent(d.rows, d.C, d.ld_h, d.branch_type) : 0),
-                       span(codes, codes ? svg::fp4_codes_bytes(d.rows, d.C) : 0),
-                       span(scales, codes ? svg::fp4_scales_bytes(d.rows, d.C) : 0)};
+  const Span in[2] = {row_span(x, d.rows, d.C, d.ld_x, d.stream_type), row_span(y, d.rows, d.C, d.ld_y, d.branch_type)};
+  const Span out[4] = {row_span(r, d.rows, d.C, d.ld_r, d.stream_type), row_span(h, d.rows, d.C, d.ld_h, d.branch_type),
+                       span(codes, svg::fp4_codes_bytes(d.rows, d.C)), span(scales, svg::fp4_scales_bytes(d.rows, d.C))};
   const bool in_place = r == x && (d.ld_r ? d.ld_r : d.C) == (d.ld_x ? d.ld_x : d.C);
   for (int o = 0; o < 4; ++o) {
     for (int k = 0; k < 2; ++k)
@@ -154,10 +163,9 @@ int svg_gate_norm_bwd(const svg_gate_norm_t* desc, const void* r, const void* y,
   if (need && (!workspace || workspace_bytes < need)) return SVG_ERR_WORKSPACE;
   if (svg::misaligned16(workspace)) return SVG_ERR_INVALID_ARG;
   const int64_t lx = d.ld_x ? d.ld_x : d.C, ly = d.ld_y ? d.ld_y : d.C, lr = d.ld_r ? d.ld_r : d.C, lh = d.ld_h ? d.ld_h : d.C;
-  const Span in[4] = {span(r, r ? extent(d.rows, d.C, lr, d.stream_type) : 0), span(y, y ? extent(d.rows, d.C, ly, d.branch_type) : 0),
-                      span(dr, dr ? extent(d.rows, d.C, lr, d.stream_type) : 0), span(dh, dh ? extent(d.rows, d.C, lh, d.branch_type) : 0)};
-  const Span out[3] = {span(dx, dx ? extent(d.rows, d.C, lx, d.stream_type) : 0), span(dy, dy ? extent(d.rows, d.C, ly, d.branch_type) : 0),
-                       span(workspace, need)};
+  const Span in[4] = {row_span(r, d.rows, d.C, lr, d.stream_type), row_span(y, d.rows, d.C, ly, d.branch_type),
+                      row_span(dr, d.rows, d.C, lr, d.stream_type), row_span(dh, d.rows, d.C, lh, d.branch_type)};
+  const Span out[3] = {row_span(dx, d.rows, d.C, lx, d.stream_type), row_span(dy, d.rows, d.C, ly, d.branch_type), span(workspace, need)};
   for (int o = 0; o < 3; ++o) {
     for (int k = 0; k < 4; ++k) {
       const bool in_place = (o == 0 && k == 2 && dx == dr && lx == lr) || (o == 1 && k == 1 && dy == y) ||

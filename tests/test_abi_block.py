@@ -157,3 +157,12 @@ def test_tensors_whose_extent_passes_64_bits_are_refused(strides):
     grads = S.gate_norm_grads(gate=A, ld_mod=2 ** 40)
     big = desc(rows=2 ** 20, groups=2 ** 20)
     assert S.lib().svg_gate_norm_bwd(C.byref(big), X, Y, Z, W, A, B_, C.byref(grads), None, 0, None) == -2
+
+
+def test_overlaps_of_rows_of_one_stride():
+    """Slices that reach one element into each other's columns, or around the end of a row into the next one's."""
+    wide = dict(ld_x=600, ld_r=600, ld_y=600, ld_h=600)
+    for columns in (-599, -255, -1, 1, 255, 345, 599, 600 * 63 + 255):
+        assert fwd(desc(**wide), r=X + 2 * columns) == -4, columns
+    assert fwd(desc(**{**wide, "ld_r": 602}), r=X + 2 * 300) == -4          # another stride: their rows meet somewhere
+    assert fwd(desc(rows=1, groups=1, **wide), r=X + 2 * 255) == -4

@@ -452,3 +452,31 @@ def test_parameters_that_a_norm_does_not_have_get_zero_gradients(post, pre, grou
         there = {"weight": pre != 0, "bias": pre == 2, "post_weight": post != 0, "post_bias": post == 2}
         for name, has in there.items():
             assert has or not got[name].any(), name
+
+
+@pytest.mark.parametrize("C", [64, 37, 520])
+def test_column_slices_of_one_tensor(C):
+    """Results beside their inputs in one tensor, without and with alignment: nothing is written outside of their columns."""
+    rows = 70
+    c = Case(rows, C, 2, [0, 31, rows], post=1, pre=2, seed=C)
+    r, h = run_forward(c)
+    grads = run_backward(c, ())
+    wide, wide_b = (torch.full((rows, 3 * C), 7.0, dtype=t, device="cuda") for t in (c.ts, c.tb))
+    cut = lambda t, i: t[:, i * C:(i + 1) * C]  # noqa: E731
+    cut(wide, 1).copy_(c.x)
+    cut(wide_b, 1).copy_(c.y)
+    desc = S.gate_norm_desc(rows, C, 2, c.ptr, post_norm=1, pre_norm=2, post_eps=EPS, eps=EPS, ld_x=3 * C, ld_y=3 * C, ld_r=3 * C, ld_h=3 * C,
+                            gate=c.gate, scale=c.scale, shift=c.shift, post_weight=c.post_weight, post_bias=c.post_bias, weight=c.weight,
+                            bias=c.bias)
+    S.svg_gate_norm_fwd(desc, cut(wide, 1), cut(wide_b, 1), cut(wide, 2), cut(wide_b, 2))
+    torch.cuda.synchronize()
+    assert torch.equal(cut(wide, 2), r) and torch.equal(cut(wide_b, 2), h)
+    assert torch.equal(cut(wide, 1), c.x) and torch.equal(cut(wide_b, 1), c.y) and (cut(wide, 0) == 7).all() and (cut(wide_b, 0) == 7).all()
+    for t, i, v in ((wide, 2, c.dr), (wide_b, 2, c.dh)):
+        cut(t, i).copy_(v)
+    n = S.svg_gate_norm_workspace_bytes(desc)
+    S.svg_gate_norm_bwd(desc, cut(wide, 1), cut(wide_b, 1), cut(wide, 2), cut(wide_b, 2), cut(wide, 0), cut(wide_b, 0), None,
+                        torch.empty(n, dtype=torch.uint8, device="cuda"), n)
+    torch.cuda.synchronize()
+    assert torch.equal(cut(wide, 0), grads["dx"]) and torch.equal(cut(wide_b, 0), grads["dy"])
+    assert torch.equal(cut(wide, 1), c.x) and torch.equal(cut(wide, 2), c.dr) and torch.equal(cut(wide_b, 1), c.y) and torch.equal(cut(wide_b, 2), c.dh)
