@@ -419,8 +419,8 @@ typedef struct svg_gate_norm {
  * h  branch, written, or NULL
  * codes, scales  the same h as a microscaled 4-bit operand (below), rounded from fp32; both or
  *    neither; C must be a multiple of 32, and all tensors 16-byte aligned with strides that are multiples of 8
- * At least one output.  Any other overlap of an output with a tensor: SVG_ERR_ALIAS.  Column slices of one tensor
- * (the same row stride in bytes) do not overlap.
+ * At least one output.  Any other overlap of an output with a tensor of the call or the descriptor: SVG_ERR_ALIAS.  Column
+ * slices of one tensor (the same row stride in bytes) do not overlap.
  */
 int svg_gate_norm_fwd(const svg_gate_norm_t* desc, const void* x, const void* y, void* r, void* h,
                       void* codes, void* scales, void* stream);

@@ -37,6 +37,8 @@ struct Tokens {
 bool tokens_vectors(const Tokens& t, const void* x);
 
 // Kernel launchers.  All arguments validated by the caller; rows > 0 except for the gradients.
+// Has the call a form that writes 4-bit codes?
+bool gate_norm_writes_codes(const svg_gate_norm_t& d, const void* x, const void* y, const void* r, const void* h);
 int launch_gate_norm(const svg_gate_norm_t& d, const void* x, const void* y, void* r, void* h, void* codes, void* scales,
                      hipStream_t stream);
 size_t gate_norm_workspace_bytes(const svg_gate_norm_t& d);

@@ -1,5 +1,6 @@
 // C-ABI entry points of the operators around the attention: argument checks, then the launchers.
 #include <algorithm>
+#include <array>
 
 #include "svg_block.h"
 
@@ -52,6 +53,15 @@ int check_gate_norm(const svg_gate_norm_t* d) {
   for (int64_t ld : lds)
     if ((__int128)std::max<int64_t>(d->rows, d->groups) * ld >= ((__int128)1 << 60)) return SVG_ERR_UNSUPPORTED;
   return SVG_OK;
+}
+
+// The tables and weights of a descriptor.
+constexpr int kParameters = 8;
+std::array<Span, kParameters> parameter_spans(const svg_gate_norm_t& d) {
+  auto table = [&](const float* p) { return row_span(p, d.groups, d.C, d.ld_mod, SVG_F32); };
+  auto vector = [&](const float* p) { return row_span(p, 1, d.C, 0, SVG_F32); };
+  return {table(d.gate), table(d.scale), table(d.shift), span(d.group_ptr, (size_t)(d.groups + 1ll) * sizeof(int32_t)),
+          vector(d.post_weight), vector(d.post_bias), vector(d.weight), vector(d.bias)};
 }
 
 // Checks a token matrix; fills t, its rows and columns and the bytes it spans.  An output's elements must not share places.
@@ -122,12 +132,16 @@ int svg_gate_norm_fwd(const svg_gate_norm_t* desc, const void* x, const void* y,
   const Span in[2] = {row_span(x, d.rows, d.C, d.ld_x, d.stream_type), row_span(y, d.rows, d.C, d.ld_y, d.branch_type)};
   const Span out[4] = {row_span(r, d.rows, d.C, d.ld_r, d.stream_type), row_span(h, d.rows, d.C, d.ld_h, d.branch_type),
                        span(codes, svg::fp4_codes_bytes(d.rows, d.C)), span(scales, svg::fp4_scales_bytes(d.rows, d.C))};
+  if (codes && d.rows && !svg::gate_norm_writes_codes(d, x, y, r, h)) return SVG_ERR_UNSUPPORTED;
+  const std::array<Span, kParameters> parameters = parameter_spans(d);
   const bool in_place = r == x && (d.ld_r ? d.ld_r : d.C) == (d.ld_x ? d.ld_x : d.C);
   for (int o = 0; o < 4; ++o) {
     for (int k = 0; k < 2; ++k)
       if (overlap(out[o], in[k]) && !(o == 0 && k == 0 && in_place)) return SVG_ERR_ALIAS;
     for (int k = o + 1; k < 4; ++k)
       if (overlap(out[o], out[k])) return SVG_ERR_ALIAS;
+    for (const Span& p : parameters)
+      if (overlap(out[o], p)) return SVG_ERR_ALIAS;
   }
   if (!d.rows) return SVG_OK;
   return svg::launch_gate_norm(d, x, y, r, h, codes, scales, static_cast<hipStream_t>(stream));

@@ -969,16 +969,26 @@ size_t gate_norm_workspace_bytes(const svg_gate_norm_t& d) {
   return (size_t)(g.strips + (long long)d.groups * (2 + (g.splits > 1 ? g.splits : 0))) * 4 * d.C * sizeof(float);
 }
 
+namespace {
+GateNormArgs forward_args(const svg_gate_norm_t& d, const void* x, const void* y, const void* r, const void* h) {
+  GateNormArgs a = gate_norm_args(d);
+  a.x = x; a.y = y; a.r = const_cast<void*>(r); a.h = const_cast<void*>(h);
+  return a;
+}
+}  // namespace
+
+bool gate_norm_writes_codes(const svg_gate_norm_t& d, const void* x, const void* y, const void* r, const void* h) {
+  return aligned(forward_args(d, x, y, r, h)) && d.C % 32 == 0;
+}
+
 int launch_gate_norm(const svg_gate_norm_t& d, const void* x, const void* y, void* r, void* h, void* codes, void* scales,
                      hipStream_t stream) {
-  GateNormArgs a = gate_norm_args(d);
-  a.x = x; a.y = y; a.r = r; a.h = h;
+  GateNormArgs a = forward_args(d, x, y, r, h);
   a.codes = static_cast<unsigned*>(codes);
   a.scales = static_cast<unsigned char*>(scales);
   a.col_tiles = (int)fp4_col_tiles(d.C);
   a.col_groups = (int)fp4_col_groups(d.C);
   const bool vec = aligned(a);
-  if (codes && (!vec || d.C % 32)) return SVG_ERR_UNSUPPORTED;
   if (codes) a.row_limit = fp4_row_tiles(d.rows) * kFp4Rows;
   const int bytes = type_bytes(d.stream_type) + 2;
   const Way w = way(d.C, vec, bytes);

@@ -166,3 +166,16 @@ def test_overlaps_of_rows_of_one_stride():
         assert fwd(desc(**wide), r=X + 2 * columns) == -4, columns
     assert fwd(desc(**{**wide, "ld_r": 602}), r=X + 2 * 300) == -4          # another stride: their rows meet somewhere
     assert fwd(desc(rows=1, groups=1, **wide), r=X + 2 * 255) == -4
+
+
+TABLES = ("gate", "scale", "shift", "group_ptr", "post_weight", "post_bias", "weight", "bias")
+
+
+@pytest.mark.parametrize("name", TABLES)
+def test_results_over_the_parameters_are_refused(name):
+    for out in (dict(r=Z), dict(h=W), dict(codes=Y, scales=B_), dict(codes=B_, scales=Y)):
+        at = next(v for k, v in out.items() if v != B_)
+        args = {**dict(x=X, y=None, r=7 * A, h=8 * A), **out}
+        assert fwd(desc(**{name: at}), **args) == -4, out
+        assert fwd(desc(**{name: at + 64}), **args) == -4, out
+    assert fwd(desc(ld_mod=512, gate=Z + 4 * 200), r=None, h=Z) == -4        # the second group's row of a table, one stride apart
