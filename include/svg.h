@@ -438,7 +438,8 @@ typedef struct svg_gate_norm_grads {
  *   y   branch [rows, C]: the branch's output; NULL if there was none
  *   dr  stream [rows, C]: gradient of r from what follows, or NULL (zero)
  *   dh  branch [rows, C]: gradient of h, or NULL (the forward pass had no h)
- *   dx, dy  written, or NULL.  dx == dr and dy == y or dy == dh (same stride) are allowed.
+ *   dx, dy  written, or NULL.  dx == dr and dy == y or dy == dh (same stride) are allowed.  Any other overlap of dx, dy,
+ *       the workspace or a parameter's gradient with each other or with a tensor of the call or the descriptor: SVG_ERR_ALIAS.
  * Sums are fp32 in an order that depends on the descriptor and the tensors' alignment only: results repeat bit for bit.
  * workspace: >= svg_gate_norm_workspace_bytes(desc), 16-byte aligned.
  */

@@ -179,15 +179,22 @@ int svg_gate_norm_bwd(const svg_gate_norm_t* desc, const void* r, const void* y,
   const int64_t lx = d.ld_x ? d.ld_x : d.C, ly = d.ld_y ? d.ld_y : d.C, lr = d.ld_r ? d.ld_r : d.C, lh = d.ld_h ? d.ld_h : d.C;
   const Span in[4] = {row_span(r, d.rows, d.C, lr, d.stream_type), row_span(y, d.rows, d.C, ly, d.branch_type),
                       row_span(dr, d.rows, d.C, lr, d.stream_type), row_span(dh, d.rows, d.C, lh, d.branch_type)};
-  const Span out[3] = {row_span(dx, d.rows, d.C, lx, d.stream_type), row_span(dy, d.rows, d.C, ly, d.branch_type), span(workspace, need)};
-  for (int o = 0; o < 3; ++o) {
+  auto table = [&](const float* p) { return row_span(p, d.groups, d.C, gr.ld_mod, SVG_F32); };
+  auto vector = [&](const float* p) { return row_span(p, 1, d.C, 0, SVG_F32); };
+  const Span out[10] = {row_span(dx, d.rows, d.C, lx, d.stream_type), row_span(dy, d.rows, d.C, ly, d.branch_type), span(workspace, need),
+                        table(gr.gate), table(gr.scale), table(gr.shift),
+                        vector(gr.post_weight), vector(gr.post_bias), vector(gr.weight), vector(gr.bias)};
+  const std::array<Span, kParameters> parameters = parameter_spans(d);
+  for (int o = 0; o < 10; ++o) {
     for (int k = 0; k < 4; ++k) {
       const bool in_place = (o == 0 && k == 2 && dx == dr && lx == lr) || (o == 1 && k == 1 && dy == y) ||
                             (o == 1 && k == 3 && dy == dh && ly == lh);
       if (overlap(out[o], in[k]) && !in_place) return SVG_ERR_ALIAS;
     }
-    for (int k = o + 1; k < 3; ++k)
+    for (int k = o + 1; k < 10; ++k)
       if (overlap(out[o], out[k])) return SVG_ERR_ALIAS;
+    for (const Span& p : parameters)
+      if (overlap(out[o], p)) return SVG_ERR_ALIAS;
   }
   return svg::launch_gate_norm_grad(d, r, y, dr, dh, dx, dy, gr, static_cast<float*>(workspace), static_cast<hipStream_t>(stream));
 }

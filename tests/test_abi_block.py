@@ -179,3 +179,32 @@ def test_results_over_the_parameters_are_refused(name):
         assert fwd(desc(**{name: at}), **args) == -4, out
         assert fwd(desc(**{name: at + 64}), **args) == -4, out
     assert fwd(desc(ld_mod=512, gate=Z + 4 * 200), r=None, h=Z) == -4        # the second group's row of a table, one stride apart
+
+
+GRADS = ("gate", "scale", "shift", "post_weight", "post_bias", "weight", "bias")
+
+
+@pytest.mark.parametrize("name", GRADS)
+def test_gradients_over_other_tensors_are_refused(name):
+    """Over the rows, the workspace, the descriptor's tables (a table is read again behind a gradient's write), and each other."""
+    d = desc(gate=100 * A, scale=101 * A, shift=102 * A, post_weight=103 * A, post_bias=104 * A, weight=105 * A, bias=106 * A, group_ptr=107 * A,
+             post_norm=2)
+    free = 110 * A
+    for at in (X, Y, Z, W, 7 * A, 8 * A, 9 * A, *(k * A for k in range(100, 108))):
+        assert bwd(d, grads=S.gate_norm_grads(**{name: at})) == -4, hex(at)
+        assert bwd(d, grads=S.gate_norm_grads(**{name: at + 8})) == -4, hex(at)
+    for other in GRADS:
+        if other != name:
+            assert bwd(d, grads=S.gate_norm_grads(**{name: free, other: free + 4 * 255})) == -4, other
+    table = name in GRADS[:3]
+    if table:                                                            # slices of one tensor that reach into each other
+        for columns in (-255, 255, 513, 600):
+            assert bwd(d, grads=S.gate_norm_grads(**{n: free if n == name else free + 4 * columns for n in (name, "shift" if name != "shift" else "gate")},
+                                                  ld_mod=600)) == -4, columns
+
+
+@pytest.mark.parametrize("name", TABLES)
+def test_row_gradients_and_workspace_over_the_parameters_are_refused(name):
+    d = desc(**{"gate": 100 * A, "scale": 101 * A, "shift": 102 * A, name: 110 * A})
+    for out in ("dx", "dy", "ws"):
+        assert bwd(d, **{out: 110 * A}) == -4, out
