@@ -254,8 +254,8 @@ int svg_fp4_linear(int64_t M, int64_t N, int64_t K, const void* a, const void* a
   if (!M) return SVG_OK;
   rc = check_workspace(M, N, K, workspace, workspace_bytes);
   if (rc != SVG_OK) return rc;
-  const Span in[4] = {span(a, svg::fp4_codes_bytes(M, K)), span(a_scales, svg::fp4_scales_bytes(M, K)), span(w, svg::fp4_codes_bytes(N, K)),
-                      span(w_scales, svg::fp4_scales_bytes(N, K))};
+  const Span in[5] = {span(a, svg::fp4_codes_bytes(M, K)), span(a_scales, svg::fp4_scales_bytes(M, K)), span(w, svg::fp4_codes_bytes(N, K)),
+                      span(w_scales, svg::fp4_scales_bytes(N, K)), span(bias, (size_t)N * sizeof(float))};
   const Span outs[2] = {span(out, bytes), span(workspace, svg::fp4_linear_workspace_bytes(M, N, K))};
   for (const Span& i : in)
     for (const Span& o : outs)
@@ -274,8 +274,8 @@ int svg_fp4_linear_quantize(int64_t M, int64_t N, int64_t K, const void* a, cons
   if (!M) return SVG_OK;
   rc = check_workspace(M, N, K, workspace, workspace_bytes);
   if (rc != SVG_OK) return rc;
-  const Span in[4] = {span(a, svg::fp4_codes_bytes(M, K)), span(a_scales, svg::fp4_scales_bytes(M, K)), span(w, svg::fp4_codes_bytes(N, K)),
-                      span(w_scales, svg::fp4_scales_bytes(N, K))};
+  const Span in[5] = {span(a, svg::fp4_codes_bytes(M, K)), span(a_scales, svg::fp4_scales_bytes(M, K)), span(w, svg::fp4_codes_bytes(N, K)),
+                      span(w_scales, svg::fp4_scales_bytes(N, K)), span(bias, (size_t)N * sizeof(float))};
   const Span outs[3] = {span(codes, svg::fp4_codes_bytes(M, N)), span(scales, svg::fp4_scales_bytes(M, N)),
                         span(workspace, svg::fp4_linear_workspace_bytes(M, N, K))};
   for (const Span& o : outs)

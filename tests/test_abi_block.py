@@ -208,3 +208,9 @@ def test_row_gradients_and_workspace_over_the_parameters_are_refused(name):
     d = desc(**{"gate": 100 * A, "scale": 101 * A, "shift": 102 * A, name: 110 * A})
     for out in ("dx", "dy", "ws"):
         assert bwd(d, **{out: 110 * A}) == -4, out
+
+
+def test_products_over_their_bias_are_refused():
+    for at in (9 * A, 9 * A - 4 * 255, 9 * A + 64):
+        assert linear(bias=at, out=9 * A) == -4 and linear_quantize(bias=at, codes=9 * A) == -4, hex(at)
+        assert linear_quantize(bias=at, scales=9 * A) == -4, hex(at)
