@@ -375,7 +375,8 @@ int svg_probe_lds(int form, int32_t waves, int32_t iterations, void* scratch, si
  * stride) instead of [B,H,N,D]; the projections read and write the [B,H,N,D] tensors of the
  * attention in place (svg_tokens_t).  As above: device pointers owned by the caller, no
  * allocation, no host synchronisation, arguments checked on the host before anything is
- * enqueued, graph capturable.  Calls with no rows return SVG_OK and enqueue nothing.
+ * enqueued, graph capturable.  Calls with no rows return SVG_OK and enqueue nothing, but for svg_gate_norm_bwd, which
+ * writes the parameters' gradients that are wanted as zeros.
  * ==========================================================================================
  */
 enum { SVG_BF16 = 0, SVG_F16 = 1, SVG_F32 = 2 };   /* element types */
