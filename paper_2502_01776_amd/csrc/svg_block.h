@@ -49,6 +49,11 @@ int launch_fp4_quantize(const Tokens& t, long long rows, int cols, const void* x
 int launch_fp4_dequantize(const Tokens& t, long long rows, int cols, const void* codes, const void* scales, void* x,
                           hipStream_t stream);
 size_t fp4_linear_workspace_bytes(long long M, long long N, long long K);
+// Forms of a product: operands straight from memory for one, two (K over eight or four wavefronts) and four token tiles; output
+// tiles of 64 x 128, 128 x 256 and 256 x 256.
+enum class LinearForm : int { kRows1, kRows2Eight, kRows2, kRows4, kTiles64, kTiles128, kSquare };
+// By row tiles of the tokens, pairs of column tiles of the output (of its whole operand where it is one) and column tiles of K.
+LinearForm fp4_linear_form(long long m_tiles, long long pairs, int k_tiles, bool activation);
 // tok and out, or codes and scales
 int launch_fp4_linear(long long M, int N, int K, const void* a, const void* a_scales, const void* w, const void* w_scales,
                       const float* bias, int activation, const Tokens* tok, void* out, void* codes, void* scales, void* workspace,

@@ -767,6 +767,19 @@ int launch_rows(const LinearArgs& a, Output out, hipStream_t stream) {
   return hip_status(hipGetLastError());
 }
 
+int launch(const LinearArgs& a, Output form, hipStream_t stream) {
+  switch (fp4_linear_form(a.m_tiles, a.n_pairs, a.kt, a.activation != SVG_ACT_NONE)) {
+    case LinearForm::kRows1: return launch_rows<1, 1, 8>(a, form, stream);
+    case LinearForm::kRows2Eight: return launch_rows<2, 1, 8>(a, form, stream);
+    case LinearForm::kRows2: return launch_rows<2, 1, 4>(a, form, stream);
+    case LinearForm::kRows4: return launch_rows<4, 1, 4>(a, form, stream);
+    case LinearForm::kTiles64: return launch_tiles<4, 1, 1, 4>(a, form, stream);
+    case LinearForm::kTiles128: return launch_tiles<8, 2, 1, 4>(a, form, stream);
+    default: return launch_square<8, 2, 2, 4>(a, form, stream);
+  }
+}
+
+}  // namespace
 
 // Which form a product takes, by estimates of its time: what a round of workgroups needs is a part for its beginning and end, more of it
 // with an activation, and one that grows with K.  A launch's workgroups of 256 x 256 run one to a compute unit, the smaller ones
@@ -783,25 +796,22 @@ int launch_rows(const LinearArgs& a, Output out, hipStream_t stream) {
 //   8000 x 4096 x 1024 35.1 33.5 46.3 86.1;  32760 x 20480 x 5120 1569 1558 2212
 // Straight, one token tile (K over 8 wavefronts), two (4, or 8 where there are fewer workgroups than compute units) and four (4):
 //   16 x 5120 x 5120 7.1 7.8 (8: 7.5) 8.9;  32 x 5120 x 5120 9.6 7.9 (7.5) 8.9;  32 x 20480 x 5120 22.8 15.7 (19.5) 17.6
-int launch(const LinearArgs& a, Output form, hipStream_t stream) {
-  const long long pairs = a.n_pairs, m = a.m_tiles;
-  if (m == 1) return launch_rows<1, 1, 8>(a, form, stream);
-  if (m == 2) return pairs < kComputeUnits ? launch_rows<2, 1, 8>(a, form, stream) : launch_rows<2, 1, 4>(a, form, stream);
-  if (m <= 4 || (m + 3) / 4 * pairs <= 400) return launch_rows<4, 1, 4>(a, form, stream);
+LinearForm fp4_linear_form(long long m, long long pairs, int kt, bool activation) {
+  if (m == 1) return LinearForm::kRows1;
+  if (m == 2) return pairs < kComputeUnits ? LinearForm::kRows2Eight : LinearForm::kRows2;
+  if (m <= 4 || (m + 3) / 4 * pairs <= 400) return LinearForm::kRows4;
   auto tiles = [&](int m_tiles, int n_pairs) { return (m + m_tiles - 1) / m_tiles * ((pairs + n_pairs - 1) / n_pairs); };
   auto rounds = [](long long tiles, double whole, double alone) {
     const long long rest = tiles % (2 * kComputeUnits);
     return (double)(tiles / (2 * kComputeUnits)) * whole + (rest > kComputeUnits ? whole : rest ? alone : 0.0);
   };
-  const double k = a.kt * 0.128, act = a.activation != SVG_ACT_NONE ? 1.0 : 0.0;
+  const double k = kt * 0.128, act = activation ? 1.0 : 0.0;
   const double square = (double)((tiles(16, 8) + kComputeUnits - 1) / kComputeUnits) * (9.0 + 3.5 * act + 5.1 * k);
   const double large = rounds(tiles(8, 8), 9.0 + 3.5 * act + 5.35 * k, 6.1 + 2.6 * act + 3.44 * k);
   const double one = 3.6 + 0.5 * act + 1.9 * k, small = rounds(tiles(4, 4), one, 0.85 * one);
-  if (square <= large && square <= small) return launch_square<8, 2, 2, 4>(a, form, stream);
-  return large <= small ? launch_tiles<8, 2, 1, 4>(a, form, stream) : launch_tiles<4, 1, 1, 4>(a, form, stream);
+  if (square <= large && square <= small) return LinearForm::kSquare;
+  return large <= small ? LinearForm::kTiles128 : LinearForm::kTiles64;
 }
-
-}  // namespace
 
 size_t fp4_linear_workspace_bytes(long long, long long, long long) { return 0; }
 
