@@ -301,3 +301,29 @@ def test_activations_far_from_zero():
             S.svg_fp4_linear(1, 32, 32, *quantise(v), *quantise(w), None, act, S.tokens_of(out), out)
             value = O.mx_values(*O.mx_quantise(f64(v)))[0, k]
             assert out[0, k].item() == (pytest.approx(value, rel=1e-6) if value > 0 else pytest.approx(0.0, abs=1e-30))
+
+
+@pytest.mark.parametrize("act", [S.SVG_ACT_SILU, S.SVG_ACT_GELU_TANH])
+@pytest.mark.parametrize("M", [1, 130])
+def test_activations_relative_to_their_value(act, M):
+    """The sum is zero, so an output is the activation of its bias, any fp32 number.  In units of 2^-24 of the value: the exponent is off by
+    1.224 |v| (its constant 0.224, one product) and 7.23 |z| (constants 2.23 and 4.23, square 1, sum 1, product 1), which counts with the share
+    1 - sigmoid; there also the exponential's unit in the last place (2); sum 1, reciprocal 2, product 1.  The reciprocal of what is above 2^126
+    may be flushed: |v| 2^-126."""
+    rng = np.random.default_rng(M)
+    v = np.concatenate([np.linspace(-87, 87, 4096), rng.normal(size=3000) * 3, -np.geomspace(1e-30, 12, 1000), np.geomspace(1e-30, 12, 96)]).astype(np.float32)
+    N, K = v.size, 64
+    a, w = quantise(torch.zeros(M, K, device="cuda")), quantise(torch.randn(N, K, device="cuda"))
+    out = torch.full((M, N), float("nan"), device="cuda")
+    S.svg_fp4_linear(M, N, K, *a, *w, torch.from_numpy(v).cuda(), act, S.tokens_of(out), out)
+    torch.cuda.synchronize()
+    x = v.astype(np.longdouble)
+    z = x if act == S.SVG_ACT_SILU else 2 * np.sqrt(np.longdouble(2) / np.longdouble(np.pi)) * (x + np.longdouble("0.044715") * x ** 3)
+    near = np.exp(-np.abs(z))
+    sigmoid, rest = np.where(z < 0, near, 1) / (1 + near), np.where(z < 0, 1, near) / (1 + near)
+    ref = x * sigmoid
+    units = ((1.224 if act == S.SVG_ACT_SILU else 7.23) * np.abs(z) + 2) * rest + 4
+    allowed = units * U * np.abs(ref) * (1 + 1e-4) + np.abs(x) * 2.0 ** -126
+    err = np.abs(f64(out).astype(np.longdouble) - ref)
+    assert (err <= allowed).all(), (act, float((err / allowed).max()))
+    assert torch.equal(out, out[:1].expand(M, N))
