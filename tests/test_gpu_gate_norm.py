@@ -7,6 +7,7 @@ import torch
 
 import paper_2502_01776_amd as S
 from oracle import block_oracle as O
+from workloads import CONFIGS
 
 pytestmark = pytest.mark.gpu
 
@@ -480,3 +481,18 @@ def test_column_slices_of_one_tensor(C):
     torch.cuda.synchronize()
     assert torch.equal(cut(wide, 0), grads["dx"]) and torch.equal(cut(wide_b, 0), grads["dy"])
     assert torch.equal(cut(wide, 1), c.x) and torch.equal(cut(wide, 2), c.dr) and torch.equal(cut(wide_b, 1), c.y) and torch.equal(cut(wide_b, 2), c.dh)
+
+
+@pytest.mark.parametrize("C", sorted({c["H"] * c["D"] for c in CONFIGS.values()}))
+def test_widths_of_the_workloads(C):
+    """Rows, gradients and the 4-bit form at the width of every workload of the library."""
+    for stream, post, pre in (("bf16", 0, 2), ("f32", 1, 1)):
+        c = Case(70, C, 2, [0, 30, 70], stream, "bf16", post, pre, seed=C)
+        codes, scales = (torch.full((S.svg_fp4_buffer_bytes(70, C, w),), 0xAA, dtype=torch.uint8, device="cuda") for w in (0, 1))
+        r, h = run_forward(c, codes=codes, scales=scales)
+        ref_r, ref_h = c.forward()
+        noise_r, noise_h = c.noise()
+        close(r, ref_r, HALF[c.ts], noise_r, "r")
+        close(h, ref_h, HALF[c.tb], noise_h, "h")
+        assert_four_bit(codes, scales, ref_h, noise_h)
+        check_backward(c)
