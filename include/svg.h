@@ -499,7 +499,8 @@ int svg_fp4_dequantize(const svg_tokens_t* tokens, const void* codes, const void
  * exponent in fp32: of their value they are off by at most 2^-24 times 8 for v >= 0, and for v < 0 times 6 + 1.3 |v| (SiLU) and
  * 6 + 7.3 |z|, z = 1.596 (v + 0.0447 v^3) (GELU); what is smaller than 2e-36 may become zero.  K >= 1, N >= 1; results repeat bit for bit.  An
  * output that overlaps an operand, the bias or another output: SVG_ERR_ALIAS.
- * workspace: >= svg_fp4_linear_workspace_bytes(M, N, K), 16-byte aligned; NULL where that is 0.
+ * workspace: >= svg_fp4_linear_workspace_bytes(M, N, K) bytes.  No form needs any: that is 0 for all sizes, and the arguments are
+ * not looked at.
  */
 size_t svg_fp4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
 int svg_fp4_linear(int64_t M, int64_t N, int64_t K, const void* a, const void* a_scales, const void* w,

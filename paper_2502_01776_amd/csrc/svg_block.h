@@ -48,7 +48,6 @@ int launch_fp4_quantize(const Tokens& t, long long rows, int cols, const void* x
                         hipStream_t stream);
 int launch_fp4_dequantize(const Tokens& t, long long rows, int cols, const void* codes, const void* scales, void* x,
                           hipStream_t stream);
-size_t fp4_linear_workspace_bytes(long long M, long long N, long long K);
 // Forms of a product: operands straight from memory for one, two (K over eight or four wavefronts) and four token tiles; output
 // tiles of 64 x 128, 128 x 256 and 256 x 256.
 enum class LinearForm : int { kRows1, kRows2Eight, kRows2, kRows4, kTiles64, kTiles128, kSquare };
@@ -56,7 +55,7 @@ enum class LinearForm : int { kRows1, kRows2Eight, kRows2, kRows4, kTiles64, kTi
 LinearForm fp4_linear_form(long long m_tiles, long long pairs, int k_tiles, bool activation);
 // tok and out, or codes and scales
 int launch_fp4_linear(long long M, int N, int K, const void* a, const void* a_scales, const void* w, const void* w_scales,
-                      const float* bias, int activation, const Tokens* tok, void* out, void* codes, void* scales, void* workspace,
+                      const float* bias, int activation, const Tokens* tok, void* out, void* codes, void* scales,
                       hipStream_t stream);
 
 __host__ __device__ constexpr int type_bytes(int type) { return type == SVG_F32 ? 4 : 2; }
@@ -101,7 +100,7 @@ __device__ __forceinline__ unsigned quad_max(unsigned x) {
   return max(x, (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0x4e, 0xf, 0xf, true));
 }
 
-// Eight neighbouring elements from / to memory (16-byte aligned), as fp32.
+// Eight neighbouring elements from memory (16-byte aligned), as fp32.
 template <int TYPE>
 __device__ __forceinline__ void load8(const void* base, size_t element, float (&v)[8]) {
   if constexpr (TYPE == SVG_F32) {
@@ -122,20 +121,7 @@ __device__ __forceinline__ void load8(const void* base, size_t element, float (&
     for (int e = 0; e < 8; ++e) v[e] = (float)a[e];
   }
 }
-template <int TYPE>
-__device__ __forceinline__ void store8(void* base, size_t element, const float (&v)[8]) {
-  const block_f32x8 f = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
-  if constexpr (TYPE == SVG_F32) {
-    block_f32x4* p = reinterpret_cast<block_f32x4*>(static_cast<float*>(base) + element);
-    p[0] = block_f32x4{v[0], v[1], v[2], v[3]};
-    p[1] = block_f32x4{v[4], v[5], v[6], v[7]};
-  } else if constexpr (TYPE == SVG_BF16) {
-    *reinterpret_cast<block_bf16x8*>(static_cast<unsigned short*>(base) + element) = __builtin_convertvector(f, block_bf16x8);
-  } else {
-    *reinterpret_cast<block_f16x8*>(static_cast<unsigned short*>(base) + element) = __builtin_convertvector(f, block_f16x8);
-  }
-}
-// The same at any element's address: the vector unit's loads and stores of 16 bytes need no alignment of their own.
+// From and to any element's address: the vector unit's loads and stores of 16 bytes need no alignment of their own.
 typedef unsigned block_u32x4_of2 __attribute__((ext_vector_type(4), aligned(2)));
 typedef unsigned block_u32x4_of4 __attribute__((ext_vector_type(4), aligned(4)));
 template <int TYPE>

@@ -109,13 +109,6 @@ int check_linear(int64_t M, int64_t N, int64_t K, const void* a, const void* a_s
   return SVG_OK;
 }
 
-int check_workspace(int64_t M, int64_t N, int64_t K, void* workspace, size_t bytes) {
-  const size_t need = svg::fp4_linear_workspace_bytes(M, N, K);
-  if (!need) return SVG_OK;
-  if (!workspace || bytes < need) return SVG_ERR_WORKSPACE;
-  return svg::misaligned16(workspace) ? SVG_ERR_INVALID_ARG : SVG_OK;
-}
-
 }  // namespace
 
 extern "C" {
@@ -235,14 +228,10 @@ int svg_fp4_dequantize(const svg_tokens_t* tokens, const void* codes, const void
   return svg::launch_fp4_dequantize(t, rows, (int)cols, codes, scales, x, static_cast<hipStream_t>(stream));
 }
 
-size_t svg_fp4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-  if (M < 1 || N < 1 || K < 1 || M > svg::kMaxTokenRows || N > svg::kMaxColumns || K > svg::kMaxColumns) return 0;
-  return svg::fp4_linear_workspace_bytes(M, N, K);
-}
+size_t svg_fp4_linear_workspace_bytes(int64_t, int64_t, int64_t) { return 0; }
 
 int svg_fp4_linear(int64_t M, int64_t N, int64_t K, const void* a, const void* a_scales, const void* w, const void* w_scales,
-                   const float* bias, int activation, const svg_tokens_t* out_desc, void* out, void* workspace,
-                   size_t workspace_bytes, void* stream) {
+                   const float* bias, int activation, const svg_tokens_t* out_desc, void* out, void*, size_t, void* stream) {
   int rc = check_linear(M, N, K, a, a_scales, w, w_scales, bias, activation);
   if (rc != SVG_OK) return rc;
   svg::Tokens t;
@@ -252,37 +241,28 @@ int svg_fp4_linear(int64_t M, int64_t N, int64_t K, const void* a, const void* a
   if (rc != SVG_OK) return rc;
   if (rows != M || cols != N || !out || misaligned(out, svg::type_bytes(t.type))) return SVG_ERR_INVALID_ARG;
   if (!M) return SVG_OK;
-  rc = check_workspace(M, N, K, workspace, workspace_bytes);
-  if (rc != SVG_OK) return rc;
   const Span in[5] = {span(a, svg::fp4_codes_bytes(M, K)), span(a_scales, svg::fp4_scales_bytes(M, K)), span(w, svg::fp4_codes_bytes(N, K)),
                       span(w_scales, svg::fp4_scales_bytes(N, K)), span(bias, (size_t)N * sizeof(float))};
-  const Span outs[2] = {span(out, bytes), span(workspace, svg::fp4_linear_workspace_bytes(M, N, K))};
   for (const Span& i : in)
-    for (const Span& o : outs)
-      if (overlap(i, o)) return SVG_ERR_ALIAS;
-  if (overlap(outs[0], outs[1])) return SVG_ERR_ALIAS;
-  return svg::launch_fp4_linear(M, (int)N, (int)K, a, a_scales, w, w_scales, bias, activation, &t, out, nullptr, nullptr, workspace,
+    if (overlap(i, span(out, bytes))) return SVG_ERR_ALIAS;
+  return svg::launch_fp4_linear(M, (int)N, (int)K, a, a_scales, w, w_scales, bias, activation, &t, out, nullptr, nullptr,
                                 static_cast<hipStream_t>(stream));
 }
 
 int svg_fp4_linear_quantize(int64_t M, int64_t N, int64_t K, const void* a, const void* a_scales, const void* w, const void* w_scales,
-                            const float* bias, int activation, void* codes, void* scales, void* workspace, size_t workspace_bytes,
-                            void* stream) {
+                            const float* bias, int activation, void* codes, void* scales, void*, size_t, void* stream) {
   int rc = check_linear(M, N, K, a, a_scales, w, w_scales, bias, activation);
   if (rc != SVG_OK) return rc;
   if (!codes || !scales || svg::misaligned16(codes) || svg::misaligned16(scales)) return SVG_ERR_INVALID_ARG;
   if (!M) return SVG_OK;
-  rc = check_workspace(M, N, K, workspace, workspace_bytes);
-  if (rc != SVG_OK) return rc;
   const Span in[5] = {span(a, svg::fp4_codes_bytes(M, K)), span(a_scales, svg::fp4_scales_bytes(M, K)), span(w, svg::fp4_codes_bytes(N, K)),
                       span(w_scales, svg::fp4_scales_bytes(N, K)), span(bias, (size_t)N * sizeof(float))};
-  const Span outs[3] = {span(codes, svg::fp4_codes_bytes(M, N)), span(scales, svg::fp4_scales_bytes(M, N)),
-                        span(workspace, svg::fp4_linear_workspace_bytes(M, N, K))};
+  const Span outs[2] = {span(codes, svg::fp4_codes_bytes(M, N)), span(scales, svg::fp4_scales_bytes(M, N))};
   for (const Span& o : outs)
     for (const Span& i : in)
       if (overlap(i, o)) return SVG_ERR_ALIAS;
-  if (overlap(outs[0], outs[1]) || overlap(outs[0], outs[2]) || overlap(outs[1], outs[2])) return SVG_ERR_ALIAS;
-  return svg::launch_fp4_linear(M, (int)N, (int)K, a, a_scales, w, w_scales, bias, activation, nullptr, nullptr, codes, scales, workspace,
+  if (overlap(outs[0], outs[1])) return SVG_ERR_ALIAS;
+  return svg::launch_fp4_linear(M, (int)N, (int)K, a, a_scales, w, w_scales, bias, activation, nullptr, nullptr, codes, scales,
                                 static_cast<hipStream_t>(stream));
 }
 

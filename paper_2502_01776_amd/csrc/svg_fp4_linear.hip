@@ -813,8 +813,6 @@ LinearForm fp4_linear_form(long long m, long long pairs, int kt, bool activation
   return large <= small ? LinearForm::kTiles128 : LinearForm::kTiles64;
 }
 
-size_t fp4_linear_workspace_bytes(long long, long long, long long) { return 0; }
-
 namespace {
 // Do the tokens of an output tile of 256 x 256 ascend in memory, and does it span less than 2^29 bytes?  (They may lie in as many batch entries.)
 bool tile_spans_little(const Tokens& t, long long M, int N) {
@@ -827,7 +825,7 @@ bool tile_spans_little(const Tokens& t, long long M, int N) {
 }  // namespace
 
 int launch_fp4_linear(long long M, int N, int K, const void* a, const void* a_scales, const void* w, const void* w_scales,
-                      const float* bias, int activation, const Tokens* tok, void* out, void* codes, void* scales, void*,
+                      const float* bias, int activation, const Tokens* tok, void* out, void* codes, void* scales,
                       hipStream_t stream) {
   LinearArgs A = {};
   A.a = static_cast<const unsigned char*>(a);

@@ -464,7 +464,6 @@ __global__ __launch_bounds__(64 * kMaxWaves, FP4 && VPL == 1 ? 5 : 4) void gate_
       if (a.h && there) team.lane.template store<TB>(a.h, (size_t)row * a.ld_h, v);
     }
     if constexpr (FP4) {
-      if (row >= a.row_limit) continue;
       const long long rt = row / kFp4Rows;
       const int i16 = (int)(row % kFp4Rows);
 #pragma unroll
@@ -540,8 +539,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_grad_kernel(GateNorm
   const int turns = (int)min((long long)a.strip, a.rows - r0);
   for (int k = 0; k < turns; ++k) {
     const long long row = r0 + k;
-    const bool there = row < a.rows;
-    if (there && row >= group_end) {
+    if (row >= group_end) {
       const int now = group_of(a, row, group_end);
       if (now != group) {
         if (group >= 0) {
@@ -623,17 +621,15 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_grad_kernel(GateNorm
         for (int i = 0; i < N; ++i) d[i] += e[i];
       }
     }
-    if (a.dx && there) {
+    if (a.dx) {
 #pragma unroll
       for (int i = 0; i < N; ++i) e[i] = a.alpha * d[i];
       team.lane.template store<TS>(a.dx, (size_t)row * a.ld_x, e);
     }
-    if (there) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        t1[i] += d[i];
-        t2[i] = __builtin_fmaf(d[i], yhat[i], t2[i]);
-      }
+    for (int i = 0; i < N; ++i) {
+      t1[i] += d[i];
+      t2[i] = __builtin_fmaf(d[i], yhat[i], t2[i]);
     }
     if (a.dy) {
 #pragma unroll
@@ -651,7 +647,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gate_norm_grad_kernel(GateNorm
 #pragma unroll
         for (int i = 0; i < N; ++i) d[i] = rho_y * __builtin_fmaf(-yhat[i], m2, d[i] - m1);
       }
-      if (there) team.lane.template store<TB>(a.dy, (size_t)row * a.ld_y, d);
+      team.lane.template store<TB>(a.dy, (size_t)row * a.ld_y, d);
     }
   }
   if constexpr (!SINGLE) wait_ring<0>();
