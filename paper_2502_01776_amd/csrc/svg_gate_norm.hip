@@ -910,6 +910,13 @@ Way way(int C, bool whole, int bytes) {                  // bytes of an element 
   if (row.waves <= kMaxWaves && depth(row)) return {form, row, depth(row)};
   return {kSingle, row_shape(C), 0};
 }
+// Gradients of two vectors a lane always come in registers: beside their sums and tables the 128 registers of 16 wavefronts hold no
+// row, and what is spilt in front of a ring is read back behind its waits (bf16, 8200 x 12288 2634 us through the ring, 1408 in registers; 4000 x 9001
+// 2971 and 617; fp32 stream, 8200 x 12288 6617 and 1749, 4000 x 16384 1229 and 1259).  Still 0.7 to 1 TB/s.
+Way grad_way(int C, bool whole, int bytes) {
+  const Way w = way(C, whole, bytes);
+  return w.row.vpl == 1 ? w : Way{kSingle, row_shape(C), 0};
+}
 // f(form, depth) as integral constants
 template <class F>
 void with_way(const Way& w, F f) {
@@ -949,7 +956,7 @@ struct GradShape {                    // by the descriptor alone: the workspace 
 GradShape grad_shape(const svg_gate_norm_t& d) {
   GradShape g;
   const int bytes = 2 * (type_bytes(d.stream_type) + 2);
-  const Way w = way(d.C, true, bytes);
+  const Way w = grad_way(d.C, true, bytes);
   g.strip = std::max(strip_rows(d.rows, w.row.waves, 16, w.bytes(bytes)), kGradLeast);
   g.strips = (d.rows + g.strip - 1) / g.strip;
   // parts of the strips that are added up side by side: enough workgroups for the chip, at least 128 strips each
@@ -1015,7 +1022,7 @@ int launch_gate_norm_grad(const svg_gate_norm_t& d, const void* r, const void* y
   a.partial = workspace;
   const GradShape g = grad_shape(d);
   const int bytes = 2 * (type_bytes(d.stream_type) + 2);
-  const Way w = way(d.C, aligned(a), bytes);
+  const Way w = grad_way(d.C, aligned(a), bytes);
   a.waves = w.row.waves;
   a.strip = g.strip;
   (void)hipGetLastError();
@@ -1027,8 +1034,10 @@ int launch_gate_norm_grad(const svg_gate_norm_t& d, const void* r, const void* y
       with_way(w, [&](auto form, auto depth) {
         constexpr Form FORM = decltype(form)::value;
         constexpr int D = decltype(depth)::value;
-        static std::atomic<unsigned long long> allowed;
-        e = launch_with_lds(gate_norm_grad_kernel<TS, TB, VPL, D, FORM>, allowed, grid, block, w.bytes(bytes), stream, a);
+        if constexpr (VPL == 1 || FORM == kSingle) {
+          static std::atomic<unsigned long long> allowed;
+          e = launch_with_lds(gate_norm_grad_kernel<TS, TB, VPL, D, FORM>, allowed, grid, block, w.bytes(bytes), stream, a);
+        }
       });
     });
     if (e != hipSuccess) return hip_status(e);
