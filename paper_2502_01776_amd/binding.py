@@ -361,14 +361,16 @@ def gate_norm_grads(gate=None, scale=None, shift=None, post_weight=None, post_bi
 
 def tokens_of(x) -> SvgTokens:
     """The token matrix of a tensor [rows, columns] or [B, H, N, D] with neighbouring last elements."""
-    shape, stride = x.shape, x.stride()
+    shape, stride, kind = x.shape, x.stride(), _TYPE_OF.get(x.dtype)
     if len(shape) not in (2, 4):
         raise ValueError("a token matrix is [rows, columns] or [B, H, N, D]")
     if stride[-1] != 1 and shape[-1] > 1:
         raise ValueError("the elements of a row (of a head) have to be neighbours")
+    if kind is None:
+        raise ValueError(f"a token matrix has no element type {x.dtype}: bfloat16, float16 or float32")
     if len(shape) == 2:
-        return SvgTokens(1, shape[0], 1, shape[1], 0, stride[0], 0, _TYPE_OF[x.dtype])
-    return SvgTokens(shape[0], shape[2], shape[1], shape[3], stride[0], stride[2], stride[1], _TYPE_OF[x.dtype])
+        return SvgTokens(1, shape[0], 1, shape[1], 0, stride[0], 0, kind)
+    return SvgTokens(shape[0], shape[2], shape[1], shape[3], stride[0], stride[2], stride[1], kind)
 
 
 def svg_gate_norm_fwd(desc, x, y, r, h, codes=None, scales=None, stream=None):

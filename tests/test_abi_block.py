@@ -214,3 +214,11 @@ def test_products_over_their_bias_are_refused():
     for at in (9 * A, 9 * A - 4 * 255, 9 * A + 64):
         assert linear(bias=at, out=9 * A) == -4 and linear_quantize(bias=at, codes=9 * A) == -4, hex(at)
         assert linear_quantize(bias=at, scales=9 * A) == -4, hex(at)
+
+
+def test_token_matrices_of_other_types_are_refused():
+    import torch
+    for dtype in (torch.float64, torch.int32, torch.float8_e4m3fn):
+        for shape in ((4, 6), (1, 2, 3, 4)):
+            with pytest.raises(ValueError, match="element type"):
+                S.tokens_of(torch.zeros(shape).to(dtype))
