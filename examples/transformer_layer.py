@@ -39,7 +39,10 @@ class Operand:
                                    for part in (S.SVG_FP4_CODES, S.SVG_FP4_SCALES))
 
     def write(self, x, activation=S.SVG_ACT_NONE):
-        S.svg_fp4_quantize(S.tokens_of(x), x, activation, self.codes, self.scales)
+        tokens = S.tokens_of(x)
+        if (tokens.B * tokens.N, tokens.H * tokens.D) != (self.rows, self.cols):
+            raise ValueError(f"the operand is {self.rows} x {self.cols}, not {tokens.B * tokens.N} x {tokens.H * tokens.D}")
+        S.svg_fp4_quantize(tokens, x, activation, self.codes, self.scales)
         return self
 
 
@@ -51,6 +54,8 @@ class Linear:
         self.weight, self.bias = Operand(self.N, self.K).write(weight), bias
 
     def _operands(self, a):
+        if a.cols != self.K:
+            raise ValueError(f"the projection's operand has {self.K} columns, not {a.cols}")
         bytes_ = S.svg_fp4_linear_workspace_bytes(a.rows, self.N, self.K)
         workspace = torch.empty(bytes_, dtype=torch.uint8, device="cuda") if bytes_ else None
         return (a.rows, self.N, self.K, a.codes, a.scales, self.weight.codes, self.weight.scales, self.bias), (workspace, bytes_)
@@ -62,6 +67,8 @@ class Linear:
 
     def to_operand(self, a, out, activation):
         product, workspace = self._operands(a)
+        if (out.rows, out.cols) != (a.rows, self.N):
+            raise ValueError(f"the projection's result is {a.rows} x {self.N}, not {out.rows} x {out.cols}")
         S.svg_fp4_linear_quantize(*product, activation, out.codes, out.scales, *workspace)
         return out
 
@@ -105,6 +112,8 @@ class Layer:
 
     def forward(self, x, embedding):
         """x: bf16 [B N, C]; embedding: [B, C] of any of the element types.  Returns the next layer's x."""
+        if x.shape != (self.rows, self.C) or x.dtype != torch.bfloat16 or not x.is_contiguous():
+            raise ValueError(f"x has to be [{self.rows}, {self.C}] in bfloat16, row behind row")
         self.modulation(self.emb.write(embedding, S.SVG_ACT_SILU), self.mod)
         S.svg_gate_norm_fwd(self.before, x, None, None, None, self.h1.codes, self.h1.scales)
         for proj, out in ((self.q_proj, self.q), (self.k_proj, self.k), (self.v_proj, self.v)):
