@@ -476,7 +476,8 @@ typedef struct svg_tokens {
  *           tile, the even column of two in the low half of a byte
  *   scales  per row tile groups of four column tiles (the last group may be half used), in each
  *           64 pieces of 4 bytes; byte j of piece 16 g + i belongs to piece 16 g + i of the group's column tile j
- * Rows are padded to a multiple of 16 and columns to one of 256; the padding's codes are zero.
+ * Rows are padded to a multiple of 16 and columns to one of 256; the padding's codes and scale bytes are zero (a product takes it
+ * as part of K, where a scale byte of 255 would make it NaN).  Scale bytes of column tiles that do not exist are not looked at.
  * svg_fp4_buffer_bytes(rows, cols, SVG_FP4_CODES / _SCALES): sizes (0 for sizes out of range).
  * Buffers are 16-byte aligned.  rows 0 .. 2^31 - 64, cols 1 .. 2^20.
  *

@@ -327,3 +327,21 @@ def test_activations_relative_to_their_value(act, M):
     err = np.abs(f64(out).astype(np.longdouble) - ref)
     assert (err <= allowed).all(), (act, float((err / allowed).max()))
     assert torch.equal(out, out[:1].expand(M, N))
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 32), (17, 64), (33, 288), (70, 544), (500, 1312), (1030, 4128)])
+def test_the_padding_of_every_writer_is_zero(rows, cols):
+    """Codes and scale bytes behind the last row and column, in column tiles that exist: a product takes them as part of K."""
+    x = torch.randn(rows, cols, device="cuda")
+    w, a = quantise(torch.randn(cols, 64, device="cuda")), quantise(torch.randn(rows, 64, device="cuda"))
+    bias = torch.full((cols,), 5.0, device="cuda")
+    product, norm = buffers(rows, cols), buffers(rows, cols)
+    S.svg_fp4_linear_quantize(rows, cols, 64, *a, *w, bias, S.SVG_ACT_NONE, *product)
+    S.svg_gate_norm_fwd(S.gate_norm_desc(rows, cols, stream_type=S.SVG_F32, pre_norm=2, shift=bias), x, None, None, None, *norm)
+    torch.cuda.synchronize()
+    rt, ct = -(-rows // 16), -(-cols // 256) * 2
+    for name, q in (("quantiser", quantise(x)), ("product", product), ("norm", norm)):
+        codes, scales = O.from_operand(*(t.cpu().numpy() for t in q), rt * 16, ct * 128)
+        assert not codes[rows:].any() and not codes[:, cols:].any(), name
+        assert not scales[rows:].any() and not scales[:, -(-cols // 32):].any(), name
+        assert scales[:rows, :cols // 32].all(), name
