@@ -54,3 +54,25 @@ def test_rows_on_their_way_are_not_waited_for(compiled):
         assert not bad, (k.name, bad)
         checked += 1
     assert checked == 8 + 2
+
+
+def test_rows_of_every_type_depth_and_alignment_are_not_waited_for(compiled):
+    """The same for every ring of one vector a lane: all types, one to three rows ahead, aligned rows and granules, with and without 4 bits.
+    Gradients of two vectors have no ring."""
+    if compiled[0] != "svg_gate_norm.hip":
+        pytest.skip("the ring of rows is the norm's")
+    checked = {"gate_norm_kernel": 0, "gate_norm_grad_kernel": 0}
+    for k in compiled[1]:
+        m = re.search(r"(gate_norm_kernel|gate_norm_grad_kernel)ILi\dELi\dELi(\d)ELi\dELNS0_4FormE(\d)E", k.name)
+        if not m or m.group(3) == "2":
+            continue
+        assert m.groups()[:2] != ("gate_norm_grad_kernel", "2"), k.name
+        if m.group(2) == "2":
+            continue
+        waits = [i for i, (op, args, asm) in enumerate(k.ins) if asm and op == "s_waitcnt" and args[0].startswith("vmcnt(") and args[0] != "vmcnt(0)"]
+        barriers = [i for i, (op, _, _) in enumerate(k.ins) if op == "s_barrier"]
+        inside = [(op, args) for op, args, asm in k.ins[waits[-1] + 1:barriers[-1]] if not asm]
+        bad = [(op, args) for op, args in inside if op.startswith("scratch_load") or (op == "s_waitcnt" and any("vmcnt" in a for a in args))]
+        assert not bad, (k.name, bad)
+        checked[m.group(1)] += 1
+    assert checked == {"gate_norm_kernel": 4 * 3 * 3, "gate_norm_grad_kernel": 4 * 3 * 2}
