@@ -396,7 +396,9 @@ enum { SVG_BF16 = 0, SVG_F16 = 1, SVG_F32 = 2 };   /* element types */
  * group g holds rows group_ptr[g] to group_ptr[g + 1] - 1 (device int32 [groups + 1],
  * ascending; the first and the last entry are taken to be 0 and rows, groups may be empty).
  * group_ptr == NULL: groups of rows / groups rows each (rows must be a multiple).  groups ==
- * rows gives every token its own modulation.
+ * rows gives every token its own modulation: made for the forward pass; the gradients' sums are slow over very many groups
+ * (32760 rows and groups of 5120 channels take 68 ms and 5.4 GB of workspace).  So are all gradients above 8192 channels, whose
+ * sums the registers do not hold (0.7 to 1 TB/s).
  */
 typedef struct svg_gate_norm {
   int64_t rows;                     /* token rows, 0 .. 2^31 - 64 */

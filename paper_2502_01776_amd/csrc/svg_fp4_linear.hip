@@ -546,9 +546,11 @@ int launch_tiles(const LinearArgs& a, Output out, hipStream_t stream) {
 // Output tiles of 256 x 256 for large products: eight wavefronts of 8 token tiles x 2 pairs, both operands through LDS in four stages of a
 // step each, asked for four steps ahead; one barrier a step, in front of its last pair of products, behind which the loads of the
 // stage that is free are issued between products.  The 128 x 64 outputs of a wavefront take 12 KB of LDS reads for 32 products.
-// 32760 x 5120 x 20480: 1340 us, 5.1 PFLOP/s; the matrix units are busy 69 % of the cycles at 1.78 GHz (a loop of the same products from
-// registers alone reaches 6.4 to 6.8 PFLOP/s on random operands, 9.5 on zeros: power).  32760 x 20480 x 5120 behind GELU: 1560 us, 50 of them
-// the activation.
+// 32760 x 5120 x 20480: 1315 us into 4 bits and 1365 into bf16 rows, 5.2 and 5.0 PFLOP/s; the matrix units are busy 69 % of the cycles at 1.78 GHz
+// (a loop of the same products from registers alone reaches 6.4 to 6.8 PFLOP/s on random operands, 9.5 on zeros: power).  32760 x 20480 x 5120: 1477 and
+// 1527 us, behind GELU 1585 and 1608.
+// What a round of tiles costs beside its K part (9 us) is largely the wait for the results of the tile before: their stores are issued behind the
+// next tile's first loads, and the counts of its first steps are of loads alone, so the stores have to end first.
 constexpr int kStages = 4;
 
 template <int TM, int TP, int WM, int WN>
@@ -785,9 +787,9 @@ int launch(const LinearArgs& a, Output form, hipStream_t stream) {
 // with an activation, and one that grows with K.  A launch's workgroups of 256 x 256 run one to a compute unit, the smaller ones
 // two, and one that has its compute unit to itself is faster.  In us, K in thousands:
 //   256 x 256: 9 + 5.1 K a round of 256;  128 x 256: 9 + 5.35 K a round of 512, 6.1 + 3.44 K for a last one of up to 256;
-//   64 x 128: 3.6 + 1.9 K, 85 % of it;  an activation: + 3.5, 3.5, 2.6, 0.5.
+//   64 x 128: 3.6 + 1.9 K, 85 % of it;  an activation: + 3.5, 3.5, 2.6, 0.5 (a fit over the products below; 2.0 to 2.7 in 40 rounds of 32760 x 20480 x 5120).
 // Up to 64 tokens, or up to 400 workgroups of 64 tokens and 32 columns, operands straight from memory (K split over the wavefronts).
-// us, 256 x 256 | 128 x 256 | 64 x 128 | straight (M x N x K):
+// us, 256 x 256 | 128 x 256 | 64 x 128 | straight (M x N x K), all forms in one run; between runs a time differs by up to 4 %:
 //   64 x 5120 x 5120 30.3 22.9 12.5 9.3;  226 x 5120 x 4096 27.1 19.5 10.9 13.3;  226 x 1536 x 1536 15.8 11.3 6.9 6.4;
 //   1573 x 512 x 512 11.3 8.6 6.0 5.9;  1573 x 1536 x 6144 34.3 25.4 16.8 26.7;  1573 x 6144 x 1536 17.3 17.2 18.0 26.6;
 //   4096 x 1536 x 1536 17.0 12.4 13.5 17.5;  2048 x 5120 x 5120 33.3 34.5 36.6 63.3;  4096 x 5120 x 5120 73.4 60.2 77.8 117;
