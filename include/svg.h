@@ -513,6 +513,109 @@ int svg_fp4_linear_quantize(int64_t M, int64_t N, int64_t K, const void* a, cons
                             const void* w_scales, const float* bias, int activation, void* codes, void* scales,
                             void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Few rows of activations (a timestep's embedding, the newest token of a sequence) times weights kept in 4 bits:
+ *     out[m, n] = act(sum_k in_act(x[m, k]) w[n, k] + bias[n])        m < M, n < N, k < K
+ * as svg_fp4_linear, but the activations stay as they are: x is a token matrix of B*N = M rows and H*D = K columns, in_act is taken in
+ * fp32 and not rounded, and every product is exact in the accumulation's fp32.  w, w_scales: an operand [N, K] (svg_fp4_quantize).  out: a token
+ * matrix of M rows and N columns, which must not overlap an input (SVG_ERR_ALIAS).  M <= 1024; made for up to 16 rows (every further
+ * 16 read the weights once more).  An infinite or NaN activation makes its row NaN or infinite.  K >= 1, N >= 1; results repeat bit for bit.
+ */
+int svg_fp4_linear_rows(const svg_tokens_t* x_desc, const void* x, int in_activation, int64_t N, const void* w, const void* w_scales,
+                        const float* bias, int activation, const svg_tokens_t* out_desc, void* out, void* stream);
+
+/*
+ * ==========================================================================================
+ * A cache of keys and values in 4 bits, for video that is generated chunk by chunk: the tokens
+ * so far stay as microscaled 4-bit floating point (4.25 bits an element), the next chunk's
+ * queries attend to them.
+ *
+ * The cache is a pool of `pages` pages of `page_size` tokens.  For each page and head it holds one record of
+ * page_size (D + D/16) bytes, pages outermost:
+ *   keys' codes    [page_size][D/2]     the even element of two in the low half of a byte
+ *   values' codes  [page_size][D/2]
+ *   keys' scales   [page_size][D/32]    a byte E + 127 for 32 neighbouring elements, as in svg_fp4_quantize
+ *   values' scales [page_size][D/32]
+ * Row b of the page table names the pages of sequence b in the order of its tokens: token j of it lies at place j % page_size of
+ * page page_table[b][j / page_size].  A slot is page * page_size + place.  An entry outside of 0 .. pages - 1 (say -1) is a page that
+ * is not there: nobody sees its tokens.  What lies behind a sequence's length, in pages or table, is never looked at for a result.
+ * ==========================================================================================
+ */
+typedef struct svg_kv4 {
+  int32_t B;                        /* sequences, 0 .. 65536 */
+  int32_t H, D;                     /* heads of keys and values; head dimension, 64 or 128 */
+  int32_t page_size;                /* a power of two, 16 .. 65536 */
+  int32_t pages, max_pages;         /* pages of the pool; entries of a row of the page table */
+  int64_t reserved;                 /* 0 */
+  void* data;                       /* device, 16-byte aligned: svg_kv4_bytes(cache) */
+  int32_t* page_table;              /* device [B, max_pages] */
+} svg_kv4_t;
+
+/* Bytes of the pool (0 for sizes out of range).  The fields that a call does not name below are not looked at. */
+size_t svg_kv4_bytes(const svg_kv4_t* cache);
+
+/*
+ * Sequences grow and shrink: the page table, the stack of free pages and the slots of the new tokens, from the lengths, on the device.
+ *   lengths    int32 [B]: tokens that the sequences hold
+ *   wanted     int32 [B]: tokens that they are to hold (0: finished)
+ *   free_pages int32 [pages], free_count int32 [1]: a stack, free_pages[*free_count - 1] on top
+ * Pages are given back first, of every sequence with fewer pages wanted than held those behind, sequences and pages ascending, and
+ * pushed; then every sequence that needs more takes pages from the top, sequences and pages ascending.  Table entries of pages given
+ * back keep what they held.
+ *   new_lengths int32 [B], new_count int32 [1]: written; each may be lengths or free_count itself
+ *   slots      int64 [B, tokens], or NULL: the slots of tokens lengths[b], lengths[b] + 1, .. of sequence b up to wanted[b], then -1
+ *   status     int32 [1]: SVG_KV4_OK; SVG_KV4_FULL: too few free pages; SVG_KV4_LENGTHS: a length or count out of range, a sequence that
+ *              grows by more than `tokens` (where slots are wanted), or a stack with no room for what is given back.  In the last two
+ *              cases nothing but new_lengths (= lengths), new_count (= *free_count) and slots (-1) is written.
+ * Uses B, page_size, pages, max_pages and page_table of the cache.  Overlaps of what is written with anything else: SVG_ERR_ALIAS.
+ */
+enum { SVG_KV4_OK = 0, SVG_KV4_FULL = 1, SVG_KV4_LENGTHS = 2 };
+int svg_kv4_resize(const svg_kv4_t* cache, const int32_t* lengths, const int32_t* wanted, int32_t* free_pages, const int32_t* free_count,
+                   int32_t* new_lengths, int32_t* new_count, int64_t* slots, int32_t tokens, int32_t* status, void* stream);
+
+/*
+ * svg_kv4_write  keys and values (token matrices [B,H,N,D], or one of H*D columns) into the cache; row m = b*N + n goes to slots[m]
+ * svg_kv4_read   the values that they stand for out of it, rounded to k's and v's types (exact in bf16 and fp32 but for underflow)
+ * Both skip rows whose slot is outside of the pool: those of k and v are left as they were.  The slots of a write have to differ
+ * (of two rows with one slot, parts of both may stay).  k and v have equal B, H, N and D; the cache's B is not looked at.
+ * A block of 32 elements that holds an infinity or a NaN stands for 32 NaNs.  slots: device int64 [B*N].
+ */
+int svg_kv4_write(const svg_kv4_t* cache, const svg_tokens_t* k_desc, const void* k, const svg_tokens_t* v_desc, const void* v,
+                  const int64_t* slots, void* stream);
+int svg_kv4_read(const svg_kv4_t* cache, const int64_t* slots, const svg_tokens_t* k_desc, void* k, const svg_tokens_t* v_desc, void* v,
+                 void* stream);
+
+/*
+ * Attention of queries over the cache.  The queries of sequence b are its last q_len[b] tokens of kv_len[b] (their own keys
+ * and values are in the cache already): query i stands at place p = kv_len[b] - q_len[b] + i.  With blocks of `block` tokens (a frame; 1: single
+ * tokens) it sees token j < kv_len[b] if the page of j is there and
+ *     causal == 0  or  floor(j / block) <= floor(p / block)              its own block and those before
+ *     window < 0   or  floor(j / block) >= floor(p / block) - window  or  j < sink
+ * A query that sees nothing has the result 0 and the log-sum-exp -inf.
+ */
+typedef struct svg_kv4_attn {
+  float softmax_scale;              /* <= 0 selects 1/sqrt(D) */
+  int32_t causal;                   /* 0 or 1 */
+  int32_t block;                    /* >= 1 */
+  int32_t window;                   /* blocks before its own that a query sees; < 0: all */
+  int32_t sink;                     /* tokens at the beginning that every query sees, >= 0 */
+  int32_t max_kv;                   /* the longest kv_len, if known: the work is divided by it; 0: max_pages * page_size */
+  const int32_t* kv_len;            /* device [B]; taken as at most max_pages * page_size, and as 0 where negative */
+  const int32_t* q_len;             /* device [B]; NULL: N each; taken as at most N, and as 0 where negative */
+} svg_kv4_attn_t;
+
+/*
+ * q, o  bf16 token matrices [B,Hq,N,D] (or of Hq*D columns where B is 1), Hq a multiple of the cache's H: query head h reads head h / (Hq / H)
+ * lse   device fp32 [B,Hq,N]: natural log of the sum of exponentials of the scaled scores, or NULL
+ * Rows of o and lse from q_len[b] on are left as they were.  Scores are fp32 sums of exact products, the weights are rounded to bf16 for the
+ * second product, sums are fp32.  Results repeat bit for bit.
+ * workspace: >= svg_kv4_attn_workspace_bytes(cache, attn, q_desc) bytes, 16-byte aligned (0: may be NULL).
+ * Overlaps of o, lse or the workspace with each other or an input: SVG_ERR_ALIAS.
+ */
+size_t svg_kv4_attn_workspace_bytes(const svg_kv4_t* cache, const svg_kv4_attn_t* attn, const svg_tokens_t* q_desc);
+int svg_kv4_attn_fwd(const svg_kv4_t* cache, const svg_kv4_attn_t* attn, const svg_tokens_t* q_desc, const void* q,
+                     const svg_tokens_t* o_desc, void* o, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

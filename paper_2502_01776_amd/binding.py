@@ -28,6 +28,7 @@ SVG_ATTN_KV_TOKEN_ORDER = 4          # svg_sparse_attn_fwd_ex: k, v of temporal 
 SVG_BF16, SVG_F16, SVG_F32 = 0, 1, 2                            # element types of the operators around the attention
 SVG_FP4_CODES, SVG_FP4_SCALES = 0, 1                            # svg_fp4_buffer_bytes
 SVG_ACT_NONE, SVG_ACT_SILU, SVG_ACT_GELU_TANH = 0, 1, 2
+SVG_KV4_OK, SVG_KV4_FULL, SVG_KV4_LENGTHS = 0, 1, 2              # status of svg_kv4_resize
 SVG_OK = 0
 
 EXPORTS = ("svg_strerror", "svg_version", "svg_last_hip_error", "svg_workspace_bytes", "svg_profile_plan", "svg_tile_counts",
@@ -38,7 +39,8 @@ EXPORTS = ("svg_strerror", "svg_version", "svg_last_hip_error", "svg_workspace_b
            "svg_probe_mfma_bf16", "svg_probe_lds",
            "svg_gate_norm_fwd", "svg_gate_norm_workspace_bytes", "svg_gate_norm_bwd",
            "svg_fp4_buffer_bytes", "svg_fp4_quantize", "svg_fp4_dequantize",
-           "svg_fp4_linear_workspace_bytes", "svg_fp4_linear", "svg_fp4_linear_quantize")
+           "svg_fp4_linear_workspace_bytes", "svg_fp4_linear", "svg_fp4_linear_quantize", "svg_fp4_linear_rows",
+           "svg_kv4_bytes", "svg_kv4_resize", "svg_kv4_write", "svg_kv4_read", "svg_kv4_attn_workspace_bytes", "svg_kv4_attn_fwd")
 
 
 class SvgShape(C.Structure):
@@ -69,6 +71,16 @@ class SvgGateNormGrads(C.Structure):
 class SvgTokens(C.Structure):
     _fields_ = [("B", C.c_int64), ("N", C.c_int64), ("H", C.c_int32), ("D", C.c_int32), ("stride_b", C.c_int64),
                 ("stride_n", C.c_int64), ("stride_h", C.c_int64), ("type", C.c_int32), ("reserved", C.c_int32)]
+
+
+class SvgKv4(C.Structure):
+    _fields_ = [("B", C.c_int32), ("H", C.c_int32), ("D", C.c_int32), ("page_size", C.c_int32), ("pages", C.c_int32),
+                ("max_pages", C.c_int32), ("reserved", C.c_int64), ("data", C.c_void_p), ("page_table", C.c_void_p)]
+
+
+class SvgKv4Attn(C.Structure):
+    _fields_ = [("softmax_scale", C.c_float), ("causal", C.c_int32), ("block", C.c_int32), ("window", C.c_int32), ("sink", C.c_int32),
+                ("max_kv", C.c_int32), ("kv_len", C.c_void_p), ("q_len", C.c_void_p)]
 
 
 class SvgError(RuntimeError):
@@ -155,6 +167,21 @@ def lib():
         L.svg_fp4_linear.argtypes = [i64, i64, i64, vp, vp, vp, vp, vp, C.c_int, tp, vp, vp, C.c_size_t, vp]
         L.svg_fp4_linear_quantize.restype = C.c_int
         L.svg_fp4_linear_quantize.argtypes = [i64, i64, i64, vp, vp, vp, vp, vp, C.c_int, vp, vp, vp, C.c_size_t, vp]
+        L.svg_fp4_linear_rows.restype = C.c_int
+        L.svg_fp4_linear_rows.argtypes = [tp, vp, C.c_int, i64, vp, vp, vp, C.c_int, tp, vp, vp]
+        kp, ap = C.POINTER(SvgKv4), C.POINTER(SvgKv4Attn)
+        L.svg_kv4_bytes.restype = C.c_size_t
+        L.svg_kv4_bytes.argtypes = [kp]
+        L.svg_kv4_resize.restype = C.c_int
+        L.svg_kv4_resize.argtypes = [kp, vp, vp, vp, vp, vp, vp, vp, C.c_int32, vp, vp]
+        L.svg_kv4_write.restype = C.c_int
+        L.svg_kv4_write.argtypes = [kp, tp, vp, tp, vp, vp, vp]
+        L.svg_kv4_read.restype = C.c_int
+        L.svg_kv4_read.argtypes = [kp, vp, tp, vp, tp, vp, vp]
+        L.svg_kv4_attn_workspace_bytes.restype = C.c_size_t
+        L.svg_kv4_attn_workspace_bytes.argtypes = [kp, ap, tp]
+        L.svg_kv4_attn_fwd.restype = C.c_int
+        L.svg_kv4_attn_fwd.argtypes = [kp, ap, tp, vp, tp, vp, vp, vp, C.c_size_t, vp]
         _lib = L
     return _lib
 
@@ -417,3 +444,61 @@ def svg_fp4_linear_quantize(M, N, K, a, a_scales, w, w_scales, bias, activation,
     _check(lib().svg_fp4_linear_quantize(M, N, K, _ptr(a), _ptr(a_scales), _ptr(w), _ptr(w_scales), _ptr(bias), int(activation),
                                          _ptr(codes), _ptr(scales), _ptr(workspace), int(workspace_bytes), _stream(stream)),
            "svg_fp4_linear_quantize")
+
+
+def svg_fp4_linear_rows(x_tokens, x, in_activation, N, w, w_scales, bias, activation, out_tokens, out, stream=None):
+    _check(lib().svg_fp4_linear_rows(C.byref(x_tokens), _ptr(x), int(in_activation), int(N), _ptr(w), _ptr(w_scales), _ptr(bias),
+                                     int(activation), C.byref(out_tokens), _ptr(out), _stream(stream)), "svg_fp4_linear_rows")
+
+
+# ---- a cache of keys and values in 4 bits ---------------------------------------------------------
+
+def _whole(x, kind, name):
+    """Address of a tensor of whole numbers, which the device reads as they lie."""
+    if isinstance(x, torch.Tensor) and (x.dtype != kind or not x.is_contiguous()):
+        raise ValueError(f"{name} has to be a contiguous tensor of {kind}")
+    return _ptr(x)
+
+
+def kv4_cache(sequences, pages, max_pages, heads, head_dim, page_size, data=None, page_table=None) -> SvgKv4:
+    """The descriptor of a cache: `pages` pages of `page_size` tokens, `max_pages` entries in a row of the page table.  The caller keeps
+    data (uint8, svg_kv4_bytes) and page_table (int32 [sequences, max_pages]) alive."""
+    return SvgKv4(sequences, heads, head_dim, page_size, pages, max_pages, 0, _ptr(data), _whole(page_table, torch.int32, "page_table"))
+
+
+def kv4_attn(kv_len, q_len=None, max_kv=0, causal=False, block=1, window=-1, sink=0, softmax_scale=0.0) -> SvgKv4Attn:
+    """The descriptor of svg_kv4_attn_fwd; lengths as int32 tensors [sequences], which the caller keeps alive."""
+    return SvgKv4Attn(softmax_scale, int(causal), block, window, sink, max_kv, _whole(kv_len, torch.int32, "kv_len"),
+                      _whole(q_len, torch.int32, "q_len"))
+
+
+def svg_kv4_bytes(cache) -> int:
+    return int(lib().svg_kv4_bytes(C.byref(cache)))
+
+
+def svg_kv4_resize(cache, lengths, wanted, free_pages, free_count, new_lengths, new_count, slots, tokens, status, stream=None):
+    i32 = torch.int32
+    _check(lib().svg_kv4_resize(C.byref(cache), _whole(lengths, i32, "lengths"), _whole(wanted, i32, "wanted"),
+                                _whole(free_pages, i32, "free_pages"), _whole(free_count, i32, "free_count"),
+                                _whole(new_lengths, i32, "new_lengths"), _whole(new_count, i32, "new_count"),
+                                _whole(slots, torch.int64, "slots"), int(tokens), _whole(status, i32, "status"), _stream(stream)),
+           "svg_kv4_resize")
+
+
+def svg_kv4_write(cache, k_tokens, k, v_tokens, v, slots, stream=None):
+    _check(lib().svg_kv4_write(C.byref(cache), C.byref(k_tokens), _ptr(k), C.byref(v_tokens), _ptr(v),
+                               _whole(slots, torch.int64, "slots"), _stream(stream)), "svg_kv4_write")
+
+
+def svg_kv4_read(cache, slots, k_tokens, k, v_tokens, v, stream=None):
+    _check(lib().svg_kv4_read(C.byref(cache), _whole(slots, torch.int64, "slots"), C.byref(k_tokens), _ptr(k), C.byref(v_tokens), _ptr(v),
+                              _stream(stream)), "svg_kv4_read")
+
+
+def svg_kv4_attn_workspace_bytes(cache, attn, q_tokens) -> int:
+    return int(lib().svg_kv4_attn_workspace_bytes(C.byref(cache), C.byref(attn), C.byref(q_tokens)))
+
+
+def svg_kv4_attn_fwd(cache, attn, q_tokens, q, o_tokens, o, lse=None, workspace=None, workspace_bytes=0, stream=None):
+    _check(lib().svg_kv4_attn_fwd(C.byref(cache), C.byref(attn), C.byref(q_tokens), _ptr(q), C.byref(o_tokens), _ptr(o), _ptr(lse),
+                                  _ptr(workspace), int(workspace_bytes), _stream(stream)), "svg_kv4_attn_fwd")

@@ -10,7 +10,8 @@ ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libsvg_gfx950.so")
 SOURCES = ["svg_host.cpp", "svg_api.cpp", "svg_layout.hip", "svg_attn.hip", "svg_split.hip", "svg_teams.hip", "svg_fp8.hip", "svg_qkrope.hip", "svg_static.hip", "svg_probe.hip",
-           "svg_block_api.cpp", "svg_gate_norm.hip", "svg_fp4.hip", "svg_fp4_linear.hip"]
+           "svg_block_api.cpp", "svg_gate_norm.hip", "svg_fp4.hip", "svg_fp4_linear.hip",
+           "svg_kv4_api.cpp", "svg_kv4.hip", "svg_kv4_attn.hip", "svg_fp4_rows.hip"]
 
 
 def hipcc_path() -> str:

@@ -1,0 +1,721 @@
+// Attention of new queries over a cache of keys and values in 4 bits (svg_kv4_attn_fwd).
+//
+// With c = scale log2 e, one pass over the visible keys j in tiles of 64, in fp32:
+//     p_ij = 2^(c q_i k_j - m_i),  l_i = sum_j p_ij,  o_i = sum_j p_ij v_j / l_i
+// against a reference m_i that follows the largest score where it has to: when a lane's sum of a tile passes 2^13, the tile is taken again
+// against its own maximum and what was summed is rescaled.  Both products are computed transposed on v_mfma_f32_16x16x32_bf16,
+//     S^T = K Q^T      O^T += V^T P^T
+// as in svg_attn_kernel.h: a lane has one query and four neighbouring keys of every 16, so that sums over keys stay in its registers and the
+// weights are the second product's operand as they are.  The weights are rounded to bf16 for it; sums take them unrounded.
+//
+// Every 4-bit value under its power of two is a bf16 number, so keys and values are dequantised exactly (two a v_cvt_scalef32_pk_bf16_fp4) and the
+// scores are exact products summed in fp32.  (The matrix instruction that takes 4-bit keys as they are, with a query as two 8-bit parts, costs the
+// same and cuts what is 2^-14 below the largest of 128 products: scores off by 4e-6 of their size.)
+//
+// Two forms:
+//  * 16 or 32 query rows: the wavefronts of a workgroup share them and split the keys, every one with its own tiles, straight
+//    from memory into registers one tile ahead; no barrier before the results are merged through LDS.  Bound: HBM.
+//  * 128 rows, 32 a wavefront: a tile of keys and values is dequantised once for all, a quarter by each wavefront, into LDS.  Bound: MFMA.
+// Few workgroups for the chip: the keys are cut into parts for several, whose results a second launch joins.
+#include <algorithm>
+
+#include "svg_attn_common.h"
+#include "svg_kv4.h"
+
+namespace svg {
+
+namespace {
+
+using namespace attn;
+
+constexpr int kTile = 64;              // keys of a tile
+constexpr int kWaves = 4;
+constexpr int kGroups = kTile / 16;    // 16-key groups of a tile: pages begin and end between them
+
+struct Kv4AttnArgs {
+  Kv4 c;
+  HeadRows q, o;
+  const __bf16* qp;
+  __bf16* op;
+  float* lse;
+  const int32_t *kv_len, *q_len;
+  float* part;               // [splits][head of a sequence][row][D], and behind them (reference, sum) [splits][head of a sequence][row]
+  float2* stats;
+  int N, group, rows, tiles, splits;
+  unsigned total;
+  int causal, block, window, sink, capacity;
+  float scale_log2;
+};
+
+// A sequence, and the keys that its query rows see.
+struct Sequence {
+  int kv, qn;
+  __device__ __forceinline__ Sequence(const Kv4AttnArgs& a, int b) {
+    kv = min(max(__builtin_amdgcn_readfirstlane(a.kv_len[b]), 0), a.capacity);
+    qn = a.q_len ? min(max(__builtin_amdgcn_readfirstlane(a.q_len[b]), 0), a.N) : a.N;
+  }
+};
+// Keys [begin, end), and of those in front of begin the first `sink`.
+struct Visible {
+  int begin, end;
+};
+__device__ __forceinline__ Visible visible(const Kv4AttnArgs& a, const Sequence& s, int n) {
+  const int p = s.kv - s.qn + n;                         // may be negative: a query without a token of its own
+  if (!a.causal && a.window < 0) return {0, s.kv};
+  const int f = p >= 0 ? p / a.block : -1 - (-1 - p) / a.block;
+  Visible v = {0, s.kv};
+  if (a.causal) v.end = (int)max(0ll, min((long long)s.kv, (f + 1ll) * a.block));
+  if (a.window >= 0) v.begin = (int)min((long long)s.kv, max(0ll, ((long long)f - a.window) * a.block));
+  return v;
+}
+__device__ __forceinline__ bool sees(const Visible& v, int sink, int key) { return key < v.end && (key >= v.begin || key < sink); }
+
+// The tiles of a range of rows, whose windows ascend: those of the sink, then those from the first row's begin to the last row's end.
+struct Tiles {
+  int sink_tiles, first, count;
+  __device__ __forceinline__ Tiles(const Visible& lo, const Visible& hi, int sink) {
+    sink_tiles = min(sink, hi.end) > 0 ? (min(sink, hi.end) + kTile - 1) / kTile : 0;
+    first = max(lo.begin / kTile, sink_tiles);
+    count = sink_tiles + max(0, (hi.end + kTile - 1) / kTile - first);
+  }
+  __device__ __forceinline__ int at(int t) const { return t < sink_tiles ? t : t - sink_tiles + first; }
+};
+
+// A page that is there, or -1.
+__device__ __forceinline__ int page_of(const Kv4AttnArgs& a, const int32_t* row, int key) {
+  const int entry = key >> a.c.page_log2;
+  const int page = entry < a.c.max_pages ? __builtin_amdgcn_readfirstlane(row[entry]) : -1;
+  return (unsigned)page < (unsigned)a.c.pages ? page : -1;
+}
+
+__device__ __forceinline__ float power_of(unsigned scale) { return __uint_as_float(scale << 23); }
+// A block of values that are not finite: zeros in the product, NaN put into the results of the queries that see it afterwards, since a
+// weight of zero does not take it away.
+__device__ __forceinline__ bool not_finite(unsigned scale) { return scale >= 253; }
+
+// Eight values of a word of codes.
+__device__ __forceinline__ bf16x8 dequantise8(unsigned code, float scale) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 1),
+               c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 3);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// Values in LDS: rows of D bf16, 32-byte slots swizzled with the row for the transposing read (svg_attn_kernel.h).
+template <int D>
+__device__ __forceinline__ int value_slot(int row, int slot) {
+  return row * (2 * D) + ((slot ^ (D == 128 ? row & 7 : (row >> 1) & 3)) << 5);
+}
+// Keys in LDS: 16-byte pieces swizzled with the row, so that one piece of 16 rows lies on different banks.
+template <int D>
+__device__ __forceinline__ int key_piece(int row, int piece) {
+  return row * (2 * D) + ((piece ^ (D == 128 ? row & 15 : (row >> 1) & 7)) << 4);
+}
+
+// Online softmax of a wavefront's tile.  s: scores; on return p is the second product's operand.
+template <int QB, int CB>
+__device__ __forceinline__ void take_tile(f32x4 (&s)[kGroups][QB], bf16x8 (&p)[kGroups / 2][QB], float (&m)[QB], float (&l)[QB],
+                                          f32x4 (&o)[CB][QB], const float c) {
+  float sum[QB];
+  auto exponentials = [&]() {
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      sum[qb] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < kGroups / 2; ++ks) {
+        f32x8 e;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * ks + j / 4][qb][j % 4], c, -m[qb]));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[qb] += e[j];
+        p[ks][qb] = __builtin_convertvector(e, bf16x8);
+      }
+    }
+  };
+  exponentials();
+  bool over = false;
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) over |= sum[qb] > kLazySum;
+  if (__builtin_amdgcn_ballot_w64(over)) {
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      float top = s[0][qb][0];
+#pragma unroll
+      for (int kb = 0; kb < kGroups; ++kb)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) top = fmaxf(top, s[kb][qb][j]);
+      const float reference = fmaxf(m[qb], quarters_max(top) * c);
+      const float f = __builtin_amdgcn_exp2f(m[qb] - reference);
+      m[qb] = reference;
+      l[qb] *= f;
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) o[cb][qb] *= f;
+    }
+    exponentials();
+  }
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) l[qb] += sum[qb];
+}
+
+template <int QB>
+__device__ __forceinline__ void mask_tile(f32x4 (&s)[kGroups][QB], const Visible (&v)[QB], int sink, int key0, unsigned missing, int g) {
+#pragma unroll
+  for (int kb = 0; kb < kGroups; ++kb)
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        s[kb][qb][j] = !(missing >> kb & 1) && sees(v[qb], sink, key0 + 16 * kb + 4 * g + j) ? s[kb][qb][j] : -INFINITY;
+}
+
+// NaN into the channels [32 block, + 32) of the queries that see this key.
+template <int QB, int CB>
+__device__ __forceinline__ void poison(f32x4 (&o)[CB][QB], const Visible (&v)[QB], int sink, int key, int block) {
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const bool hit = sees(v[qb], sink, key);
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+      if (cb >> 1 == block && hit) o[cb][qb] = f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
+  }
+}
+
+// This lane's query rows, one in each 16-query block, as the operand of the first product.  WIDE: the order of channels in which a lane's
+// D / 4 neighbouring channels are its parts of the D / 32 products.
+template <int D, int QB, bool WIDE>
+struct Queries {
+  int n[QB], head[QB];
+  bool there[QB];
+  Visible seen[QB];
+  bf16x8 q[QB][D / 32];
+  __device__ __forceinline__ void load(const Kv4AttnArgs& a, const Sequence& s, int b, int kvh, int m0) {
+    const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      const int m = m0 + 16 * qb + r;
+      n[qb] = a.group == 1 ? m : m / a.group;
+      head[qb] = kvh * a.group + (a.group == 1 ? 0 : m - n[qb] * a.group);
+      there[qb] = n[qb] < s.qn;
+      // a row that does not exist sees nothing and has any query
+      seen[qb] = there[qb] ? visible(a, s, n[qb]) : Visible{0, 0};
+      const size_t at = (size_t)b * a.q.sb + (size_t)(there[qb] ? n[qb] : 0) * a.q.sn + (size_t)head[qb] * a.q.sh;
+#pragma unroll
+      for (int st = 0; st < D / 32; ++st)
+        q[qb][st] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const block_u32x4_of2*>(a.qp + at + (WIDE ? g * (D / 4) + st * 8 : st * 32 + g * 8)));
+    }
+  }
+};
+
+typedef unsigned u32x2_of2 __attribute__((ext_vector_type(2), aligned(2)));
+
+// ---- few rows ------------------------------------------------------------------------------------------------------
+
+// A wavefront's tile in registers, as it comes from memory.
+template <int D>
+struct RawTile {
+  static constexpr int kKeyWords = D / 32;               // words of codes a lane has of a key
+  static constexpr int kValueLoads = D / 32;             // 16 bytes each
+  unsigned k[kGroups][kKeyWords];
+  block_u32x4 v[kValueLoads];
+  unsigned char ks[kGroups], vs[kValueLoads];
+  unsigned missing;
+
+  __device__ __forceinline__ void load(const Kv4AttnArgs& a, const int32_t* table_row, int kvh, int key0) {
+    const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+    const long long record = a.c.record();
+    const int mask = (1 << a.c.page_log2) - 1;
+    const unsigned char* group[kGroups];
+    int place[kGroups];
+    missing = 0;
+#pragma unroll
+    for (int kb = 0; kb < kGroups; ++kb) {
+      const int page = page_of(a, table_row, key0 + 16 * kb);
+      missing |= page < 0 ? 1u << kb : 0u;
+      group[kb] = a.c.data + ((size_t)max(page, 0) * a.c.H + kvh) * record;
+      place[kb] = (key0 + 16 * kb) & mask;
+    }
+#pragma unroll
+    for (int kb = 0; kb < kGroups; ++kb) {
+      const int row = place[kb] + r;
+      const unsigned char* const p = group[kb] + row * (D / 2) + g * (D / 8);
+      if constexpr (D == 128) {
+        const block_u32x4 x = *reinterpret_cast<const block_u32x4*>(p);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) k[kb][e] = x[e];
+      } else {
+        const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+        k[kb][0] = x[0];
+        k[kb][1] = x[1];
+      }
+      ks[kb] = group[kb][a.c.key_scales() + row * (D / 32) + (D == 128 ? g : g >> 1)];
+    }
+#pragma unroll
+    for (int i = 0; i < kValueLoads; ++i) {
+      // D = 128: 16 keys a load, four lanes each; D = 64: 32 keys, two lanes each
+      const unsigned char* from;
+      int row, block;
+      if constexpr (D == 128) {
+        from = group[i];
+        row = place[i] + (lane >> 2);
+        block = lane & 3;
+      } else {
+        from = lane < 32 ? group[2 * i] : group[2 * i + 1];
+        row = (lane < 32 ? place[2 * i] : place[2 * i + 1]) + ((lane >> 1) & 15);
+        block = lane & 1;
+      }
+      v[i] = *reinterpret_cast<const block_u32x4*>(from + a.c.values() + row * (D / 2) + block * 16);
+      vs[i] = from[a.c.value_scales() + row * (D / 32) + block];
+    }
+  }
+};
+
+template <int D, int QB>
+__global__ __launch_bounds__(64 * kWaves, 2) void kv4_rows_kernel(Kv4AttnArgs a) {
+  constexpr int DS = D / 32, CB = D / 16, BM = 16 * QB;
+  constexpr int STAGE = 32 * 2 * D;                      // half a tile of values
+  constexpr int MERGE = BM * D * 4;                      // a wavefront's results
+  constexpr int OWN = STAGE > MERGE ? STAGE : MERGE;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[kWaves * OWN];
+  __shared__ float2 merged[kWaves][BM];
+  const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // splits innermost
+  unsigned id = blockIdx.x;
+  const int split = id % a.splits;
+  id /= a.splits;
+  const int tile_m = id % a.tiles;
+  const unsigned bh = id / a.tiles;
+  const int b = bh / a.c.H, kvh = bh - b * a.c.H;
+  const int m0 = tile_m * BM;
+  const Sequence s(a, b);
+  const int n0 = m0 / a.group;
+  if (n0 >= s.qn) return;
+  const int n1 = min((m0 + BM - 1) / a.group, s.qn - 1);
+  const int sink = a.window >= 0 ? a.sink : 0;
+  const Visible lo = visible(a, s, n0), hi = visible(a, s, n1);
+  const Tiles tiles(lo, hi, sink);
+  const int t0 = (int)((long long)tiles.count * split / a.splits), t1 = (int)((long long)tiles.count * (split + 1) / a.splits);
+  const int32_t* const table_row = a.c.table + (size_t)b * a.c.max_pages;
+
+  Queries<D, QB, true> rows;
+  rows.load(a, s, b, kvh, m0);
+  f32x4 o[CB][QB] = {};
+  float m[QB], l[QB];
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    m[qb] = kNegBig;
+    l[qb] = 0.f;
+  }
+  unsigned char* const own = lds + wave * OWN;
+  int v_off[CB];
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb) v_off[cb] = value_slot<D>(4 * g + (r >> 2), cb) + ((r & 3) << 3);
+
+  RawTile<D> next;
+  int t = t0 + wave;
+  if (t < t1) next.load(a, table_row, kvh, tiles.at(t) * kTile);
+  for (; t < t1; t += kWaves) {
+    const int key0 = tiles.at(t) * kTile;
+    RawTile<D> now = next;
+    if (t + kWaves < t1) next.load(a, table_row, kvh, tiles.at(t + kWaves) * kTile);
+    f32x4 sc[kGroups][QB];
+#pragma unroll
+    for (int kb = 0; kb < kGroups; ++kb) {
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) sc[kb][qb] = f32x4{0.f, 0.f, 0.f, 0.f};
+      const float scale = power_of(now.ks[kb]);
+#pragma unroll
+      for (int st = 0; st < DS; ++st) {
+        const bf16x8 k = dequantise8(now.k[kb][st], scale);
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) sc[kb][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, rows.q[qb][st], sc[kb][qb], 0, 0, 0);
+      }
+    }
+    const bool whole = key0 + kTile <= lo.end && (key0 >= hi.begin || key0 + kTile <= sink) && !now.missing && n0 + (BM - 1) / a.group < s.qn;
+    if (!whole) mask_tile<QB>(sc, rows.seen, sink, key0, now.missing, g);
+    bf16x8 p[kGroups / 2][QB];
+    take_tile<QB, CB>(sc, p, m, l, o, a.scale_log2);
+    bool odd = false;
+#pragma unroll
+    for (int ks = 0; ks < kGroups / 2; ++ks) {
+      constexpr int LOADS = RawTile<D>::kValueLoads / 2;
+#pragma unroll
+      for (int x = 0; x < LOADS; ++x) {
+        const int i = ks * LOADS + x;
+        const int row = D == 128 ? 16 * x + (lane >> 2) : lane >> 1, block = D == 128 ? lane & 3 : lane & 1;
+        const int key = key0 + 32 * ks + row;
+        const bool gone = key >= hi.end || (now.missing >> (2 * ks + (row >> 4)) & 1) != 0;
+        const bool bad = !gone && not_finite(now.vs[i]);
+        odd |= bad;
+        const float scale = power_of(now.vs[i]);
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+          *reinterpret_cast<bf16x8*>(own + value_slot<D>(row, 2 * block + (w >> 1)) + (w & 1) * 16) =
+              dequantise8(gone || bad ? 0u : now.v[i][w], gone || bad ? 1.f : scale);
+      }
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) {
+        const unsigned char* const src = own + v_off[cb];
+        const i16x4 first = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)src);
+        const i16x4 second = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(src + 16 * 2 * D));
+        const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(first, second, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) o[cb][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[ks][qb], o[cb][qb], 0, 0, 0);
+      }
+    }
+    if (__builtin_amdgcn_ballot_w64(odd)) {
+      for (int i = 0; i < RawTile<D>::kValueLoads; ++i) {
+        const int row = D == 128 ? 16 * i + (lane >> 2) : 32 * i + (lane >> 1);
+        unsigned char scale = 0;
+#pragma unroll
+        for (int x = 0; x < RawTile<D>::kValueLoads; ++x) scale = x == i ? now.vs[x] : scale;
+        const bool bad = key0 + row < hi.end && !(now.missing >> (row >> 4) & 1) && not_finite(scale);
+        unsigned long long hits = __builtin_amdgcn_ballot_w64(bad);
+        while (hits) {
+          const int at = __builtin_ctzll(hits);
+          hits &= hits - 1;
+          poison<QB, CB>(o, rows.seen, sink, key0 + (D == 128 ? 16 * i + (at >> 2) : 32 * i + (at >> 1)), D == 128 ? at & 3 : at & 1);
+        }
+      }
+    }
+  }
+
+  // ---- the wavefronts' results joined
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) l[qb] = quarters_sum(l[qb]);
+  if (g == 0)
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) merged[wave][16 * qb + r] = float2{m[qb], l[qb]};
+  __syncthreads();
+  float* const sums = reinterpret_cast<float*>(lds);
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    float top = m[qb];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, merged[w][16 * qb + r].x);
+    const float f = __builtin_amdgcn_exp2f(m[qb] - top);
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+      *reinterpret_cast<f32x4*>(sums + (wave * BM + 16 * qb + r) * D + ((4 * cb + g) ^ r) * 4) = o[cb][qb] * f;
+  }
+  __syncthreads();
+  constexpr int PIECES = D / 4;
+  const size_t first_row = (size_t)bh * a.rows + m0;
+  for (int u = threadIdx.x; u < BM * PIECES; u += 64 * kWaves) {
+    const int row = u / PIECES, piece = u % PIECES;
+    const int mm = m0 + row, n = mm / a.group;
+    if (n >= s.qn) continue;
+    float top = kNegBig, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, merged[w][row].x);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) sum += merged[w][row].y * __builtin_amdgcn_exp2f(merged[w][row].x - top);
+    f32x4 x = {};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) x += *reinterpret_cast<const f32x4*>(sums + (w * BM + row) * D + (piece ^ (row & 15)) * 4);
+    if (a.splits > 1) {
+      const size_t at = (size_t)split * a.total + first_row + row;
+      *reinterpret_cast<f32x4*>(a.part + at * D + piece * 4) = x;
+      if (piece == 0) a.stats[at] = float2{top, sum};
+      continue;
+    }
+    const int head = kvh * a.group + (mm - n * a.group);
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const bf16x4 y = __builtin_convertvector(x * inv, bf16x4);
+    *reinterpret_cast<u32x2_of2*>(a.op + (size_t)b * a.o.sb + (size_t)n * a.o.sn + (size_t)head * a.o.sh + piece * 4) = __builtin_bit_cast(u32x2, y);
+    if (piece == 0 && a.lse)
+      a.lse[((size_t)b * a.c.H * a.group + head) * a.N + n] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+  }
+}
+
+// ---- many rows -----------------------------------------------------------------------------------------------------
+
+template <int D>
+__global__ __launch_bounds__(64 * kWaves, 2) void kv4_tiles_kernel(Kv4AttnArgs a) {
+  constexpr int QB = 2, DS = D / 32, CB = D / 16, BM = 32 * kWaves;
+  constexpr int WORDS = D / 32;                          // words of codes that a thread stages of a tile's keys, and of its values
+  constexpr int HALF = kTile * 2 * D;                    // a tile of keys, or of values
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * HALF];
+  __shared__ unsigned long long odd_values[2][kWaves];   // threads of a wavefront whose values are not finite
+  __shared__ unsigned missing_pages[2][kWaves];
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, r = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // neighbouring row tiles of a head on one XCD, whose L2 they share
+  const unsigned all = a.total / (unsigned)a.rows * (unsigned)a.tiles * (unsigned)a.splits;
+  const unsigned per_xcd = (all + 7) / 8;
+  unsigned id = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+  if ((blockIdx.x >> 3) >= per_xcd || id >= all) return;
+  const int tile_m = id % a.tiles;
+  id /= a.tiles;
+  const int split = id % a.splits;
+  const unsigned bh = id / a.splits;
+  const int b = bh / a.c.H, kvh = bh - b * a.c.H;
+  const int m0 = tile_m * BM;
+  const Sequence s(a, b);
+  const int n0 = m0 / a.group;
+  if (n0 >= s.qn) return;
+  const int n1 = min((m0 + BM - 1) / a.group, s.qn - 1);
+  const int sink = a.window >= 0 ? a.sink : 0;
+  const Visible lo = visible(a, s, n0), hi = visible(a, s, n1);
+  const Tiles tiles(lo, hi, sink);
+  const int t0 = (int)((long long)tiles.count * split / a.splits), t1 = (int)((long long)tiles.count * (split + 1) / a.splits);
+  const int32_t* const table_row = a.c.table + (size_t)b * a.c.max_pages;
+  // this wavefront's rows; one without any stages its share and computes nothing
+  const int wm0 = m0 + 32 * wave, wn0 = wm0 / a.group, wn1 = min((wm0 + 31) / a.group, s.qn - 1);
+  const bool active = wn0 < s.qn, full_rows = (wm0 + 31) / a.group < s.qn;
+  const Visible wlo = visible(a, s, min(wn0, s.qn - 1)), whi = visible(a, s, wn1);
+
+  Queries<D, QB, false> rows;
+  rows.load(a, s, b, kvh, wm0);
+  f32x4 o[CB][QB] = {};
+  float m[QB], l[QB];
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    m[qb] = kNegBig;
+    l[qb] = 0.f;
+  }
+
+  // ---- staging: a wavefront has 16 keys of a tile, which are in one page; four threads a key
+  unsigned kw[WORDS], vw[WORDS];
+  unsigned char ks, vs;
+  int staged_key;
+  bool missing;
+  const int sub = tid & 3, stage_row = tid >> 2;
+  auto load = [&](int t) {
+    const int key0 = tiles.at(t) * kTile + 16 * wave;
+    const int page = page_of(a, table_row, key0);
+    missing = page < 0;
+    staged_key = key0 + (lane >> 2);
+    const unsigned char* const record = a.c.data + ((size_t)max(page, 0) * a.c.H + kvh) * a.c.record();
+    const int place = (key0 & ((1 << a.c.page_log2) - 1)) + (lane >> 2);
+    const unsigned char* const p = record + place * (D / 2) + sub * (D / 8);
+    const int scale = place * (D / 32) + (D == 128 ? sub : sub >> 1);
+    if constexpr (D == 128) {
+      const block_u32x4 x = *reinterpret_cast<const block_u32x4*>(p), y = *reinterpret_cast<const block_u32x4*>(p + a.c.values());
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        kw[e] = x[e];
+        vw[e] = y[e];
+      }
+    } else {
+      const u32x2 x = *reinterpret_cast<const u32x2*>(p), y = *reinterpret_cast<const u32x2*>(p + a.c.values());
+      kw[0] = x[0];
+      kw[1] = x[1];
+      vw[0] = y[0];
+      vw[1] = y[1];
+    }
+    ks = record[a.c.key_scales() + scale];
+    vs = record[a.c.value_scales() + scale];
+  };
+  auto stage = [&](int buffer) {
+    unsigned char* const keys = lds + buffer * 2 * HALF;
+    unsigned char* const values = keys + HALF;
+    // keys that nobody sees may be anything: a value that is not finite would not be taken away by its weight of zero
+    const bool gone = missing || staged_key >= hi.end;
+    const bool odd = !gone && not_finite(vs);
+    const float k_scale = gone ? 1.f : power_of(ks), v_scale = gone || odd ? 1.f : power_of(vs);
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) {
+      *reinterpret_cast<bf16x8*>(keys + key_piece<D>(stage_row, WORDS * sub + w)) = dequantise8(gone ? 0u : kw[w], k_scale);
+      const int piece = WORDS * sub + w;
+      *reinterpret_cast<bf16x8*>(values + value_slot<D>(stage_row, piece >> 1) + (piece & 1) * 16) = dequantise8(gone || odd ? 0u : vw[w], v_scale);
+    }
+    const unsigned long long hits = __builtin_amdgcn_ballot_w64(odd);
+    if (lane == 0) {
+      odd_values[buffer][wave] = hits;
+      missing_pages[buffer][wave] = missing;
+    }
+  };
+
+  int k_off[DS], v_off[CB];
+#pragma unroll
+  for (int st = 0; st < DS; ++st) k_off[st] = key_piece<D>(r, 4 * st + g);       // (16 rows on, the swizzle is the same)
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb) v_off[cb] = value_slot<D>(4 * g + (r >> 2), cb) + ((r & 3) << 3);
+
+  if (t0 < t1) {
+    load(t0);
+    stage(0);
+    if (t0 + 1 < t1) load(t0 + 1);
+  }
+  __syncthreads();
+  for (int t = t0; t < t1; ++t) {
+    const int buffer = (t - t0) & 1, key0 = tiles.at(t) * kTile;
+    if (t + 1 < t1) {
+      stage(buffer ^ 1);
+      if (t + 2 < t1) load(t + 2);
+    }
+    const unsigned char* const keys = lds + buffer * 2 * HALF;
+    const unsigned char* const values = keys + HALF;
+    const unsigned gone = (unsigned)__builtin_amdgcn_ballot_w64(missing_pages[buffer][lane & 3] != 0) & 15u;
+    const bool in_reach = active && key0 < whi.end && (key0 + kTile > wlo.begin || key0 < sink);
+    if (in_reach) {
+      f32x4 sc[kGroups][QB];
+#pragma unroll
+      for (int kb = 0; kb < kGroups; ++kb) {
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) sc[kb][qb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int st = 0; st < DS; ++st) {
+          const bf16x8 k = *reinterpret_cast<const bf16x8*>(keys + kb * 16 * 2 * D + k_off[st]);
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb) sc[kb][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, rows.q[qb][st], sc[kb][qb], 0, 0, 0);
+        }
+      }
+      const bool whole = full_rows && key0 + kTile <= wlo.end && (key0 >= whi.begin || key0 + kTile <= sink) && !gone;
+      if (!whole) mask_tile<QB>(sc, rows.seen, sink, key0, gone, g);
+      bf16x8 p[kGroups / 2][QB];
+      take_tile<QB, CB>(sc, p, m, l, o, a.scale_log2);
+#pragma unroll
+      for (int ks2 = 0; ks2 < kGroups / 2; ++ks2)
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+          const unsigned char* const src = values + ks2 * 32 * 2 * D + v_off[cb];
+          const i16x4 first = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)src);
+          const i16x4 second = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(src + 16 * 2 * D));
+          const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(first, second, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb) o[cb][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[ks2][qb], o[cb][qb], 0, 0, 0);
+        }
+      const unsigned long long odd = odd_values[buffer][lane & 3];
+      if (__builtin_amdgcn_ballot_w64(odd != 0)) {
+        for (int w = 0; w < kWaves; ++w) {
+          unsigned long long hits = odd_values[buffer][w];
+          while (hits) {
+            const int at = __builtin_ctzll(hits);
+            hits &= hits - 1;
+            poison<QB, CB>(o, rows.seen, sink, key0 + 16 * w + (at >> 2), D == 128 ? at & 3 : (at & 3) >> 1);
+          }
+        }
+      }
+    }
+    __syncthreads();
+  }
+
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const float sum = quarters_sum(l[qb]);
+    if (!rows.there[qb]) continue;
+    if (a.splits > 1) {
+      const size_t at = (size_t)split * a.total + (size_t)bh * a.rows + wm0 + 16 * qb + r;
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) *reinterpret_cast<f32x4*>(a.part + at * D + 16 * cb + 4 * g) = o[cb][qb];
+      if (g == 0) a.stats[at] = float2{m[qb], sum};
+      continue;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    __bf16* const to = a.op + (size_t)b * a.o.sb + (size_t)rows.n[qb] * a.o.sn + (size_t)rows.head[qb] * a.o.sh;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+      *reinterpret_cast<u32x2_of2*>(to + 16 * cb + 4 * g) = __builtin_bit_cast(u32x2, __builtin_convertvector(o[cb][qb] * inv, bf16x4));
+    if (g == 0 && a.lse)
+      a.lse[((size_t)b * a.c.H * a.group + rows.head[qb]) * a.N + rows.n[qb]] =
+          sum == 0.f ? -INFINITY : (m[qb] + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+  }
+}
+
+// ---- parts of the keys joined -----------------------------------------------------------------------------------------
+
+template <int D>
+__global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a) {
+  constexpr int LANES = D / 4;                           // of a row, four channels each
+  const long long row = (long long)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+  const int piece = threadIdx.x % LANES;
+  if (row >= a.total) return;
+  const unsigned bh = (unsigned)(row / a.rows);
+  const int mm = (int)(row - (long long)bh * a.rows);
+  const int b = bh / a.c.H, kvh = bh - b * a.c.H;
+  const int n = mm / a.group;
+  const int qn = a.q_len ? min(max(a.q_len[b], 0), a.N) : a.N;
+  if (n >= qn) return;
+  float top = kNegBig;
+  for (int x = 0; x < a.splits; ++x) top = fmaxf(top, a.stats[(size_t)x * a.total + row].x);
+  float sum = 0.f;
+  f32x4 o = {};
+  for (int x = 0; x < a.splits; ++x) {
+    const size_t at = (size_t)x * a.total + row;
+    const float2 st = a.stats[at];
+    const float f = __builtin_amdgcn_exp2f(st.x - top);
+    sum += st.y * f;
+    o += *reinterpret_cast<const f32x4*>(a.part + at * D + piece * 4) * f;
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  const int head = kvh * a.group + (mm - n * a.group);
+  *reinterpret_cast<u32x2_of2*>(a.op + (size_t)b * a.o.sb + (size_t)n * a.o.sn + (size_t)head * a.o.sh + piece * 4) =
+      __builtin_bit_cast(u32x2, __builtin_convertvector(o * inv, bf16x4));
+  if (piece == 0 && a.lse)
+    a.lse[((size_t)b * a.c.H * a.group + head) * a.N + n] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+}
+
+}  // namespace
+
+Kv4Plan kv4_plan(const Kv4& c, const svg_kv4_attn_t& attn, long long N, int group) {
+  Kv4Plan p = {};
+  p.rows = (int)(N * group);
+  p.tile = p.rows <= 16 ? 16 : p.rows <= 32 ? 32 : 128;
+  p.tiles = std::max(1, (p.rows + p.tile - 1) / p.tile);
+  p.total = (long long)c.B * c.H * p.rows;
+  // keys that a row tile may have to visit
+  const long long capacity = (long long)c.max_pages << c.page_log2;
+  long long keys = attn.max_kv > 0 ? std::min<long long>(attn.max_kv, capacity) : capacity;
+  if (attn.window >= 0 && attn.causal) {
+    const long long reach = (attn.window + 1ll) * attn.block + (attn.sink < keys ? attn.sink : keys) + p.tile / group;
+    keys = std::min(keys, reach);
+  }
+  const long long units = (keys + kTile - 1) / kTile;
+  const long long whole = (long long)c.B * c.H * p.tiles;
+  const long long wanted = p.tile == 128 ? 512 : 1024, least = p.tile == 128 ? 8 : 2 * kWaves;
+  p.splits = 1;
+  if (whole > 0 && whole < wanted) p.splits = (int)std::max<long long>(1, std::min(std::min((wanted + whole - 1) / whole, units / least), 64ll));
+  return p;
+}
+
+size_t kv4_workspace_bytes(const Kv4& c, const Kv4Plan& p) {
+  return p.splits > 1 ? (size_t)p.splits * (size_t)p.total * ((size_t)c.D * 4 + 8) : 0;
+}
+
+int launch_kv4_attn(const Kv4& c, const svg_kv4_attn_t& attn, const Kv4Plan& plan, const HeadRows& q, const void* qp, const HeadRows& o,
+                    void* op, int group, float* lse, void* workspace, hipStream_t stream) {
+  Kv4AttnArgs a = {};
+  a.c = c;
+  a.q = q;
+  a.o = o;
+  a.qp = static_cast<const __bf16*>(qp);
+  a.op = static_cast<__bf16*>(op);
+  a.lse = lse;
+  a.kv_len = attn.kv_len;
+  a.q_len = attn.q_len;
+  a.N = plan.rows / group;
+  a.group = group;
+  a.rows = plan.rows;
+  a.tiles = plan.tiles;
+  a.splits = plan.splits;
+  if (plan.total > 0x7fffffffll) return SVG_ERR_UNSUPPORTED;
+  a.total = (unsigned)plan.total;
+  a.part = static_cast<float*>(workspace);
+  a.stats = reinterpret_cast<float2*>(static_cast<char*>(workspace) + (size_t)plan.splits * plan.total * c.D * 4);
+  a.causal = attn.causal;
+  a.block = attn.block;
+  a.window = attn.window;
+  a.sink = attn.sink;
+  a.capacity = c.pages ? c.max_pages << c.page_log2 : 0;      // (without a pool there is nothing that a load could be sent to)
+  const float scale = attn.softmax_scale > 0.f ? attn.softmax_scale : 1.f / sqrtf((float)c.D);
+  a.scale_log2 = scale * 1.4426950408889634f;
+  const long long blocks = (long long)c.B * c.H * plan.tiles * plan.splits;
+  if (blocks > (1ll << 24)) return SVG_ERR_UNSUPPORTED;
+  (void)hipGetLastError();
+  const bool wide = c.D == 128;
+  if (plan.tile == 128)
+    hipLaunchKernelGGL((wide ? kv4_tiles_kernel<128> : kv4_tiles_kernel<64>), dim3((unsigned)((blocks + 7) / 8 * 8)), dim3(64 * kWaves), 0, stream, a);
+  else if (plan.tile == 32)
+    hipLaunchKernelGGL((wide ? kv4_rows_kernel<128, 2> : kv4_rows_kernel<64, 2>), dim3((unsigned)blocks), dim3(64 * kWaves), 0, stream, a);
+  else
+    hipLaunchKernelGGL((wide ? kv4_rows_kernel<128, 1> : kv4_rows_kernel<64, 1>), dim3((unsigned)blocks), dim3(64 * kWaves), 0, stream, a);
+  if (plan.splits > 1) {
+    const int per_block = 256 / (c.D / 4);
+    hipLaunchKernelGGL((wide ? kv4_join_kernel<128> : kv4_join_kernel<64>), dim3((unsigned)((plan.total + per_block - 1) / per_block)), dim3(256), 0,
+                       stream, a);
+  }
+  return hip_status(hipGetLastError());
+}
+
+}  // namespace svg
