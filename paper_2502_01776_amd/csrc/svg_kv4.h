@@ -40,8 +40,9 @@ int launch_kv4_read(const Kv4& c, const HeadRows& k, void* kp, const HeadRows& v
 struct Kv4Plan {
   int rows;              // query rows of a head of the cache: N times the query heads that share it
   int tile;              // rows of a workgroup: 16 or 32 (its wavefronts share the rows and split the keys) or 128 (32 rows a wavefront)
-  int tiles, splits;     // workgroups of a head of a sequence: row tiles, parts of the keys
-  long long total;       // workgroups
+  int tiles;             // row tiles of a head of a sequence
+  int parts;             // parts that the keys of all sequences are cut into, one each at least
+  int reach;             // keys that a row tile sees at the most
 };
 Kv4Plan kv4_plan(const Kv4& c, const svg_kv4_attn_t& attn, long long N, int group);
 size_t kv4_workspace_bytes(const Kv4& c, const Kv4Plan& plan);

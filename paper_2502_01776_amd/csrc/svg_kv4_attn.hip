@@ -18,6 +18,8 @@
 //  * 128 rows, 32 a wavefront: a tile of keys and values is dequantised once for all, a quarter by each wavefront, into LDS.  Bound: MFMA.
 // Few workgroups for the chip: the keys are cut into parts for several, whose results a second launch joins.
 #include <algorithm>
+#include <type_traits>
+#include <utility>
 
 #include "svg_attn_common.h"
 #include "svg_kv4.h"
@@ -32,6 +34,14 @@ constexpr int kTile = 64;              // keys of a tile
 constexpr int kWaves = 4;
 constexpr int kGroups = kTile / 16;    // 16-key groups of a tile: pages begin and end between them
 
+// f(0), f(1), .. f(N - 1) with constants.
+template <class F, int... I>
+__device__ __forceinline__ void each_of(F f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void each(F f) { each_of(f, std::make_integer_sequence<int, N>{}); }
+
 struct Kv4AttnArgs {
   Kv4 c;
   HeadRows q, o;
@@ -39,10 +49,11 @@ struct Kv4AttnArgs {
   __bf16* op;
   float* lse;
   const int32_t *kv_len, *q_len;
-  float* part;               // [splits][head of a sequence][row][D], and behind them (reference, sum) [splits][head of a sequence][row]
+  float* part;               // [part][head][row][D], and behind them (reference, sum) [part][head][row]; null: no sequence is cut
   float2* stats;
-  int N, group, rows, tiles, splits;
-  unsigned total;
+  int N, group, rows, tiles;
+  int parts;                 // of all sequences together
+  int reach;                 // keys that a row tile sees at the most
   int causal, block, window, sink, capacity;
   float scale_log2;
 };
@@ -70,6 +81,12 @@ __device__ __forceinline__ Visible visible(const Kv4AttnArgs& a, const Sequence&
 }
 __device__ __forceinline__ bool sees(const Visible& v, int sink, int key) { return key < v.end && (key >= v.begin || key < sink); }
 
+// The same for a row that is the same in all lanes.
+__device__ __forceinline__ Visible visible_uniform(const Kv4AttnArgs& a, const Sequence& s, int n) {
+  const Visible v = visible(a, s, n);
+  return {__builtin_amdgcn_readfirstlane(v.begin), __builtin_amdgcn_readfirstlane(v.end)};
+}
+
 // The tiles of a range of rows, whose windows ascend: those of the sink, then those from the first row's begin to the last row's end.
 struct Tiles {
   int sink_tiles, first, count;
@@ -80,6 +97,47 @@ struct Tiles {
   }
   __device__ __forceinline__ int at(int t) const { return t < sink_tiles ? t : t - sink_tiles + first; }
 };
+
+// The keys of long sequences are cut into more parts than those of short ones: beside the one that each has, the parts are dealt by the number
+// of tiles.  Up to 64 sequences, one to a lane; more are cut alike.
+struct Part {
+  int b;              // the sequence of a part, or -1
+  int first, count;   // its sequence's parts
+};
+__device__ __forceinline__ Part parts_from(const Kv4AttnArgs& a, bool by_part, int x) {
+  Part p;
+  if (a.parts == a.c.B) return {x, x, 1};
+  if (a.c.B > 64) {
+    p.count = a.parts / a.c.B;
+    p.b = by_part ? x / p.count : x;
+    p.first = p.b * p.count;
+    return p;
+  }
+  const int lane = threadIdx.x & 63;
+  const int kv = lane < a.c.B ? min(min(max(a.kv_len[lane], 0), a.capacity), a.reach) : 0;
+  const unsigned tiles = (unsigned)(kv + kTile - 1) / kTile;
+  unsigned sum = tiles;                                  // (64 sequences of at most 2^24 tiles)
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const unsigned y = (unsigned)__shfl_up((int)sum, d, 64);
+    if (lane >= d) sum += y;
+  }
+  const unsigned all = (unsigned)__builtin_amdgcn_readlane((int)sum, 63);
+  const unsigned more = (unsigned)(a.parts - a.c.B);
+  // where a sequence's parts begin: rounded down from the tiles in front of it
+  auto begin = [&](int i, unsigned front) { return all ? i + (int)((unsigned long long)more * front / all) : i; };
+  const int first = begin(lane, sum - tiles), end = lane < a.c.B ? begin(lane + 1, sum) : 0x7fffffff;
+  const int b = by_part ? (int)__builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < a.c.B && end <= x)) : x;
+  if (b >= a.c.B) return {-1, 0, 0};                     // (no keys at all: a part for each sequence)
+  p.b = b;
+  p.first = __builtin_amdgcn_readlane(first, b);
+  p.count = __builtin_amdgcn_readlane(end, b) - p.first;
+  return p;
+}
+// Where part `split` of `splits` of n tiles begins, in a scalar register (the division is the vector unit's).
+__device__ __forceinline__ int part_of(int n, int split, int splits) {
+  return __builtin_amdgcn_readfirstlane(splits == 1 ? n * split : (int)((unsigned)n * (unsigned long long)(unsigned)split / (unsigned)splits));
+}
 
 // A page that is there, or -1.
 __device__ __forceinline__ int page_of(const Kv4AttnArgs& a, const int32_t* row, int key) {
@@ -127,7 +185,10 @@ __device__ __forceinline__ void take_tile(f32x4 (&s)[kGroups][QB], bf16x8 (&p)[k
         for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * ks + j / 4][qb][j % 4], c, -m[qb]));
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum[qb] += e[j];
-        p[ks][qb] = __builtin_convertvector(e, bf16x8);
+        // rounded here, not where they are used: eight fewer registers for every eight weights while the scores are still needed
+        block_u32x4 bits = __builtin_bit_cast(block_u32x4, __builtin_convertvector(e, bf16x8));
+        asm volatile("" : "+v"(bits));
+        p[ks][qb] = __builtin_bit_cast(bf16x8, bits);
       }
     }
   };
@@ -179,25 +240,41 @@ __device__ __forceinline__ void poison(f32x4 (&o)[CB][QB], const Visible (&v)[QB
   }
 }
 
-// This lane's query rows, one in each 16-query block, as the operand of the first product.  WIDE: the order of channels in which a lane's
+// Query row m of a head of the cache: its token, and the query head.
+struct Row {
+  int n, head;
+  __device__ __forceinline__ Row(const Kv4AttnArgs& a, int kvh, int m) {
+    n = a.group == 1 ? m : m / a.group;
+    head = kvh * a.group + (a.group == 1 ? 0 : m - n * a.group);
+  }
+};
+// What this lane's rows see, one in each 16-query block from row m0 on; a row that does not exist sees nothing.  Taken anew where a tile needs
+// it, behind an opaque m0, so that it does not occupy registers in the loop over tiles.
+template <int QB>
+struct Seen {
+  Visible v[QB];
+  __device__ __forceinline__ Seen(const Kv4AttnArgs& a, const Sequence& s, int m0) {
+    asm volatile("" : "+s"(m0));
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      const int n = Row(a, 0, m0 + 16 * qb + (int)(threadIdx.x & 15)).n;
+      v[qb] = n < s.qn ? visible(a, s, n) : Visible{0, 0};
+    }
+  }
+};
+
+// This lane's query rows as the operand of the first product.  WIDE: the order of channels in which a lane's
 // D / 4 neighbouring channels are its parts of the D / 32 products.
 template <int D, int QB, bool WIDE>
 struct Queries {
-  int n[QB], head[QB];
-  bool there[QB];
-  Visible seen[QB];
   bf16x8 q[QB][D / 32];
   __device__ __forceinline__ void load(const Kv4AttnArgs& a, const Sequence& s, int b, int kvh, int m0) {
     const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
-      const int m = m0 + 16 * qb + r;
-      n[qb] = a.group == 1 ? m : m / a.group;
-      head[qb] = kvh * a.group + (a.group == 1 ? 0 : m - n[qb] * a.group);
-      there[qb] = n[qb] < s.qn;
-      // a row that does not exist sees nothing and has any query
-      seen[qb] = there[qb] ? visible(a, s, n[qb]) : Visible{0, 0};
-      const size_t at = (size_t)b * a.q.sb + (size_t)(there[qb] ? n[qb] : 0) * a.q.sn + (size_t)head[qb] * a.q.sh;
+      const Row row(a, kvh, m0 + 16 * qb + r);
+      // (a row that does not exist has any query)
+      const size_t at = (size_t)b * a.q.sb + (size_t)(row.n < s.qn ? row.n : 0) * a.q.sn + (size_t)row.head * a.q.sh;
 #pragma unroll
       for (int st = 0; st < D / 32; ++st)
         q[qb][st] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const block_u32x4_of2*>(a.qp + at + (WIDE ? g * (D / 4) + st * 8 : st * 32 + g * 8)));
@@ -278,22 +355,24 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_rows_kernel(Kv4AttnArgs a)
   __shared__ float2 merged[kWaves][BM];
   const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // splits innermost
+  // parts innermost
   unsigned id = blockIdx.x;
-  const int split = id % a.splits;
-  id /= a.splits;
+  const int part = __builtin_amdgcn_readfirstlane(id % a.parts);
+  id /= a.parts;
   const int tile_m = id % a.tiles;
-  const unsigned bh = id / a.tiles;
-  const int b = bh / a.c.H, kvh = bh - b * a.c.H;
-  const int m0 = tile_m * BM;
+  const int kvh = __builtin_amdgcn_readfirstlane(id / a.tiles);
+  const Part cut = parts_from(a, true, part);
+  const int b = __builtin_amdgcn_readfirstlane(cut.b);
+  if (b < 0) return;
+  const int m0 = __builtin_amdgcn_readfirstlane(tile_m * BM);
   const Sequence s(a, b);
-  const int n0 = m0 / a.group;
+  const int n0 = __builtin_amdgcn_readfirstlane(m0 / a.group);
   if (n0 >= s.qn) return;
   const int n1 = min((m0 + BM - 1) / a.group, s.qn - 1);
   const int sink = a.window >= 0 ? a.sink : 0;
-  const Visible lo = visible(a, s, n0), hi = visible(a, s, n1);
+  const Visible lo = visible_uniform(a, s, n0), hi = visible_uniform(a, s, n1);
   const Tiles tiles(lo, hi, sink);
-  const int t0 = (int)((long long)tiles.count * split / a.splits), t1 = (int)((long long)tiles.count * (split + 1) / a.splits);
+  const int t0 = part_of(tiles.count, part - cut.first, cut.count), t1 = part_of(tiles.count, part - cut.first + 1, cut.count);
   const int32_t* const table_row = a.c.table + (size_t)b * a.c.max_pages;
 
   Queries<D, QB, true> rows;
@@ -330,8 +409,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_rows_kernel(Kv4AttnArgs a)
         for (int qb = 0; qb < QB; ++qb) sc[kb][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, rows.q[qb][st], sc[kb][qb], 0, 0, 0);
       }
     }
-    const bool whole = key0 + kTile <= lo.end && (key0 >= hi.begin || key0 + kTile <= sink) && !now.missing && n0 + (BM - 1) / a.group < s.qn;
-    if (!whole) mask_tile<QB>(sc, rows.seen, sink, key0, now.missing, g);
+    const bool whole = key0 + kTile <= lo.end && (key0 >= hi.begin || key0 + kTile <= sink) && !now.missing;
+    if (!whole) mask_tile<QB>(sc, Seen<QB>(a, s, m0).v, sink, key0, now.missing, g);
     bf16x8 p[kGroups / 2][QB];
     take_tile<QB, CB>(sc, p, m, l, o, a.scale_log2);
     bool odd = false;
@@ -373,7 +452,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_rows_kernel(Kv4AttnArgs a)
         while (hits) {
           const int at = __builtin_ctzll(hits);
           hits &= hits - 1;
-          poison<QB, CB>(o, rows.seen, sink, key0 + (D == 128 ? 16 * i + (at >> 2) : 32 * i + (at >> 1)), D == 128 ? at & 3 : at & 1);
+          poison<QB, CB>(o, Seen<QB>(a, s, m0).v, sink, key0 + (D == 128 ? 16 * i + (at >> 2) : 32 * i + (at >> 1)), D == 128 ? at & 3 : at & 1);
         }
       }
     }
@@ -399,7 +478,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_rows_kernel(Kv4AttnArgs a)
   }
   __syncthreads();
   constexpr int PIECES = D / 4;
-  const size_t first_row = (size_t)bh * a.rows + m0;
+  const size_t first_row = ((size_t)part * a.c.H + kvh) * a.rows + m0;
   for (int u = threadIdx.x; u < BM * PIECES; u += 64 * kWaves) {
     const int row = u / PIECES, piece = u % PIECES;
     const int mm = m0 + row, n = mm / a.group;
@@ -412,8 +491,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_rows_kernel(Kv4AttnArgs a)
     f32x4 x = {};
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) x += *reinterpret_cast<const f32x4*>(sums + (w * BM + row) * D + (piece ^ (row & 15)) * 4);
-    if (a.splits > 1) {
-      const size_t at = (size_t)split * a.total + first_row + row;
+    if (a.part != nullptr) {
+      const size_t at = first_row + row;
       *reinterpret_cast<f32x4*>(a.part + at * D + piece * 4) = x;
       if (piece == 0) a.stats[at] = float2{top, sum};
       continue;
@@ -429,44 +508,85 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_rows_kernel(Kv4AttnArgs a)
 
 // ---- many rows -----------------------------------------------------------------------------------------------------
 
+// The pages of a wavefront's 16 keys of the tiles t0, t0 + 1, ..: 64 at a time wait in a register, one to a lane, the next 64 are on their way.
+struct PageList {
+  int now, ahead, taken;
+  __device__ __forceinline__ int fetch(const Kv4AttnArgs& a, const Tiles& tiles, const int32_t* row, int t, int t1, int wave) const {
+    t += (int)(threadIdx.x & 63);
+    if (t >= t1) return -1;
+    const int entry = (tiles.at(t) * kTile + 16 * wave) >> a.c.page_log2;
+    return entry < a.c.max_pages ? row[entry] : -1;
+  }
+  __device__ __forceinline__ void open(const Kv4AttnArgs& a, const Tiles& tiles, const int32_t* row, int t0, int t1, int wave) {
+    taken = 0;
+    ahead = fetch(a, tiles, row, t0, t1, wave);
+  }
+  // the page of tile t0 + taken, or -1
+  __device__ __forceinline__ int next(const Kv4AttnArgs& a, const Tiles& tiles, const int32_t* row, int t0, int t1, int wave) {
+    const int lane = taken & 63;
+    if (lane == 0) {
+      now = ahead;
+      asm volatile("" : "+v"(now));       // the copy first: the next 64 then go to the register they are waited for in
+      ahead = fetch(a, tiles, row, t0 + taken + 64, t1, wave);
+    }
+    ++taken;
+    const int page = __builtin_amdgcn_readlane(now, lane);
+    return (unsigned)page < (unsigned)a.c.pages ? page : -1;
+  }
+};
+
+// The loop is skewed by one tile, as in svg_attn_kernel.h: with the scores of tile j in registers a wavefront takes their exponentials and then issues
+// the products of tile j + 1's scores and of tile j's output as one batch; the first operands of a batch are read in front of the exponentials, every
+// other one behind the products.  Keys of tile j + 2 and values of j + 1 are dequantised into LDS meanwhile, those behind them are on their way
+// from memory; one barrier a tile.
 template <int D>
-__global__ __launch_bounds__(64 * kWaves, 2) void kv4_tiles_kernel(Kv4AttnArgs a) {
+struct TileLds {
+  static constexpr int HALF = kTile * 2 * D;             // a tile of keys, or of values
+  __attribute__((aligned(1024))) unsigned char tiles[4 * HALF];      // keys, keys, values, values
+  unsigned long long odd_values[2][kWaves];              // threads of a wavefront whose values are not finite
+  unsigned flags[2][kWaves];                             // bit 0: the 16 keys' page is not there; bit 1: some value is not finite
+};
+
+// Row tile, part and head of the cache number `id`.
+template <int D>
+__device__ __forceinline__ void attend_tile(const Kv4AttnArgs& a, TileLds<D>& shared, unsigned id) {
   constexpr int QB = 2, DS = D / 32, CB = D / 16, BM = 32 * kWaves;
   constexpr int WORDS = D / 32;                          // words of codes that a thread stages of a tile's keys, and of its values
-  constexpr int HALF = kTile * 2 * D;                    // a tile of keys, or of values
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * HALF];
-  __shared__ unsigned long long odd_values[2][kWaves];   // threads of a wavefront whose values are not finite
-  __shared__ unsigned missing_pages[2][kWaves];
+  constexpr int HALF = TileLds<D>::HALF;
+  constexpr int NS = kGroups * DS, NV = kGroups / 2 * CB; // operands of the two products
+  constexpr int AHEAD = D == 128 ? 8 : 4;                // of them in registers
+  constexpr bool SKEWED = D == 128;
+  unsigned char* const lds = shared.tiles;
+  auto& odd_values = shared.odd_values;
+  auto& flags = shared.flags;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, r = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // neighbouring row tiles of a head on one XCD, whose L2 they share
-  const unsigned all = a.total / (unsigned)a.rows * (unsigned)a.tiles * (unsigned)a.splits;
-  const unsigned per_xcd = (all + 7) / 8;
-  unsigned id = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-  if ((blockIdx.x >> 3) >= per_xcd || id >= all) return;
   const int tile_m = id % a.tiles;
   id /= a.tiles;
-  const int split = id % a.splits;
-  const unsigned bh = id / a.splits;
-  const int b = bh / a.c.H, kvh = bh - b * a.c.H;
-  const int m0 = tile_m * BM;
+  const int part = __builtin_amdgcn_readfirstlane(id / a.c.H);
+  const int kvh = __builtin_amdgcn_readfirstlane(id - part * a.c.H);
+  const Part cut = parts_from(a, true, part);
+  const int b = __builtin_amdgcn_readfirstlane(cut.b);
+  if (b < 0) return;
+  const int m0 = __builtin_amdgcn_readfirstlane(tile_m * BM);
   const Sequence s(a, b);
-  const int n0 = m0 / a.group;
+  const int n0 = __builtin_amdgcn_readfirstlane(m0 / a.group);
   if (n0 >= s.qn) return;
   const int n1 = min((m0 + BM - 1) / a.group, s.qn - 1);
   const int sink = a.window >= 0 ? a.sink : 0;
-  const Visible lo = visible(a, s, n0), hi = visible(a, s, n1);
+  const Visible lo = visible_uniform(a, s, n0), hi = visible_uniform(a, s, n1);
   const Tiles tiles(lo, hi, sink);
-  const int t0 = (int)((long long)tiles.count * split / a.splits), t1 = (int)((long long)tiles.count * (split + 1) / a.splits);
+  const int t0 = part_of(tiles.count, part - cut.first, cut.count), t1 = part_of(tiles.count, part - cut.first + 1, cut.count);
   const int32_t* const table_row = a.c.table + (size_t)b * a.c.max_pages;
-  // this wavefront's rows; one without any stages its share and computes nothing
-  const int wm0 = m0 + 32 * wave, wn0 = wm0 / a.group, wn1 = min((wm0 + 31) / a.group, s.qn - 1);
-  const bool active = wn0 < s.qn, full_rows = (wm0 + 31) / a.group < s.qn;
-  const Visible wlo = visible(a, s, min(wn0, s.qn - 1)), whi = visible(a, s, wn1);
+  // What this wavefront's rows see, all of them and any of them; of rows that do not exist nothing is written, whatever they see.  A wavefront
+  // without rows stages its share and computes nothing.
+  const int wm0 = m0 + 32 * wave, wn0 = __builtin_amdgcn_readfirstlane(wm0 / a.group), wn1 = min(__builtin_amdgcn_readfirstlane((wm0 + 31) / a.group), s.qn - 1);
+  const bool active = wn0 < s.qn;
+  const Visible wlo = visible_uniform(a, s, min(wn0, s.qn - 1)), whi = visible_uniform(a, s, wn1);
 
   Queries<D, QB, false> rows;
   rows.load(a, s, b, kvh, wm0);
-  f32x4 o[CB][QB] = {};
+  f32x4 o[CB][QB] = {}, sc[kGroups][QB];
   float m[QB], l[QB];
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
@@ -475,54 +595,79 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_tiles_kernel(Kv4AttnArgs a
   }
 
   // ---- staging: a wavefront has 16 keys of a tile, which are in one page; four threads a key
-  unsigned kw[WORDS], vw[WORDS];
-  unsigned char ks, vs;
-  int staged_key;
-  bool missing;
-  const int sub = tid & 3, stage_row = tid >> 2;
-  auto load = [&](int t) {
-    const int key0 = tiles.at(t) * kTile + 16 * wave;
-    const int page = page_of(a, table_row, key0);
-    missing = page < 0;
-    staged_key = key0 + (lane >> 2);
-    const unsigned char* const record = a.c.data + ((size_t)max(page, 0) * a.c.H + kvh) * a.c.record();
-    const int place = (key0 & ((1 << a.c.page_log2) - 1)) + (lane >> 2);
-    const unsigned char* const p = record + place * (D / 2) + sub * (D / 8);
-    const int scale = place * (D / 32) + (D == 128 ? sub : sub >> 1);
-    if constexpr (D == 128) {
-      const block_u32x4 x = *reinterpret_cast<const block_u32x4*>(p), y = *reinterpret_cast<const block_u32x4*>(p + a.c.values());
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        kw[e] = x[e];
-        vw[e] = y[e];
-      }
-    } else {
-      const u32x2 x = *reinterpret_cast<const u32x2*>(p), y = *reinterpret_cast<const u32x2*>(p + a.c.values());
-      kw[0] = x[0];
-      kw[1] = x[1];
-      vw[0] = y[0];
-      vw[1] = y[1];
-    }
-    ks = record[a.c.key_scales() + scale];
-    vs = record[a.c.value_scales() + scale];
+  struct Raw {
+    unsigned w[WORDS];
+    unsigned char scale;
   };
-  auto stage = [&](int buffer) {
-    unsigned char* const keys = lds + buffer * 2 * HALF;
-    unsigned char* const values = keys + HALF;
-    // keys that nobody sees may be anything: a value that is not finite would not be taken away by its weight of zero
-    const bool gone = missing || staged_key >= hi.end;
-    const bool odd = !gone && not_finite(vs);
-    const float k_scale = gone ? 1.f : power_of(ks), v_scale = gone || odd ? 1.f : power_of(vs);
+  // The wavefront's keys of a tile: the first of them, and where they lie; the same in all lanes.
+  struct Place {
+    int key;
+    bool missing;
+    const unsigned char *codes, *scales;               // of the keys; the values' lie a fixed distance behind
+  };
+  const int sub = tid & 3, stage_row = tid >> 2;
+  const int code_at = (lane >> 2) * (D / 2) + sub * (D / 8), scale_at = (lane >> 2) * (D / 32) + (D == 128 ? sub : sub >> 1);
+  const int v_codes = a.c.values(), v_scales = a.c.value_scales() - a.c.key_scales();
+  const unsigned char* const head_data = a.c.data + (size_t)kvh * a.c.record();
+  const size_t page_step = (size_t)a.c.H * a.c.record();
+  PageList pages;
+  pages.open(a, tiles, table_row, t0, t1, wave);
+  // tile t0, t0 + 1, .. in turn
+  int next_t = t0, next_key = tiles.at(t0) * kTile + 16 * wave;
+  auto next_place = [&]() -> Place {
+    Place x;
+    const int page = pages.next(a, tiles, table_row, t0, t1, wave);
+    x.key = __builtin_amdgcn_readfirstlane(next_key);
+    x.missing = page < 0;
+    const unsigned char* const record = head_data + (unsigned)max(page, 0) * page_step;
+    const unsigned place = x.key & ((1 << a.c.page_log2) - 1);
+    x.codes = record + place * (D / 2);
+    x.scales = record + (unsigned)a.c.key_scales() + place * (D / 32);
+    next_key = x.key + kTile;
+    if (++next_t == tiles.sink_tiles) next_key = tiles.first * kTile + 16 * wave;
+    return x;
+  };
+  auto load = [&](Raw& x, const unsigned char* codes, const unsigned char* scales) {
+    if constexpr (D == 128) {
+      const block_u32x4 y = *reinterpret_cast<const block_u32x4*>(codes + code_at);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x.w[e] = y[e];
+    } else {
+      const u32x2 y = *reinterpret_cast<const u32x2*>(codes + code_at);
+      x.w[0] = y[0];
+      x.w[1] = y[1];
+    }
+    x.scale = scales[scale_at];
+  };
+  // Keys that nobody sees may be anything: scores are replaced, so keys may be staged as they are.
+  auto stage_k = [&](const Raw& x, int buffer) {
+    const float scale = power_of(x.scale);
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w)
+      *reinterpret_cast<bf16x8*>(lds + buffer * HALF + key_piece<D>(stage_row, WORDS * sub + w)) = dequantise8(x.w[w], scale);
+  };
+  // A value that is not finite would not be taken away by its weight of zero.
+  auto stage_v = [&](Raw& x, const Place& at, int buffer) {
+    const bool gone = at.missing || at.key + (lane >> 2) >= hi.end;
+    unsigned long long odd = __builtin_amdgcn_ballot_w64(gone || not_finite(x.scale));
+    if (odd) {
+      const bool bad = !gone && not_finite(x.scale);
+      odd = __builtin_amdgcn_ballot_w64(bad);
+      if (gone || bad) {
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) x.w[w] = 0;
+        x.scale = 127;
+      }
+    }
+    const float scale = power_of(x.scale);
 #pragma unroll
     for (int w = 0; w < WORDS; ++w) {
-      *reinterpret_cast<bf16x8*>(keys + key_piece<D>(stage_row, WORDS * sub + w)) = dequantise8(gone ? 0u : kw[w], k_scale);
       const int piece = WORDS * sub + w;
-      *reinterpret_cast<bf16x8*>(values + value_slot<D>(stage_row, piece >> 1) + (piece & 1) * 16) = dequantise8(gone || odd ? 0u : vw[w], v_scale);
+      *reinterpret_cast<bf16x8*>(lds + (2 + buffer) * HALF + value_slot<D>(stage_row, piece >> 1) + (piece & 1) * 16) = dequantise8(x.w[w], scale);
     }
-    const unsigned long long hits = __builtin_amdgcn_ballot_w64(odd);
     if (lane == 0) {
-      odd_values[buffer][wave] = hits;
-      missing_pages[buffer][wave] = missing;
+      flags[buffer][wave] = (at.missing ? 1u : 0u) | (odd ? 2u : 0u);
+      if (odd) odd_values[buffer][wave] = odd;
     }
   };
 
@@ -531,146 +676,225 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_tiles_kernel(Kv4AttnArgs a
   for (int st = 0; st < DS; ++st) k_off[st] = key_piece<D>(r, 4 * st + g);       // (16 rows on, the swizzle is the same)
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb) v_off[cb] = value_slot<D>(4 * g + (r >> 2), cb) + ((r & 3) << 3);
+  auto k_operand = [&](int buffer, int i) -> bf16x8 {
+    return *reinterpret_cast<const bf16x8*>(lds + buffer * HALF + (i / DS) * 16 * 2 * D + k_off[i % DS]);
+  };
+  auto v_operand = [&](int buffer, int i) -> bf16x8 {
+    const unsigned char* const src = lds + (2 + buffer) * HALF + (i / CB) * 32 * 2 * D + v_off[i % CB];
+    const i16x4 first = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)src);
+    const i16x4 second = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(src + 16 * 2 * D));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(first, second, 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  bf16x8 operand[AHEAD];
+  auto read_keys = [&](int buffer) {
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) operand[i] = k_operand(buffer, i);
+  };
+  // scores of the tile in `buffer`, whose first operands are in registers; the operands behind its own are the values in v_buffer
+  auto scores = [&](int buffer, auto values, int v_buffer) {
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      const bf16x8 k = operand[i % AHEAD];
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb)
+        sc[i / DS][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, rows.q[qb][i % DS], i % DS ? sc[i / DS][qb] : f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+      if (i + AHEAD < NS) operand[i % AHEAD] = k_operand(buffer, i + AHEAD);
+      else if constexpr (decltype(values)::value) operand[i % AHEAD] = v_operand(v_buffer, i + AHEAD - NS);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
 
   if (t0 < t1) {
-    load(t0);
-    stage(0);
-    if (t0 + 1 < t1) load(t0 + 1);
-  }
-  __syncthreads();
-  for (int t = t0; t < t1; ++t) {
-    const int buffer = (t - t0) & 1, key0 = tiles.at(t) * kTile;
-    if (t + 1 < t1) {
-      stage(buffer ^ 1);
-      if (t + 2 < t1) load(t + 2);
+    // Tiles behind the last one are staged too, from any place, and never looked at.
+    Raw k_raw, v_raw;
+    Place p1 = next_place();
+    load(k_raw, p1.codes, p1.scales);
+    load(v_raw, p1.codes + v_codes, p1.scales + v_scales);
+    int key0 = p1.key - 16 * wave;
+    Place p2 = next_place();
+    stage_k(k_raw, 0);
+    load(k_raw, p2.codes, p2.scales);
+    stage_v(v_raw, p1, 0);
+    p1 = p2;
+    load(v_raw, p1.codes + v_codes, p1.scales + v_scales);
+    if constexpr (SKEWED) {
+      p2 = next_place();
+      stage_k(k_raw, 1);
+      load(k_raw, p2.codes, p2.scales);
     }
-    const unsigned char* const keys = lds + buffer * 2 * HALF;
-    const unsigned char* const values = keys + HALF;
-    const unsigned gone = (unsigned)__builtin_amdgcn_ballot_w64(missing_pages[buffer][lane & 3] != 0) & 15u;
-    const bool in_reach = active && key0 < whi.end && (key0 + kTile > wlo.begin || key0 < sink);
-    if (in_reach) {
-      f32x4 sc[kGroups][QB];
-#pragma unroll
-      for (int kb = 0; kb < kGroups; ++kb) {
-#pragma unroll
-        for (int qb = 0; qb < QB; ++qb) sc[kb][qb] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int st = 0; st < DS; ++st) {
-          const bf16x8 k = *reinterpret_cast<const bf16x8*>(keys + kb * 16 * 2 * D + k_off[st]);
-#pragma unroll
-          for (int qb = 0; qb < QB; ++qb) sc[kb][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, rows.q[qb][st], sc[kb][qb], 0, 0, 0);
-        }
+    __syncthreads();
+    if constexpr (SKEWED) {
+      if (active) {
+        read_keys(0);
+        scores(0, std::false_type{}, 0);
       }
-      const bool whole = full_rows && key0 + kTile <= wlo.end && (key0 >= whi.begin || key0 + kTile <= sink) && !gone;
-      if (!whole) mask_tile<QB>(sc, rows.seen, sink, key0, gone, g);
-      bf16x8 p[kGroups / 2][QB];
-      take_tile<QB, CB>(sc, p, m, l, o, a.scale_log2);
-#pragma unroll
-      for (int ks2 = 0; ks2 < kGroups / 2; ++ks2)
-#pragma unroll
-        for (int cb = 0; cb < CB; ++cb) {
-          const unsigned char* const src = values + ks2 * 32 * 2 * D + v_off[cb];
-          const i16x4 first = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)src);
-          const i16x4 second = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(src + 16 * 2 * D));
-          const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(first, second, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-          for (int qb = 0; qb < QB; ++qb) o[cb][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[ks2][qb], o[cb][qb], 0, 0, 0);
+      __syncthreads();
+    }
+
+    auto needs = [&](int key) { return key < whi.end && (key + kTile > wlo.begin || key < sink); };
+    // p1: the tile whose values are on their way; p2: the tile whose keys are, one behind it where the loop is skewed
+    auto trip = [&](auto half) {
+      constexpr int buffer = decltype(half)::value;
+      const int next_key0 = p1.key - 16 * wave;
+      const unsigned flag = flags[buffer][lane & 3];
+      read_keys(SKEWED ? buffer ^ 1 : buffer);
+      __builtin_amdgcn_sched_barrier(0);
+      // the next tiles into LDS: their places were last read before the barrier
+      stage_k(k_raw, SKEWED ? buffer : buffer ^ 1);
+      stage_v(v_raw, p1, buffer ^ 1);
+      if constexpr (!SKEWED) p2 = next_place();
+      p1 = p2;
+      load(v_raw, p1.codes + v_codes, p1.scales + v_scales);
+      if constexpr (SKEWED) p2 = next_place();
+      load(k_raw, p2.codes, p2.scales);
+      __builtin_amdgcn_sched_barrier(0);
+      // skewed, the scores are of the tile behind this one: a wavefront that needs one of the two takes both, with weights of zero for the other
+      if (active && (needs(key0) || (SKEWED && needs(next_key0)))) {
+        if constexpr (!SKEWED) {
+          __builtin_amdgcn_s_setprio(1);
+          scores(buffer, std::true_type{}, buffer);
+          __builtin_amdgcn_s_setprio(0);
         }
-      const unsigned long long odd = odd_values[buffer][lane & 3];
-      if (__builtin_amdgcn_ballot_w64(odd != 0)) {
-        for (int w = 0; w < kWaves; ++w) {
-          unsigned long long hits = odd_values[buffer][w];
-          while (hits) {
-            const int at = __builtin_ctzll(hits);
-            hits &= hits - 1;
-            poison<QB, CB>(o, rows.seen, sink, key0 + 16 * w + (at >> 2), D == 128 ? at & 3 : (at & 3) >> 1);
+        const unsigned gone = (unsigned)__builtin_amdgcn_ballot_w64((flag & 1) != 0) & 15u;
+        const bool whole = key0 + kTile <= wlo.end && (key0 >= whi.begin || key0 + kTile <= sink) && !gone;
+        if (!whole) mask_tile<QB>(sc, Seen<QB>(a, s, wm0).v, sink, key0, gone, g);
+        bf16x8 p[kGroups / 2][QB];
+        take_tile<QB, CB>(sc, p, m, l, o, a.scale_log2);
+        __builtin_amdgcn_s_setprio(1);
+        if constexpr (SKEWED) scores(buffer ^ 1, std::true_type{}, buffer);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          const bf16x8 v = operand[(NS + i) % AHEAD];
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb) o[i % CB][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[i / CB][qb], o[i % CB][qb], 0, 0, 0);
+          if (i + AHEAD < NV) operand[(NS + i) % AHEAD] = v_operand(buffer, i + AHEAD);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_s_setprio(0);
+        if (__builtin_amdgcn_ballot_w64((flag & 2) != 0)) {
+#pragma unroll 1
+          for (int w = 0; w < kWaves; ++w) {
+            unsigned long long hits = flags[buffer][w] & 2 ? odd_values[buffer][w] : 0;
+            while (hits) {
+              const int at = __builtin_ctzll(hits);
+              hits &= hits - 1;
+              poison<QB, CB>(o, Seen<QB>(a, s, wm0).v, sink, key0 + 16 * w + (at >> 2), D == 128 ? at & 3 : (at & 3) >> 1);
+            }
           }
         }
       }
+      key0 = next_key0;
+      __syncthreads();
+    };
+    for (int t = t0;;) {
+      trip(std::integral_constant<int, 0>{});
+      if (++t >= t1) break;
+      trip(std::integral_constant<int, 1>{});
+      if (++t >= t1) break;
     }
-    __syncthreads();
   }
 
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
     const float sum = quarters_sum(l[qb]);
-    if (!rows.there[qb]) continue;
-    if (a.splits > 1) {
-      const size_t at = (size_t)split * a.total + (size_t)bh * a.rows + wm0 + 16 * qb + r;
+    const Row row(a, kvh, wm0 + 16 * qb + r);
+    if (row.n >= s.qn) continue;
+    if (a.part != nullptr) {
+      const size_t at = ((size_t)part * a.c.H + kvh) * a.rows + wm0 + 16 * qb + r;
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) *reinterpret_cast<f32x4*>(a.part + at * D + 16 * cb + 4 * g) = o[cb][qb];
       if (g == 0) a.stats[at] = float2{m[qb], sum};
       continue;
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    __bf16* const to = a.op + (size_t)b * a.o.sb + (size_t)rows.n[qb] * a.o.sn + (size_t)rows.head[qb] * a.o.sh;
+    __bf16* const to = a.op + (size_t)b * a.o.sb + (size_t)row.n * a.o.sn + (size_t)row.head * a.o.sh;
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb)
       *reinterpret_cast<u32x2_of2*>(to + 16 * cb + 4 * g) = __builtin_bit_cast(u32x2, __builtin_convertvector(o[cb][qb] * inv, bf16x4));
     if (g == 0 && a.lse)
-      a.lse[((size_t)b * a.c.H * a.group + rows.head[qb]) * a.N + rows.n[qb]] =
+      a.lse[((size_t)b * a.c.H * a.group + row.head) * a.N + row.n] =
           sum == 0.f ? -INFINITY : (m[qb] + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
   }
 }
 
+// Neighbouring row tiles of a head on one XCD, whose L2 they share: an XCD has an eighth of them.
+template <int D>
+__global__ __launch_bounds__(64 * kWaves, D == 128 ? 2 : 3) void kv4_tiles_kernel(Kv4AttnArgs a) {
+  __shared__ TileLds<D> shared;
+  const unsigned all = (unsigned)a.c.H * (unsigned)a.tiles * (unsigned)a.parts, per_xcd = (all + 7) / 8;
+  const unsigned id = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+  if (blockIdx.x >> 3 < per_xcd && id < all) attend_tile<D>(a, shared, id);
+}
+
 // ---- parts of the keys joined -----------------------------------------------------------------------------------------
 
+// A row's lanes look at as many parts at once, one each, and then add up their four channels over them.
 template <int D>
 __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a) {
   constexpr int LANES = D / 4;                           // of a row, four channels each
-  const long long row = (long long)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+  const int b = blockIdx.y;
+  const Part cut = parts_from(a, false, b);
+  const long long row = (long long)blockIdx.x * (256 / LANES) + threadIdx.x / LANES, of_head = a.rows;
   const int piece = threadIdx.x % LANES;
-  if (row >= a.total) return;
-  const unsigned bh = (unsigned)(row / a.rows);
-  const int mm = (int)(row - (long long)bh * a.rows);
-  const int b = bh / a.c.H, kvh = bh - b * a.c.H;
-  const int n = mm / a.group;
-  const int qn = a.q_len ? min(max(a.q_len[b], 0), a.N) : a.N;
-  if (n >= qn) return;
+  const int kvh = (int)(row / of_head), m = (int)(row - kvh * of_head);
+  const Sequence s(a, b);
+  const Row at(a, kvh, m);
+  if (kvh >= a.c.H || at.n >= s.qn) return;              // (whole rows leave)
+  const size_t step = (size_t)a.c.H * a.rows, first = (size_t)cut.first * step + (size_t)row;
   float top = kNegBig;
-  for (int x = 0; x < a.splits; ++x) top = fmaxf(top, a.stats[(size_t)x * a.total + row].x);
+  for (int base = 0; base < cut.count; base += LANES) {
+    const int x = base + piece;
+    top = fmaxf(top, x < cut.count ? a.stats[first + x * step].x : kNegBig);
+  }
+#pragma unroll
+  for (int d = LANES / 2; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, LANES));
   float sum = 0.f;
   f32x4 o = {};
-  for (int x = 0; x < a.splits; ++x) {
-    const size_t at = (size_t)x * a.total + row;
-    const float2 st = a.stats[at];
+  for (int base = 0; base < cut.count; base += LANES) {
+    const int x = base + piece;
+    const float2 st = x < cut.count ? a.stats[first + x * step] : float2{kNegBig, 0.f};
     const float f = __builtin_amdgcn_exp2f(st.x - top);
     sum += st.y * f;
-    o += *reinterpret_cast<const f32x4*>(a.part + at * D + piece * 4) * f;
+    const int n = min(LANES, cut.count - base);
+#pragma unroll 8
+    for (int y = 0; y < n; ++y) o += *reinterpret_cast<const f32x4*>(a.part + (first + (base + y) * step) * D + piece * 4) * __shfl(f, y, LANES);
   }
+#pragma unroll
+  for (int d = LANES / 2; d > 0; d >>= 1) sum += __shfl_xor(sum, d, LANES);
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  const int head = kvh * a.group + (mm - n * a.group);
-  *reinterpret_cast<u32x2_of2*>(a.op + (size_t)b * a.o.sb + (size_t)n * a.o.sn + (size_t)head * a.o.sh + piece * 4) =
+  *reinterpret_cast<u32x2_of2*>(a.op + (size_t)b * a.o.sb + (size_t)at.n * a.o.sn + (size_t)at.head * a.o.sh + piece * 4) =
       __builtin_bit_cast(u32x2, __builtin_convertvector(o * inv, bf16x4));
   if (piece == 0 && a.lse)
-    a.lse[((size_t)b * a.c.H * a.group + head) * a.N + n] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+    a.lse[((size_t)b * a.c.H * a.group + at.head) * a.N + at.n] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
 }
 
 }  // namespace
+
+// Workgroups of the form with 128 rows that the chip holds: two and three to a compute unit.
+constexpr int kv4_places(int D) { return D == 128 ? 512 : 768; }
 
 Kv4Plan kv4_plan(const Kv4& c, const svg_kv4_attn_t& attn, long long N, int group) {
   Kv4Plan p = {};
   p.rows = (int)(N * group);
   p.tile = p.rows <= 16 ? 16 : p.rows <= 32 ? 32 : 128;
   p.tiles = std::max(1, (p.rows + p.tile - 1) / p.tile);
-  p.total = (long long)c.B * c.H * p.rows;
   // keys that a row tile may have to visit
   const long long capacity = (long long)c.max_pages << c.page_log2;
   long long keys = attn.max_kv > 0 ? std::min<long long>(attn.max_kv, capacity) : capacity;
-  if (attn.window >= 0 && attn.causal) {
-    const long long reach = (attn.window + 1ll) * attn.block + (attn.sink < keys ? attn.sink : keys) + p.tile / group;
-    keys = std::min(keys, reach);
-  }
+  if (attn.window >= 0 && attn.causal) keys = std::min(keys, (attn.window + 1ll) * attn.block + std::min<long long>(attn.sink, keys) + p.tile / group);
+  p.reach = (int)keys;
   const long long units = (keys + kTile - 1) / kTile;
-  const long long whole = (long long)c.B * c.H * p.tiles;
-  const long long wanted = p.tile == 128 ? 512 : 1024, least = p.tile == 128 ? 8 : 2 * kWaves;
-  p.splits = 1;
-  if (whole > 0 && whole < wanted) p.splits = (int)std::max<long long>(1, std::min(std::min((wanted + whole - 1) / whole, units / least), 64ll));
+  // parts for one round of workgroups, each of a few tiles at least
+  const long long places = p.tile == 128 ? kv4_places(c.D) : 512, least = p.tile == 128 ? 8 : 2 * kWaves;
+  const long long parts = std::min(places / ((long long)c.H * p.tiles), c.B * std::max(1ll, units / least));
+  p.parts = (int)(c.B <= 64 ? std::max<long long>(parts, c.B) : c.B * std::max(1ll, parts / c.B));
   return p;
 }
 
 size_t kv4_workspace_bytes(const Kv4& c, const Kv4Plan& p) {
-  return p.splits > 1 ? (size_t)p.splits * (size_t)p.total * ((size_t)c.D * 4 + 8) : 0;
+  return p.parts > c.B ? (size_t)p.parts * c.H * (size_t)p.rows * ((size_t)c.D * 4 + 8) : 0;
 }
 
 int launch_kv4_attn(const Kv4& c, const svg_kv4_attn_t& attn, const Kv4Plan& plan, const HeadRows& q, const void* qp, const HeadRows& o,
@@ -688,11 +912,12 @@ int launch_kv4_attn(const Kv4& c, const svg_kv4_attn_t& attn, const Kv4Plan& pla
   a.group = group;
   a.rows = plan.rows;
   a.tiles = plan.tiles;
-  a.splits = plan.splits;
-  if (plan.total > 0x7fffffffll) return SVG_ERR_UNSUPPORTED;
-  a.total = (unsigned)plan.total;
-  a.part = static_cast<float*>(workspace);
-  a.stats = reinterpret_cast<float2*>(static_cast<char*>(workspace) + (size_t)plan.splits * plan.total * c.D * 4);
+  a.parts = plan.parts;
+  a.reach = plan.reach;
+  if (plan.parts > c.B) {
+    a.part = static_cast<float*>(workspace);
+    a.stats = reinterpret_cast<float2*>(a.part + (size_t)plan.parts * c.H * plan.rows * c.D);
+  }
   a.causal = attn.causal;
   a.block = attn.block;
   a.window = attn.window;
@@ -700,20 +925,21 @@ int launch_kv4_attn(const Kv4& c, const svg_kv4_attn_t& attn, const Kv4Plan& pla
   a.capacity = c.pages ? c.max_pages << c.page_log2 : 0;      // (without a pool there is nothing that a load could be sent to)
   const float scale = attn.softmax_scale > 0.f ? attn.softmax_scale : 1.f / sqrtf((float)c.D);
   a.scale_log2 = scale * 1.4426950408889634f;
-  const long long blocks = (long long)c.B * c.H * plan.tiles * plan.splits;
-  if (blocks > (1ll << 24)) return SVG_ERR_UNSUPPORTED;
+  const long long blocks = (long long)c.H * plan.tiles * plan.parts;
+  if (blocks > (1ll << 24)) return SVG_ERR_UNSUPPORTED;       // a launch has fewer than 2^32 threads
   (void)hipGetLastError();
   const bool wide = c.D == 128;
-  if (plan.tile == 128)
+  if (plan.tile == 128) {
     hipLaunchKernelGGL((wide ? kv4_tiles_kernel<128> : kv4_tiles_kernel<64>), dim3((unsigned)((blocks + 7) / 8 * 8)), dim3(64 * kWaves), 0, stream, a);
-  else if (plan.tile == 32)
+  } else if (plan.tile == 32)
     hipLaunchKernelGGL((wide ? kv4_rows_kernel<128, 2> : kv4_rows_kernel<64, 2>), dim3((unsigned)blocks), dim3(64 * kWaves), 0, stream, a);
   else
     hipLaunchKernelGGL((wide ? kv4_rows_kernel<128, 1> : kv4_rows_kernel<64, 1>), dim3((unsigned)blocks), dim3(64 * kWaves), 0, stream, a);
-  if (plan.splits > 1) {
+  if (plan.parts > c.B) {
+    const long long rows = (long long)c.H * plan.rows;        // of a sequence
     const int per_block = 256 / (c.D / 4);
-    hipLaunchKernelGGL((wide ? kv4_join_kernel<128> : kv4_join_kernel<64>), dim3((unsigned)((plan.total + per_block - 1) / per_block)), dim3(256), 0,
-                       stream, a);
+    hipLaunchKernelGGL((wide ? kv4_join_kernel<128> : kv4_join_kernel<64>), dim3((unsigned)((rows + per_block - 1) / per_block), (unsigned)c.B), dim3(256),
+                       0, stream, a);
   }
   return hip_status(hipGetLastError());
 }
