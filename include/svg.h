@@ -519,7 +519,8 @@ int svg_fp4_linear_quantize(int64_t M, int64_t N, int64_t K, const void* a, cons
  * as svg_fp4_linear, but the activations stay as they are: x is a token matrix of B*N = M rows and H*D = K columns, in_act is taken in
  * fp32 and not rounded, and every product is exact in the accumulation's fp32.  w, w_scales: an operand [N, K] (svg_fp4_quantize).  out: a token
  * matrix of M rows and N columns, which must not overlap an input (SVG_ERR_ALIAS).  M <= 1024; made for up to 16 rows (every further
- * 16 read the weights once more).  An infinite or NaN activation makes its row NaN or infinite.  K >= 1, N >= 1; results repeat bit for bit.
+ * 16 read the weights once more).  An infinite or NaN activation makes its row NaN or infinite.  K >= 1, N >= 1; results repeat bit for bit and do not
+ * depend on the other rows of the call.
  */
 int svg_fp4_linear_rows(const svg_tokens_t* x_desc, const void* x, int in_activation, int64_t N, const void* w, const void* w_scales,
                         const float* bias, int activation, const svg_tokens_t* out_desc, void* out, void* stream);

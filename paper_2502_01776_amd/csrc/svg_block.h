@@ -1,6 +1,8 @@
 // Shared by the operators around the attention (gate + norm + modulation, microscaled 4-bit operands and products):
 // element types, token matrices, the operand order of microscaled 4-bit matrices, sums over a wavefront.
 #pragma once
+#include <atomic>
+
 #include "svg_internal.h"
 
 namespace svg {
@@ -57,6 +59,18 @@ LinearForm fp4_linear_form(long long m_tiles, long long pairs, int k_tiles, bool
 int launch_fp4_linear(long long M, int N, int K, const void* a, const void* a_scales, const void* w, const void* w_scales,
                       const float* bias, int activation, const Tokens* tok, void* out, void* codes, void* scales,
                       hipStream_t stream);
+
+// Lets a kernel take more than 64 KB of LDS; once for each GPU, because the call costs a microsecond.
+inline hipError_t allow_lds(const void* kernel, int bytes, std::atomic<unsigned long long>& allowed) {
+  int device = 0;
+  hipError_t e = hipGetDevice(&device);
+  if (e != hipSuccess) return e;
+  const unsigned long long bit = device < 64 ? 1ull << device : 0;
+  if (allowed.load(std::memory_order_relaxed) & bit) return hipSuccess;
+  e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == hipSuccess) allowed.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
 
 __host__ __device__ constexpr int type_bytes(int type) { return type == SVG_F32 ? 4 : 2; }
 

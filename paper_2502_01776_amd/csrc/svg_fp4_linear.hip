@@ -281,18 +281,6 @@ __device__ __forceinline__ void load_words_to_lds(const attn::u32x4 rsrc, int vo
 template <int N>
 __device__ __forceinline__ void wait_stage() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory"); }
 
-// Lets a kernel take more than 64 KB of LDS; once for each GPU, because the call costs a microsecond.
-hipError_t allow_lds(const void* kernel, int bytes, std::atomic<unsigned long long>& allowed) {
-  int device = 0;
-  hipError_t e = hipGetDevice(&device);
-  if (e != hipSuccess) return e;
-  const unsigned long long bit = device < 64 ? 1ull << device : 0;
-  if (allowed.load(std::memory_order_relaxed) & bit) return hipSuccess;
-  e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e == hipSuccess) allowed.fetch_or(bit, std::memory_order_relaxed);
-  return e;
-}
-
 // Output tiles of WM x WN wavefronts, each TM token tiles times TP pairs of column tiles.
 //
 // A step is one column tile of K (128 columns); four steps, whose scale bytes share a word, are a group.  The token operands,
