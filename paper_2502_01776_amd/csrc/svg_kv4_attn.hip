@@ -139,13 +139,6 @@ __device__ __forceinline__ int part_of(int n, int split, int splits) {
   return __builtin_amdgcn_readfirstlane(splits == 1 ? n * split : (int)((unsigned)n * (unsigned long long)(unsigned)split / (unsigned)splits));
 }
 
-// A page that is there, or -1.
-__device__ __forceinline__ int page_of(const Kv4AttnArgs& a, const int32_t* row, int key) {
-  const int entry = key >> a.c.page_log2;
-  const int page = entry < a.c.max_pages ? __builtin_amdgcn_readfirstlane(row[entry]) : -1;
-  return (unsigned)page < (unsigned)a.c.pages ? page : -1;
-}
-
 __device__ __forceinline__ float power_of(unsigned scale) { return __uint_as_float(scale << 23); }
 // A block of values that are not finite: zeros in the product, NaN put into the results of the queries that see it afterwards, since a
 // weight of zero does not take it away.
@@ -286,7 +279,40 @@ typedef unsigned u32x2_of2 __attribute__((ext_vector_type(2), aligned(2)));
 
 // ---- few rows ------------------------------------------------------------------------------------------------------
 
-// A wavefront's tile in registers, as it comes from memory.
+// The pages of every fourth tile from t on, four 16-key groups each: 16 tiles at a time wait in a register, one group to a lane, the next 16 are on
+// their way.
+struct GroupPages {
+  int now, ahead, taken;
+  __device__ __forceinline__ int fetch(const Kv4AttnArgs& a, const Tiles& tiles, const int32_t* row, int t, int t1) const {
+    const int lane = threadIdx.x & 63;
+    t += kWaves * (lane >> 2);
+    if (t >= t1) return -1;
+    const int entry = (tiles.at(t) * kTile + 16 * (lane & 3)) >> a.c.page_log2;
+    return entry < a.c.max_pages ? row[entry] : -1;
+  }
+  __device__ __forceinline__ void open(const Kv4AttnArgs& a, const Tiles& tiles, const int32_t* row, int t, int t1) {
+    taken = 0;
+    ahead = fetch(a, tiles, row, t, t1);
+  }
+  // the pages of the next tile, t being the first of all; -1: not there
+  __device__ __forceinline__ void next(const Kv4AttnArgs& a, const Tiles& tiles, const int32_t* row, int t, int t1, int (&page)[kGroups]) {
+    const int at = taken & 15;
+    if (at == 0) {
+      now = ahead;
+      asm volatile("" : "+v"(now));       // the copy first: the next ones then go to the register they are waited for in
+      ahead = fetch(a, tiles, row, t + kWaves * (taken + 16), t1);
+    }
+    ++taken;
+#pragma unroll
+    for (int kb = 0; kb < kGroups; ++kb) {
+      const int x = __builtin_amdgcn_readlane(now, 4 * at + kb);
+      page[kb] = (unsigned)x < (unsigned)a.c.pages ? x : -1;
+    }
+  }
+};
+
+// A wavefront's tile in registers, as it comes from memory: the keys are asked for where those in front have gone into the scores, the
+// values where those in front have gone to LDS.
 template <int D>
 struct RawTile {
   static constexpr int kKeyWords = D / 32;               // words of codes a lane has of a key
@@ -294,26 +320,28 @@ struct RawTile {
   unsigned k[kGroups][kKeyWords];
   block_u32x4 v[kValueLoads];
   unsigned char ks[kGroups], vs[kValueLoads];
+  const unsigned char* group[kGroups];                   // the groups' keys; the same in all lanes
+  const unsigned char* scales[kGroups];
+  int key0;
   unsigned missing;
 
-  __device__ __forceinline__ void load(const Kv4AttnArgs& a, const int32_t* table_row, int kvh, int key0) {
-    const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
-    const long long record = a.c.record();
-    const int mask = (1 << a.c.page_log2) - 1;
-    const unsigned char* group[kGroups];
-    int place[kGroups];
+  __device__ __forceinline__ void place(const Kv4AttnArgs& a, const unsigned char* head_data, size_t page_step, int key, const int (&page)[kGroups]) {
+    key0 = key;
     missing = 0;
 #pragma unroll
     for (int kb = 0; kb < kGroups; ++kb) {
-      const int page = page_of(a, table_row, key0 + 16 * kb);
-      missing |= page < 0 ? 1u << kb : 0u;
-      group[kb] = a.c.data + ((size_t)max(page, 0) * a.c.H + kvh) * record;
-      place[kb] = (key0 + 16 * kb) & mask;
+      missing |= page[kb] < 0 ? 1u << kb : 0u;
+      const unsigned char* const record = head_data + (unsigned)max(page[kb], 0) * page_step;
+      const unsigned at = (unsigned)(key + 16 * kb) & ((1u << a.c.page_log2) - 1);
+      group[kb] = record + at * (D / 2);
+      scales[kb] = record + (unsigned)a.c.key_scales() + at * (D / 32);
     }
+  }
+  __device__ __forceinline__ void load_keys() {
+    const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
 #pragma unroll
     for (int kb = 0; kb < kGroups; ++kb) {
-      const int row = place[kb] + r;
-      const unsigned char* const p = group[kb] + row * (D / 2) + g * (D / 8);
+      const unsigned char* const p = group[kb] + (unsigned)(r * (D / 2) + g * (D / 8));
       if constexpr (D == 128) {
         const block_u32x4 x = *reinterpret_cast<const block_u32x4*>(p);
 #pragma unroll
@@ -323,30 +351,30 @@ struct RawTile {
         k[kb][0] = x[0];
         k[kb][1] = x[1];
       }
-      ks[kb] = group[kb][a.c.key_scales() + row * (D / 32) + (D == 128 ? g : g >> 1)];
+      ks[kb] = scales[kb][(unsigned)(r * (D / 32) + (D == 128 ? g : g >> 1))];
     }
-#pragma unroll
-    for (int i = 0; i < kValueLoads; ++i) {
-      // D = 128: 16 keys a load, four lanes each; D = 64: 32 keys, two lanes each
-      const unsigned char* from;
-      int row, block;
-      if constexpr (D == 128) {
-        from = group[i];
-        row = place[i] + (lane >> 2);
-        block = lane & 3;
-      } else {
-        from = lane < 32 ? group[2 * i] : group[2 * i + 1];
-        row = (lane < 32 ? place[2 * i] : place[2 * i + 1]) + ((lane >> 1) & 15);
-        block = lane & 1;
-      }
-      v[i] = *reinterpret_cast<const block_u32x4*>(from + a.c.values() + row * (D / 2) + block * 16);
-      vs[i] = from[a.c.value_scales() + row * (D / 32) + block];
+  }
+  // load i: D = 128: 16 keys, four lanes each; D = 64: 32 keys, two lanes each
+  __device__ __forceinline__ void load_value(const Kv4AttnArgs& a, int i) {
+    const int lane = threadIdx.x & 63;
+    const int v_codes = a.c.values(), v_scales = a.c.value_scales() - a.c.key_scales();
+    if constexpr (D == 128) {
+      v[i] = *reinterpret_cast<const block_u32x4*>(group[i] + v_codes + (unsigned)(lane * 16));
+      vs[i] = (scales[i] + v_scales)[(unsigned)lane];
+    } else {
+      const unsigned char* const from = lane < 32 ? group[2 * i] : group[2 * i + 1];
+      const unsigned char* const scale = lane < 32 ? scales[2 * i] : scales[2 * i + 1];
+      v[i] = *reinterpret_cast<const block_u32x4*>(from + v_codes + (lane & 31) * 16);
+      vs[i] = scale[v_scales + (lane & 31)];
     }
   }
 };
 
+// Wavefronts to a SIMD: enough that the others' work covers a trip to memory.
+constexpr int rows_waves(int D, int QB) { return D == 64 ? (QB == 1 ? 4 : 3) : QB == 1 ? 3 : 2; }
+
 template <int D, int QB>
-__global__ __launch_bounds__(64 * kWaves, 2) void kv4_rows_kernel(Kv4AttnArgs a) {
+__global__ __launch_bounds__(64 * kWaves, rows_waves(D, QB)) void kv4_rows_kernel(Kv4AttnArgs a) {
   constexpr int DS = D / 32, CB = D / 16, BM = 16 * QB;
   constexpr int STAGE = 32 * 2 * D;                      // half a tile of values
   constexpr int MERGE = BM * D * 4;                      // a wavefront's results
@@ -389,66 +417,93 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_rows_kernel(Kv4AttnArgs a)
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb) v_off[cb] = value_slot<D>(4 * g + (r >> 2), cb) + ((r & 3) << 3);
 
-  RawTile<D> next;
-  int t = t0 + wave;
-  if (t < t1) next.load(a, table_row, kvh, tiles.at(t) * kTile);
-  for (; t < t1; t += kWaves) {
-    const int key0 = tiles.at(t) * kTile;
-    RawTile<D> now = next;
-    if (t + kWaves < t1) next.load(a, table_row, kvh, tiles.at(t + kWaves) * kTile);
+  const unsigned char* const head_data = a.c.data + (size_t)kvh * a.c.record();
+  const size_t page_step = (size_t)a.c.H * a.c.record();
+  constexpr int LOADS = RawTile<D>::kValueLoads;
+  RawTile<D> raw;
+  GroupPages pages;
+  const int first = t0 + wave;
+  pages.open(a, tiles, table_row, first, t1);
+  auto place = [&](int t) {
+    int page[kGroups];
+    pages.next(a, tiles, table_row, first, t1, page);
+    raw.place(a, head_data, page_step, tiles.at(t) * kTile, page);
+  };
+  if (first < t1) {
+    place(first);
+    raw.load_keys();
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) raw.load_value(a, i);
+  }
+  for (int t = first; t < t1; t += kWaves) {
+    const int key0 = raw.key0;
+    const unsigned missing = raw.missing;
     f32x4 sc[kGroups][QB];
 #pragma unroll
     for (int kb = 0; kb < kGroups; ++kb) {
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) sc[kb][qb] = f32x4{0.f, 0.f, 0.f, 0.f};
-      const float scale = power_of(now.ks[kb]);
+      const float scale = power_of(raw.ks[kb]);
 #pragma unroll
       for (int st = 0; st < DS; ++st) {
-        const bf16x8 k = dequantise8(now.k[kb][st], scale);
+        const bf16x8 k = dequantise8(raw.k[kb][st], scale);
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) sc[kb][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, rows.q[qb][st], sc[kb][qb], 0, 0, 0);
       }
     }
-    const bool whole = key0 + kTile <= lo.end && (key0 >= hi.begin || key0 + kTile <= sink) && !now.missing;
-    if (!whole) mask_tile<QB>(sc, Seen<QB>(a, s, m0).v, sink, key0, now.missing, g);
+    // (behind the last tile the same one again)
+    place(min(t + kWaves, t1 - 1));
+    raw.load_keys();
+    const bool whole = key0 + kTile <= lo.end && (key0 >= hi.begin || key0 + kTile <= sink) && !missing;
+    if (!whole) mask_tile<QB>(sc, Seen<QB>(a, s, m0).v, sink, key0, missing, g);
     bf16x8 p[kGroups / 2][QB];
     take_tile<QB, CB>(sc, p, m, l, o, a.scale_log2);
-    bool odd = false;
+    // values that are not finite, and those that nobody sees, which may be anything
+    unsigned long long odd[LOADS];
+    bool any_odd = false;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int row = D == 128 ? 16 * i + (lane >> 2) : 32 * i + (lane >> 1);
+      const bool gone = key0 + row >= hi.end || (missing >> (row >> 4) & 1) != 0;
+      odd[i] = __builtin_amdgcn_ballot_w64(gone || not_finite(raw.vs[i]));
+      if (odd[i]) {
+        const bool bad = !gone && not_finite(raw.vs[i]);
+        odd[i] = __builtin_amdgcn_ballot_w64(bad);
+        any_odd |= odd[i] != 0;
+        if (gone || bad) {
+          raw.v[i] = block_u32x4{0, 0, 0, 0};
+          raw.vs[i] = 127;
+        }
+      }
+    }
 #pragma unroll
     for (int ks = 0; ks < kGroups / 2; ++ks) {
-      constexpr int LOADS = RawTile<D>::kValueLoads / 2;
 #pragma unroll
-      for (int x = 0; x < LOADS; ++x) {
-        const int i = ks * LOADS + x;
+      for (int x = 0; x < LOADS / 2; ++x) {
+        const int i = ks * (LOADS / 2) + x;
         const int row = D == 128 ? 16 * x + (lane >> 2) : lane >> 1, block = D == 128 ? lane & 3 : lane & 1;
-        const int key = key0 + 32 * ks + row;
-        const bool gone = key >= hi.end || (now.missing >> (2 * ks + (row >> 4)) & 1) != 0;
-        const bool bad = !gone && not_finite(now.vs[i]);
-        odd |= bad;
-        const float scale = power_of(now.vs[i]);
+        const float scale = power_of(raw.vs[i]);
 #pragma unroll
         for (int w = 0; w < 4; ++w)
-          *reinterpret_cast<bf16x8*>(own + value_slot<D>(row, 2 * block + (w >> 1)) + (w & 1) * 16) =
-              dequantise8(gone || bad ? 0u : now.v[i][w], gone || bad ? 1.f : scale);
+          *reinterpret_cast<bf16x8*>(own + value_slot<D>(row, 2 * block + (w >> 1)) + (w & 1) * 16) = dequantise8(raw.v[i][w], scale);
+        raw.load_value(a, i);
       }
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) {
         const unsigned char* const src = own + v_off[cb];
-        const i16x4 first = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)src);
-        const i16x4 second = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(src + 16 * 2 * D));
-        const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(first, second, 0, 1, 2, 3, 4, 5, 6, 7));
+        const i16x4 first_keys = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)src);
+        const i16x4 second_keys = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(src + 16 * 2 * D));
+        const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(first_keys, second_keys, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) o[cb][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[ks][qb], o[cb][qb], 0, 0, 0);
       }
     }
-    if (__builtin_amdgcn_ballot_w64(odd)) {
-      for (int i = 0; i < RawTile<D>::kValueLoads; ++i) {
-        const int row = D == 128 ? 16 * i + (lane >> 2) : 32 * i + (lane >> 1);
-        unsigned char scale = 0;
+    if (any_odd) {
+#pragma unroll 1
+      for (int i = 0; i < LOADS; ++i) {
+        unsigned long long hits = 0;
 #pragma unroll
-        for (int x = 0; x < RawTile<D>::kValueLoads; ++x) scale = x == i ? now.vs[x] : scale;
-        const bool bad = key0 + row < hi.end && !(now.missing >> (row >> 4) & 1) && not_finite(scale);
-        unsigned long long hits = __builtin_amdgcn_ballot_w64(bad);
+        for (int x = 0; x < LOADS; ++x) hits = x == i ? odd[x] : hits;
         while (hits) {
           const int at = __builtin_ctzll(hits);
           hits &= hits - 1;
@@ -830,39 +885,50 @@ __global__ __launch_bounds__(64 * kWaves, D == 128 ? 2 : 3) void kv4_tiles_kerne
 
 // ---- parts of the keys joined -----------------------------------------------------------------------------------------
 
-// A row's lanes look at as many parts at once, one each, and then add up their four channels over them.
-template <int D>
+// D / 4 lanes have four channels each and GROUPS such sets of lanes a row, every GROUPS-th part each; they add up through LDS in the order of their
+// number.  Eight sets where rows are few, so that all parts are on their way at once (one token over 64 parts 11 -> 5 us), else one.
+template <int D, int GROUPS>
 __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a) {
-  constexpr int LANES = D / 4;                           // of a row, four channels each
+  constexpr int LANES = D / 4, ROWS = 256 / (LANES * GROUPS);
+  __shared__ f32x4 part_o[GROUPS > 1 ? ROWS : 1][GROUPS][LANES];
+  __shared__ float part_sum[GROUPS > 1 ? ROWS : 1][GROUPS];
   const int b = blockIdx.y;
   const Part cut = parts_from(a, false, b);
-  const long long row = (long long)blockIdx.x * (256 / LANES) + threadIdx.x / LANES, of_head = a.rows;
-  const int piece = threadIdx.x % LANES;
-  const int kvh = (int)(row / of_head), m = (int)(row - kvh * of_head);
+  const int piece = threadIdx.x % LANES, set = threadIdx.x / LANES % GROUPS, own = threadIdx.x / (LANES * GROUPS);
+  const long long row = (long long)blockIdx.x * ROWS + own, of_sequence = (long long)a.c.H * a.rows;
+  const int kvh = (int)(min(row, of_sequence - 1) / a.rows), m = (int)(min(row, of_sequence - 1) - (long long)kvh * a.rows);
   const Sequence s(a, b);
   const Row at(a, kvh, m);
-  if (kvh >= a.c.H || at.n >= s.qn) return;              // (whole rows leave)
-  const size_t step = (size_t)a.c.H * a.rows, first = (size_t)cut.first * step + (size_t)row;
+  const bool there = row < of_sequence && at.n < s.qn;
+  const size_t step = (size_t)a.c.H * a.rows, first = (size_t)cut.first * step + (size_t)kvh * a.rows + m;
+  const int count = there ? cut.count : 0;
+  // the reference of all parts, a part to a lane
   float top = kNegBig;
-  for (int base = 0; base < cut.count; base += LANES) {
-    const int x = base + piece;
-    top = fmaxf(top, x < cut.count ? a.stats[first + x * step].x : kNegBig);
-  }
+  for (int x = piece; x < count; x += LANES) top = fmaxf(top, a.stats[first + x * step].x);
 #pragma unroll
   for (int d = LANES / 2; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, LANES));
   float sum = 0.f;
   f32x4 o = {};
-  for (int base = 0; base < cut.count; base += LANES) {
-    const int x = base + piece;
-    const float2 st = x < cut.count ? a.stats[first + x * step] : float2{kNegBig, 0.f};
+#pragma unroll 4
+  for (int x = set; x < count; x += GROUPS) {
+    const float2 st = a.stats[first + x * step];
+    const f32x4 y = *reinterpret_cast<const f32x4*>(a.part + (first + x * step) * D + piece * 4);
     const float f = __builtin_amdgcn_exp2f(st.x - top);
     sum += st.y * f;
-    const int n = min(LANES, cut.count - base);
-#pragma unroll 8
-    for (int y = 0; y < n; ++y) o += *reinterpret_cast<const f32x4*>(a.part + (first + (base + y) * step) * D + piece * 4) * __shfl(f, y, LANES);
+    o += y * f;
   }
+  if constexpr (GROUPS > 1) {
+    part_o[own][set][piece] = o;
+    if (piece == 0) part_sum[own][set] = sum;
+    __syncthreads();
+    if (set > 0) return;
 #pragma unroll
-  for (int d = LANES / 2; d > 0; d >>= 1) sum += __shfl_xor(sum, d, LANES);
+    for (int x = 1; x < GROUPS; ++x) {
+      o += part_o[own][x][piece];
+      sum += part_sum[own][x];
+    }
+  }
+  if (!there) return;
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   *reinterpret_cast<u32x2_of2*>(a.op + (size_t)b * a.o.sb + (size_t)at.n * a.o.sn + (size_t)at.head * a.o.sh + piece * 4) =
       __builtin_bit_cast(u32x2, __builtin_convertvector(o * inv, bf16x4));
@@ -878,14 +944,18 @@ constexpr int kv4_places(int D) { return D == 128 ? 512 : 768; }
 Kv4Plan kv4_plan(const Kv4& c, const svg_kv4_attn_t& attn, long long N, int group) {
   Kv4Plan p = {};
   p.rows = (int)(N * group);
-  p.tile = p.rows <= 16 ? 16 : p.rows <= 32 ? 32 : 128;
-  p.tiles = std::max(1, (p.rows + p.tile - 1) / p.tile);
   // keys that a row tile may have to visit
   const long long capacity = (long long)c.max_pages << c.page_log2;
   long long keys = attn.max_kv > 0 ? std::min<long long>(attn.max_kv, capacity) : capacity;
-  if (attn.window >= 0 && attn.causal) keys = std::min(keys, (attn.window + 1ll) * attn.block + std::min<long long>(attn.sink, keys) + p.tile / group);
+  if (attn.window >= 0 && attn.causal) keys = std::min(keys, (attn.window + 1ll) * attn.block + std::min<long long>(attn.sink, keys) + 128);
   p.reach = (int)keys;
   const long long units = (keys + kTile - 1) / kTile;
+  // More than 64 rows go to the form with 128 where there is work for the whole chip.  Times of that form over those of the one with 32 rows, both
+  // head dimensions, by tiles of 32 rows times tiles of keys (4 to 64 heads, 128 and 256 rows, 272 to 16384 keys): up to 10240 1.04-1.5, at 16384 0.98-1.35,
+  // from 32768 on 0.79-0.94.  With 33 to 64 rows, which leave it half empty, 1.03-1.4.
+  const long long work = (long long)c.B * c.H * ((p.rows + 31) / 32) * units;
+  p.tile = p.rows <= 16 ? 16 : p.rows <= 64 || work <= 16384 ? 32 : 128;
+  p.tiles = std::max(1, (p.rows + p.tile - 1) / p.tile);
   // parts for one round of workgroups, each of a few tiles at least
   const long long places = p.tile == 128 ? kv4_places(c.D) : 512, least = p.tile == 128 ? 8 : 2 * kWaves;
   const long long parts = std::min(places / ((long long)c.H * p.tiles), c.B * std::max(1ll, units / least));
@@ -937,9 +1007,10 @@ int launch_kv4_attn(const Kv4& c, const svg_kv4_attn_t& attn, const Kv4Plan& pla
     hipLaunchKernelGGL((wide ? kv4_rows_kernel<128, 1> : kv4_rows_kernel<64, 1>), dim3((unsigned)blocks), dim3(64 * kWaves), 0, stream, a);
   if (plan.parts > c.B) {
     const long long rows = (long long)c.H * plan.rows;        // of a sequence
-    const int per_block = 256 / (c.D / 4);
-    hipLaunchKernelGGL((wide ? kv4_join_kernel<128> : kv4_join_kernel<64>), dim3((unsigned)((rows + per_block - 1) / per_block), (unsigned)c.B), dim3(256),
-                       0, stream, a);
+    const bool few = rows * c.B <= 2048;
+    const int per_block = 256 / (c.D / 4) / (few ? 8 : 1);
+    auto kernel = wide ? (few ? kv4_join_kernel<128, 8> : kv4_join_kernel<128, 1>) : few ? kv4_join_kernel<64, 8> : kv4_join_kernel<64, 1>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + per_block - 1) / per_block), (unsigned)c.B), dim3(256), 0, stream, a);
   }
   return hip_status(hipGetLastError());
 }

@@ -9,6 +9,7 @@ import pytest
 import torch
 
 import paper_2502_01776_amd as S
+import kv4_plan
 from oracle import kv4_oracle as O
 
 pytestmark = pytest.mark.gpu
@@ -17,11 +18,11 @@ pytestmark = pytest.mark.gpu
 class Cache:
     """Sequences of random keys and values in pages in any order; whatever no sequence holds is 0xFF bytes (NaN scales)."""
 
-    def __init__(self, lens, H, D, page_size, seed=0, spread=1.0, spare=3, odd=None):
+    def __init__(self, lens, H, D, page_size, seed=0, spread=1.0, spare=3, odd=None, capacity=0):
         rng = np.random.default_rng(seed)
         self.lens, self.H, self.D, self.page_size = list(lens), H, D, page_size
         need = [-(-n // page_size) for n in lens]
-        self.pages, self.max_pages = sum(need) + spare, max(need + [1])
+        self.pages, self.max_pages = sum(need) + spare, max(need + [1, -(-capacity // page_size)])
         order = rng.permutation(self.pages)
         self.table = np.full((len(lens), self.max_pages), -1)
         data = np.full((self.pages, H, O.record_bytes(D, page_size)), 0xFF, dtype=np.uint8)
@@ -75,10 +76,11 @@ def run(cache, q, kv_len=None, q_len=None, max_kv=0, scale=0.0, out=None, fill=7
     return o, lse
 
 
-def check(cache, q, kv_len=None, q_len=None, max_kv=0, scale=0.0, rows=None, **mask):
-    """rows: the queries that the oracle computes (all where None)."""
+def check(cache, q, kv_len=None, q_len=None, max_kv=0, scale=0.0, rows=None, heads=None, **mask):
+    """rows, heads: the queries and their heads that the oracle computes (all where None)."""
     o, lse = run(cache, q, kv_len, q_len, max_kv, scale, **mask)
     B, H, N, D = q.shape
+    heads = list(range(H)) if heads is None else heads
     for b in range(B):
         n = cache.lens[b] if kv_len is None else kv_len[b]
         n = max(0, min(n, cache.max_pages * cache.page_size))
@@ -90,15 +92,17 @@ def check(cache, q, kv_len=None, q_len=None, max_kv=0, scale=0.0, rows=None, **m
         wanted = range(q_n) if rows is None else [i for i in rows if i < q_n]
         for i in wanted:
             see = np.nonzero(O.seen(n, q_n, i, mask.get("block", 1), mask.get("causal", False), mask.get("window", -1), mask.get("sink", 0)) & exists)[0]
-            got, got_lse = o[b, :, i].double().cpu().numpy(), lse[b, :, i].double().cpu().numpy()
+            got, got_lse = o[b, heads, i].double().cpu().numpy(), lse[b, heads, i].double().cpu().numpy()
             if not len(see):
                 assert (got == 0).all() and np.isneginf(got_lse).all(), (b, i)
                 continue
             one = np.ones(len(see), dtype=bool)
-            ref, ref_lse, size, slack = O.attention(q[b, :, i:i + 1].double().cpu().numpy(), k[see], v[see], one, scale or D ** -0.5)
+            group = H // cache.H
+            own = [h // group for h in heads]                            # a head of the cache for each: the oracle's heads are not shared
+            ref, ref_lse, size, slack = O.attention(q[b, heads, i:i + 1].double().cpu().numpy(), k[see][:, own], v[see][:, own], one, scale or D ** -0.5)
             e = (D + 8 + 1.4427) * 2.0 ** -23 * slack + 2.0 ** -21
             sums = (len(see) / 32 + 64) * 2.0 ** -23
-            tol = 2.0 ** -8 * np.abs(ref[:, 0]) + (2.0 ** -8 + 2 * e + sums) * size[:, 0] * (1 + 2.0 ** -7) + len(see) * 2.0 ** -126 * np.abs(v[see]).max()
+            tol = 2.0 ** -8 * np.abs(ref[:, 0]) + (2.0 ** -8 + 2 * e + sums) * size[:, 0] * (1 + 2.0 ** -7) + len(see) * 2.0 ** -126 * np.abs(v[see][:, own]).max()
             bad = np.abs(got - ref[:, 0]) > tol
             assert not bad.any(), (b, i, float((np.abs(got - ref[:, 0]) / tol).max()))
             tol = e[:, 0] + sums + 2.0 ** -22 * np.abs(ref_lse[:, 0])
@@ -107,21 +111,49 @@ def check(cache, q, kv_len=None, q_len=None, max_kv=0, scale=0.0, rows=None, **m
     return o, lse
 
 
+# Cases of few sequences and short caches take the form whose wavefronts split the keys; the page tables of the others could hold so many keys that the
+# form with 128 rows is taken (its parts are then many and short, some of them empty), or have so many heads.
+LONG = 1 << 18
+
+
+def tile(cache, q, **kw):
+    return kv4_plan.plan(cache.desc(), S.kv4_attn(kv_len=i32(cache.lens), **kw), q.shape[2], q.shape[1] // cache.H).tile
+
+
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("N", [1, 3, 16, 17, 31, 33, 129, 200])
-def test_lengths_of_queries_and_keys(N, D):
+@pytest.mark.parametrize("capacity", [0, LONG])
+def test_lengths_of_queries_and_keys(capacity, N, D):
     lens = [1, 15, 16, 17, 63, 64, 65, 200, 517]
-    cache = Cache(lens, 2, D, 16, seed=N)
+    cache = Cache(lens, 2, D, 16, seed=N, capacity=capacity)
     q = queries(len(lens), 2, N, D, "heads", N)
+    assert tile(cache, q) == (16 if N <= 16 else 128 if capacity and N > 64 else 32)
     check(cache, q, rows=range(0, N, 1 if N < 20 else 13))                # queries without a token of their own among them
     check(cache, q, rows=range(0, N, 1 if N < 20 else 13), causal=True)
 
 
-@pytest.mark.parametrize("N", [1, 40])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("B, group", [(1, 1), (3, 1), (70, 1), (1, 3)])
+def test_form_with_128_rows_in_one_part(B, group, D):
+    """So many heads that no sequence is cut: results straight from the registers."""
+    H = 384 // group // min(B, 24)
+    rng = np.random.default_rng(B)
+    lens = [960] + [int(x) for x in rng.integers(1, 961, B - 1)]
+    cache = Cache(lens, H, D, 32, seed=B)
+    N = 210
+    q = queries(B, H * group, N, D, "packed", B)
+    q_len = [N] + [int(x) for x in rng.integers(0, N + 1, B - 1)]
+    for mask in (dict(causal=True), dict(causal=True, block=100, window=2, sink=70), dict()):
+        p = kv4_plan.plan(cache.desc(), S.kv4_attn(kv_len=i32(lens), q_len=i32(q_len), **mask), N, group)
+        assert p.tile == 128 and p.parts == B
+        check(cache, q, q_len=q_len, rows=range(0, N, 41), heads=[0, H * group // 2, H * group - 1], **mask)
+
+
+@pytest.mark.parametrize("N, capacity", [(1, 0), (40, 0), (71, LONG)])
 @pytest.mark.parametrize("layout", ["packed", "odd"])
 @pytest.mark.parametrize("group, D, page_size", [(1, 64, 32), (3, 128, 64), (4, 64, 16), (7, 128, 16), (16, 64, 256)])
-def test_shared_heads_and_layouts(group, D, page_size, layout, N):
-    cache = Cache([300, 77], 2, D, page_size, seed=group)
+def test_shared_heads_and_layouts(group, D, page_size, layout, N, capacity):
+    cache = Cache([300, 77], 2, D, page_size, seed=group, capacity=capacity)
     q = queries(2, 2 * group, N, D, layout, group)
     check(cache, q, rows=range(0, N, 7), causal=True)
     check(cache, q, rows=range(0, N, 13), scale=0.31)
@@ -132,16 +164,17 @@ def test_shared_heads_and_layouts(group, D, page_size, layout, N):
                                                         (50, 2, 64, True), (37, 0, 5, False), (37, 3, 0, False), (1000, 1, 70, True), (7, 0, 0, True)])
 def test_masks(block, window, sink, causal, D):
     cache = Cache([400, 131, 9], 1, D, 16, seed=block)
-    for N in (1, 9, 24, 150):
+    large = Cache([400, 131, 9], 1, D, 16, seed=block, capacity=8 * LONG)
+    for N, cache in ((1, cache), (9, cache), (24, cache), (150, cache), (150, large)):
         q = queries(3, 1, N, D, "heads", N)
         check(cache, q, rows=range(0, N, 1 if N < 10 else 7), block=block, window=window, sink=sink, causal=causal)
     q = queries(3, 1, 150, D, "heads", 3)
     check(cache, q, q_len=[150, 20, 0], rows=range(0, 150, 7), block=block, window=window, sink=sink, causal=causal)
 
 
-@pytest.mark.parametrize("N", [1, 2, 100])
-def test_pages_that_are_not_there(N):
-    cache = Cache([500, 300, 64], 2, 64, 16, seed=9)
+@pytest.mark.parametrize("N, capacity", [(1, 0), (2, 0), (100, 0), (100, LONG)])
+def test_pages_that_are_not_there(N, capacity):
+    cache = Cache([500, 300, 64], 2, 64, 16, seed=9, capacity=capacity)
     cache.table[0, [0, 3, 4, 5, 6, 20]] = [-1, -1, -1, cache.pages, 2 ** 30, -1]
     cache.table[1, :] = -1                                                # nothing at all
     cache.table[2, 3] = -5
@@ -151,10 +184,10 @@ def test_pages_that_are_not_there(N):
     check(cache, q, rows=range(0, N, 9), causal=True, block=16, window=3, sink=16)
 
 
-@pytest.mark.parametrize("N", [1, 20, 300])
-def test_lengths_of_the_call(N):
+@pytest.mark.parametrize("N, capacity", [(1, 0), (20, 0), (300, 0), (300, LONG)])
+def test_lengths_of_the_call(N, capacity):
     """Empty sequences and query lists, lengths out of range (cut off), no more keys than the hint says."""
-    cache = Cache([200, 90, 40, 130], 2, 128, 32, seed=2)
+    cache = Cache([200, 90, 40, 130], 2, 128, 32, seed=2, capacity=capacity)
     q = queries(4, 2, N, 128, "heads", 2)
     check(cache, q, kv_len=[0, 90, -5, 129], q_len=[N, 0, N, -1], rows=range(0, N, 17))
     check(cache, q, kv_len=[0, 1, 40, 2], q_len=[N, N + 100, 1, 2], rows=range(0, N, 17), causal=True)
@@ -165,23 +198,23 @@ def test_lengths_of_the_call(N):
 
 
 @pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("N", [1, 32, 128])
-def test_sharp_rows(N, D):
+@pytest.mark.parametrize("N, capacity", [(1, 0), (32, 0), (128, 0), (128, 8 * LONG)])
+def test_sharp_rows(N, capacity, D):
     """Scores of +-60 and more: the reference maximum moves again and again, most weights are zero."""
     def grow(b, k, v):
         k *= np.linspace(0.1, 3, len(k))[:, None, None]
-    cache = Cache([700], 1, D, 64, seed=4, spread=2.0, odd=grow)
+    cache = Cache([700], 1, D, 64, seed=4, spread=2.0, odd=grow, capacity=capacity)
     q = queries(1, 1, N, D, "heads", 4, scale=6.0)
     check(cache, q, rows=range(0, N, 5))
-    down = Cache([700], 1, D, 64, seed=4, spread=2.0, odd=lambda b, k, v: k.__imul__(np.linspace(3, 0.01, len(k))[:, None, None]))
+    down = Cache([700], 1, D, 64, seed=4, spread=2.0, odd=lambda b, k, v: k.__imul__(np.linspace(3, 0.01, len(k))[:, None, None]), capacity=capacity)
     check(down, q, rows=range(0, N, 5), causal=True)
 
 
-@pytest.mark.parametrize("N", [1, 3, 60, 140])
+@pytest.mark.parametrize("N, capacity", [(1, 0), (3, 0), (60, 0), (140, 0), (140, LONG)])
 @pytest.mark.parametrize("D", [64, 128])
-def test_values_that_are_not_finite(N, D):
+def test_values_that_are_not_finite(N, capacity, D):
     """They spoil the results of the queries that see them, in their 32 channels (values) or whole (keys), and nothing else, bit for bit."""
-    plain = Cache([333, 200], 2, D, 16, seed=6)
+    plain = Cache([333, 200], 2, D, 16, seed=6, capacity=capacity)
     at = 333 - N // 2 - 1                                                # the queries behind it see it, those in front do not
 
     def odd(b, k, v):
@@ -189,7 +222,7 @@ def test_values_that_are_not_finite(N, D):
             v[at, 1, 33], v[at, 0, 5] = np.inf, np.nan
         else:
             k[150, 0, 7] = np.nan
-    spoilt = Cache([333, 200], 2, D, 16, seed=6, odd=odd)
+    spoilt = Cache([333, 200], 2, D, 16, seed=6, odd=odd, capacity=capacity)
     q = queries(2, 2, N, D, "heads", 6)
     for mask in (dict(), dict(causal=True), dict(causal=True, window=100, sink=2)):
         want, want_lse = run(plain, q, **mask)
@@ -209,14 +242,14 @@ def test_values_that_are_not_finite(N, D):
         assert torch.equal(got_lse[0], want_lse[0])
 
 
-@pytest.mark.parametrize("N, H, D", [(1, 2, 128), (1, 1, 64), (30, 1, 128), (130, 1, 64), (130, 2, 128)])
+@pytest.mark.parametrize("N, H, D", [(1, 2, 128), (1, 1, 64), (30, 1, 128), (130, 1, 64), (130, 2, 128), (2100, 2, 64), (2100, 2, 128)])
 def test_long_caches_in_parts(N, H, D):
     """Few workgroups: the keys are cut into parts; the hint changes the cut, and with it the rounding only."""
     lens = [9001, 70]
     cache = Cache(lens, H, D, 64, seed=8)
     q = queries(2, H, N, D, "heads", 8)
     assert S.svg_kv4_attn_workspace_bytes(cache.desc(), S.kv4_attn(kv_len=i32(lens)), S.tokens_of(q)) > 0
-    rows = range(0, N, 43)
+    rows = range(0, N, 43 if N < 1000 else 517)
     a, _ = check(cache, q, rows=rows, causal=True)
     b, _ = check(cache, q, rows=rows, causal=True, max_kv=9001)
     c, _ = check(cache, q, rows=rows, causal=True, max_kv=64)               # a hint that is too low costs time, nothing else
