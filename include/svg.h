@@ -595,7 +595,7 @@ int svg_kv4_read(const svg_kv4_t* cache, const int64_t* slots, const svg_tokens_
  * A query that sees nothing has the result 0 and the log-sum-exp -inf.
  */
 typedef struct svg_kv4_attn {
-  float softmax_scale;              /* <= 0 selects 1/sqrt(D) */
+  float softmax_scale;              /* <= 0 selects 1/sqrt(D); otherwise 1e-30 .. 1e30 */
   int32_t causal;                   /* 0 or 1 */
   int32_t block;                    /* >= 1 */
   int32_t window;                   /* blocks before its own that a query sees; < 0: all */

@@ -453,17 +453,26 @@ def svg_fp4_linear_rows(x_tokens, x, in_activation, N, w, w_scales, bias, activa
 
 # ---- a cache of keys and values in 4 bits ---------------------------------------------------------
 
-def _whole(x, kind, name):
-    """Address of a tensor of whole numbers, which the device reads as they lie."""
-    if isinstance(x, torch.Tensor) and (x.dtype != kind or not x.is_contiguous()):
+def _whole(x, kind, name, count=None):
+    """Address of a tensor of whole numbers, which the device reads as they lie; count: how many there have to be."""
+    if not isinstance(x, torch.Tensor):
+        return _ptr(x)
+    if x.dtype is not kind or not x.is_contiguous():
         raise ValueError(f"{name} has to be a contiguous tensor of {kind}")
-    return _ptr(x)
+    if count is not None and x.numel() != count:
+        raise ValueError(f"{name} has to have {count} elements, not {x.numel()}")
+    return x.data_ptr()
 
 
 def kv4_cache(sequences, pages, max_pages, heads, head_dim, page_size, data=None, page_table=None) -> SvgKv4:
     """The descriptor of a cache: `pages` pages of `page_size` tokens, `max_pages` entries in a row of the page table.  The caller keeps
     data (uint8, svg_kv4_bytes) and page_table (int32 [sequences, max_pages]) alive."""
-    return SvgKv4(sequences, heads, head_dim, page_size, pages, max_pages, 0, _ptr(data), _whole(page_table, torch.int32, "page_table"))
+    if isinstance(data, torch.Tensor):
+        need = pages * heads * page_size * (head_dim + head_dim // 16)
+        if not data.is_contiguous() or data.numel() * data.element_size() < need:
+            raise ValueError(f"a cache of this size has {need} bytes in one run")
+    return SvgKv4(sequences, heads, head_dim, page_size, pages, max_pages, 0, _ptr(data),
+                  _whole(page_table, torch.int32, "page_table", sequences * max_pages))
 
 
 def kv4_attn(kv_len, q_len=None, max_kv=0, causal=False, block=1, window=-1, sink=0, softmax_scale=0.0) -> SvgKv4Attn:
@@ -477,22 +486,22 @@ def svg_kv4_bytes(cache) -> int:
 
 
 def svg_kv4_resize(cache, lengths, wanted, free_pages, free_count, new_lengths, new_count, slots, tokens, status, stream=None):
-    i32 = torch.int32
-    _check(lib().svg_kv4_resize(C.byref(cache), _whole(lengths, i32, "lengths"), _whole(wanted, i32, "wanted"),
-                                _whole(free_pages, i32, "free_pages"), _whole(free_count, i32, "free_count"),
-                                _whole(new_lengths, i32, "new_lengths"), _whole(new_count, i32, "new_count"),
-                                _whole(slots, torch.int64, "slots"), int(tokens), _whole(status, i32, "status"), _stream(stream)),
-           "svg_kv4_resize")
+    i32, n = torch.int32, cache.B
+    _check(lib().svg_kv4_resize(C.byref(cache), _whole(lengths, i32, "lengths", n), _whole(wanted, i32, "wanted", n),
+                                _whole(free_pages, i32, "free_pages", cache.pages), _whole(free_count, i32, "free_count", 1),
+                                _whole(new_lengths, i32, "new_lengths", n), _whole(new_count, i32, "new_count", 1),
+                                _whole(slots, torch.int64, "slots", n * tokens), int(tokens), _whole(status, i32, "status", 1),
+                                _stream(stream)), "svg_kv4_resize")
 
 
 def svg_kv4_write(cache, k_tokens, k, v_tokens, v, slots, stream=None):
     _check(lib().svg_kv4_write(C.byref(cache), C.byref(k_tokens), _ptr(k), C.byref(v_tokens), _ptr(v),
-                               _whole(slots, torch.int64, "slots"), _stream(stream)), "svg_kv4_write")
+                               _whole(slots, torch.int64, "slots", k_tokens.B * k_tokens.N), _stream(stream)), "svg_kv4_write")
 
 
 def svg_kv4_read(cache, slots, k_tokens, k, v_tokens, v, stream=None):
-    _check(lib().svg_kv4_read(C.byref(cache), _whole(slots, torch.int64, "slots"), C.byref(k_tokens), _ptr(k), C.byref(v_tokens), _ptr(v),
-                              _stream(stream)), "svg_kv4_read")
+    _check(lib().svg_kv4_read(C.byref(cache), _whole(slots, torch.int64, "slots", k_tokens.B * k_tokens.N), C.byref(k_tokens), _ptr(k),
+                              C.byref(v_tokens), _ptr(v), _stream(stream)), "svg_kv4_read")
 
 
 def svg_kv4_attn_workspace_bytes(cache, attn, q_tokens) -> int:

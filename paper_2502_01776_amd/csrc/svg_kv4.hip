@@ -224,7 +224,7 @@ template <int D, int KT, int VT>
 __global__ __launch_bounds__(kThreads) void write_kernel(RowsArgs a) {
   constexpr int LANES = D / 8, ROWS = kThreads / LANES;
   const int c = threadIdx.x % LANES;
-  const unsigned u0 = blockIdx.x * (ROWS * kRowsEach) + threadIdx.x / LANES;
+  const unsigned u0 = (blockIdx.y * gridDim.x + blockIdx.x) * (ROWS * kRowsEach) + threadIdx.x / LANES;
   RowPlace at[kRowsEach];
   float k[kRowsEach][8] = {}, v[kRowsEach][8] = {};
 #pragma unroll
@@ -275,7 +275,7 @@ template <int D, int KT, int VT>
 __global__ __launch_bounds__(kThreads) void read_kernel(RowsArgs a, void* kp, void* vp) {
   constexpr int LANES = D / 8, ROWS = kThreads / LANES;
   const int c = threadIdx.x % LANES;
-  const unsigned u0 = blockIdx.x * (ROWS * kRowsEach) + threadIdx.x / LANES;
+  const unsigned u0 = (blockIdx.y * gridDim.x + blockIdx.x) * (ROWS * kRowsEach) + threadIdx.x / LANES;
   RowPlace at[kRowsEach];
   unsigned kc[kRowsEach] = {}, vc[kRowsEach] = {};
   unsigned char ks[kRowsEach] = {}, vs[kRowsEach] = {};
@@ -320,12 +320,13 @@ int launch_rows(const Kv4& c, const HeadRows& k, const HeadRows& v, const int64_
   // from the layout that lies in memory: heads of a token side by side, or tokens of a head
   a.heads_inner = k.sh <= k.sn;
   const int per_block = kThreads / (c.D / 8) * kRowsEach;
-  // as many heads to a launch as 32-bit numbers of rows allow
   const long long all = rows * c.H;
-  if (all > 0xfff00000ll) return SVG_ERR_UNSUPPORTED;
+  if (all > 0xfff00000ll) return SVG_ERR_UNSUPPORTED;          // (rows are counted in 32 bits, those of the last workgroups too)
   a.units = (unsigned)all;
   (void)hipGetLastError();
-  go(a, dim3((unsigned)((all + per_block - 1) / per_block)));
+  // a launch has fewer than 2^32 threads in one dimension
+  const long long blocks = (all + per_block - 1) / per_block, wide = std::min(blocks, 1ll << 23);
+  go(a, dim3((unsigned)wide, (unsigned)((blocks + wide - 1) / wide)));
   return hip_status(hipGetLastError());
 }
 

@@ -29,7 +29,7 @@ int check_heads(const svg_tokens_t* d, bool output, int D, svg::HeadRows* h, int
   const int rc = check_tokens(d, output, &t, rows, &cols, &bytes);
   if (rc != SVG_OK) return rc;
   if (d->D != D && (d->H != 1 || d->D % D)) return SVG_ERR_INVALID_ARG;
-  if (!p || misaligned(p, svg::type_bytes(t.type))) return SVG_ERR_INVALID_ARG;
+  if ((!p && *rows) || misaligned(p, svg::type_bytes(t.type))) return SVG_ERR_INVALID_ARG;      // (an empty tensor has no address)
   *heads = (int)(cols / D);
   *h = svg::HeadRows{t.N, t.sb, t.sn, d->D == D ? t.sh : D, t.type};
   // rows one step apart whose heads lie between one and the next are column slices; anything else is taken as one run
@@ -57,7 +57,7 @@ int check_kv(const svg_kv4_t* cache, bool output, const svg_tokens_t* k_desc, co
   if ((rc = check_heads(k_desc, output, a->c.D, &a->k, &k_heads, &a->rows, &a->where_k, k)) != SVG_OK) return rc;
   if ((rc = check_heads(v_desc, output, a->c.D, &a->v, &v_heads, &v_rows, &a->where_v, v)) != SVG_OK) return rc;
   if (k_heads != a->c.H || v_heads != a->c.H || k_desc->B != v_desc->B || k_desc->N != v_desc->N) return SVG_ERR_INVALID_ARG;
-  if (!slots || misaligned(slots, 8) || (!a->c.data && a->c.pages) || svg::misaligned16(a->c.data)) return SVG_ERR_INVALID_ARG;
+  if ((!slots && a->rows) || misaligned(slots, 8) || (!a->c.data && a->c.pages) || svg::misaligned16(a->c.data)) return SVG_ERR_INVALID_ARG;
   return SVG_OK;
 }
 
@@ -72,7 +72,8 @@ int check_attn(const svg_kv4_t* cache, const svg_kv4_attn_t* attn, const svg_tok
   int rc = check_cache(cache, &a->c);
   if (rc != SVG_OK) return rc;
   if (!attn || (attn->causal != 0 && attn->causal != 1) || attn->block < 1 || attn->sink < 0 || attn->max_kv < 0) return SVG_ERR_INVALID_ARG;
-  if (!(attn->softmax_scale == attn->softmax_scale) || attn->softmax_scale > 1.0e30f) return SVG_ERR_INVALID_ARG;
+  // (a scale that is not a normal number beside the scores' would make 0 infinity of a masked one)
+  if (!(attn->softmax_scale <= 0.f || (attn->softmax_scale >= 1.0e-30f && attn->softmax_scale <= 1.0e30f))) return SVG_ERR_INVALID_ARG;
   if (!places_fit(a->c)) return SVG_ERR_UNSUPPORTED;
   long long rows;
   if ((rc = check_heads(q_desc, false, a->c.D, &a->q, &a->heads, &rows, &a->where_q, q)) != SVG_OK) return rc;
@@ -190,7 +191,7 @@ int svg_fp4_linear_rows(const svg_tokens_t* x_desc, const void* x, int in_activa
   if (rc != SVG_OK) return rc;
   if ((rc = check_tokens(out_desc, true, &ot, &rows, &cols, &out_bytes)) != SVG_OK) return rc;
   if (!activation_kind(in_activation) || !activation_kind(activation) || N < 1 || rows != M || cols != N) return SVG_ERR_INVALID_ARG;
-  if (!x || !out || !w || !w_scales || misaligned(x, svg::type_bytes(xt.type)) || misaligned(out, svg::type_bytes(ot.type)))
+  if ((M && (!x || !out)) || !w || !w_scales || misaligned(x, svg::type_bytes(xt.type)) || misaligned(out, svg::type_bytes(ot.type)))
     return SVG_ERR_INVALID_ARG;
   if (svg::misaligned16(w) || svg::misaligned16(w_scales) || misaligned(bias, 4)) return SVG_ERR_INVALID_ARG;
   if (M > 1024) return SVG_ERR_UNSUPPORTED;

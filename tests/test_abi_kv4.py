@@ -4,6 +4,7 @@ import ctypes as C
 import pytest
 import torch
 
+import kv4_plan
 import paper_2502_01776_amd as S
 
 A = 0x10000000                                                        # addresses that are never read
@@ -70,7 +71,7 @@ def test_rows_into_and_out_of_pages():
         assert call(c, kt=tokens(D=64)) == -1 and call(c, kt=tokens(H=1, D=500)) == -1 and call(c, kt=tokens(type=3)) == -1
         assert call(c, kt=tokens(B=1, N=20)) == -1                    # as many rows, but not the same batch
         assert call(c, k=DATA + 64) == -4 and call(c, v=DATA - 64) == -4
-        assert call(c, kt=tokens(N=0), vt=tokens(N=0)) == 0 and call(cache(pages=0, data=None)) == 0
+        assert call(c, kt=tokens(N=0), vt=tokens(N=0), k=None, v=None, slots=None) == 0 and call(cache(pages=0, data=None)) == 0
     assert write(c, slots=DATA + 8) == -4                             # (a read may look its slots up there)
     assert read(c, v=K) == -4 and read(c, k=SLOTS) == -4 and read(c, v=V, k=V + 256) == -4
     assert read(c, kt=tokens(stride_n=64)) == -4                      # rows of an output that share places
@@ -113,7 +114,7 @@ def test_attention():
     c = cache()
     assert attn(None) == -1 and attn(c, q=None) == -1 and attn(c, o=None) == -1 and attn(c, kv_len=None) == -1
     assert S.lib().svg_kv4_attn_fwd(ref(c), None, ref(tokens()), Q, ref(tokens()), O, LSE, WS, 1 << 40, None) == -1
-    for bad in (dict(block=0), dict(sink=-1), dict(max_kv=-1), dict(softmax_scale=float("nan")), dict(softmax_scale=float("inf")),
+    for bad in (dict(block=0), dict(sink=-1), dict(max_kv=-1), dict(softmax_scale=float("nan")), dict(softmax_scale=float("inf")), dict(softmax_scale=1e-31), dict(softmax_scale=2e30),
                 dict(kv_len=LEN + 2), dict(q_len=QLEN + 1)):
         assert attn(c, **bad) == -1, bad
     d = S.kv4_attn(kv_len=LEN)
@@ -130,7 +131,7 @@ def test_attention():
     for out in ("o", "lse", "ws"):
         for at in (Q, DATA, TABLE, LEN, QLEN, *(x for n, x in (("o", O), ("lse", LSE), ("ws", WS)) if n != out)):
             assert attn(long, **{out: at}) == -4, (out, hex(at))
-    assert attn(c, qt=tokens(N=0), ot=tokens(N=0)) == 0 and attn(cache(sequences=0), qt=tokens(B=0), ot=tokens(B=0)) == 0
+    assert attn(c, qt=tokens(N=0), ot=tokens(N=0), q=None, o=None) == 0 and attn(cache(sequences=0), qt=tokens(B=0), ot=tokens(B=0)) == 0
 
 
 def workspace(c, N=10, H=4, **kw):
@@ -160,12 +161,12 @@ def test_few_rows():
     assert rows(act=3) == -1 and rows(out_act=-1) == -1 and rows(N=0) == -1 and rows(N=255) == -1
     assert rows(xt=flat(5, 512)) == -1 and rows(xt=flat(4, 512, type=5)) == -1
     assert rows(xt=flat(1025, 512), ot=flat(1025, 256)) == -2
-    assert rows(xt=flat(0, 512), ot=flat(0, 256)) == 0
+    assert rows(xt=flat(0, 512), ot=flat(0, 256), x=None, out=None) == 0
     for at in (K, DATA, TABLE, V):
         assert rows(out=at) == -4, hex(at)
 
 
-def test_whole_numbers_of_other_types_are_refused():
+def test_whole_numbers_of_other_types_and_sizes_are_refused():
     wrong, right = torch.zeros(2, dtype=torch.int64), torch.zeros(2, dtype=torch.int32)
     with pytest.raises(ValueError, match="kv_len"):
         S.kv4_attn(kv_len=wrong)
@@ -173,7 +174,45 @@ def test_whole_numbers_of_other_types_are_refused():
         S.kv4_attn(kv_len=right, q_len=torch.zeros(4, dtype=torch.int32)[::2])
     with pytest.raises(ValueError, match="page_table"):
         cache(page_table=torch.zeros(2, 8, dtype=torch.int64))
-    with pytest.raises(ValueError, match="slots"):
-        S.svg_kv4_write(cache(), tokens(), K, tokens(), V, right, stream=0)
-    with pytest.raises(ValueError, match="wanted"):
-        S.svg_kv4_resize(cache(), right, wrong, right, right, right, right, None, 0, right, stream=0)
+    with pytest.raises(ValueError, match="page_table"):
+        cache(page_table=torch.zeros(2, 7, dtype=torch.int32))
+    for call in (lambda s: S.svg_kv4_write(cache(), tokens(), K, tokens(), V, s, stream=0), lambda s: S.svg_kv4_read(cache(), s, tokens(), K, tokens(), V, stream=0)):
+        for slots in (right, torch.zeros(19, dtype=torch.int64)):
+            with pytest.raises(ValueError, match="slots"):
+                call(slots)
+    good = dict(lengths=right, wanted=right, free_pages=torch.zeros(40, dtype=torch.int32), free_count=right[:1], new_lengths=right.clone(),
+                new_count=right[1:], slots=torch.zeros(6, dtype=torch.int64), tokens=3, status=torch.zeros(1, dtype=torch.int32))
+    for name in good:
+        if name != "tokens":
+            with pytest.raises(ValueError, match=name):
+                S.svg_kv4_resize(cache(), **{**good, name: torch.zeros(5, dtype=good[name].dtype)}, stream=0)
+
+
+def test_a_pool_that_is_too_small_is_refused():
+    need = S.svg_kv4_bytes(cache())
+    assert cache(data=torch.zeros(need, dtype=torch.uint8)).data
+    with pytest.raises(ValueError, match="bytes"):
+        cache(data=torch.zeros(need - 1, dtype=torch.uint8))
+
+
+def test_how_a_call_is_cut():
+    """At most a round of workgroups in parts, one part at least for each sequence, and the workspace that they take."""
+    def plan(N=10, group=1, B=2, H=4, D=128, keys=32768, **kw):
+        c = cache(sequences=B, heads=H, head_dim=D, max_pages=keys // 64)
+        a = S.kv4_attn(kv_len=LEN, **kw)
+        p = kv4_plan.plan(c, a, N, group)
+        q = tokens(B=B, H=H * group, N=N, D=D)
+        assert S.svg_kv4_attn_workspace_bytes(c, a, q) == (p.parts * H * N * group * (4 * D + 8) if p.parts > B else 0)
+        assert p.rows == N * group and p.tiles == -(-p.rows // p.tile) and p.parts >= B and (B <= 64 or p.parts % B == 0)
+        assert p.parts == B or p.parts * H * p.tiles <= (768 if p.tile == 128 and D == 64 else 512)
+        return p
+    assert [plan(N=n).tile for n in (1, 16, 17, 32, 33, 64, 65)] == [16, 16, 32, 32, 32, 32, 32] and plan(N=1000).tile == 128
+    assert plan(N=1, group=17).tile == 32 and plan(N=70, keys=512).tile == 32 and plan(N=70, H=100).tile == 128
+    assert plan(N=1).parts == 128 and plan(N=1, keys=64).parts == 2 and plan(N=1, max_kv=1024).parts == 4
+    assert plan(N=1, B=70).parts == 70 and plan(N=1, B=70, H=1).parts == 490 and plan(N=4000, H=40).parts == 2
+    assert plan(N=1, causal=True, block=64, window=3, sink=0).reach == 4 * 64 + 128 and plan(N=1, block=64, window=3).reach == 32768
+    for H in (1, 3, 40):
+        for N in (1, 30, 100, 5000):
+            for B in (1, 7, 64, 65, 600):
+                for D in (64, 128):
+                    plan(N=N, B=B, H=H, D=D)
