@@ -1,5 +1,6 @@
 // The 4-bit cache of keys and values: page tables and slots from the lengths, rows into the pages and out of them.
 #include <algorithm>
+#include <limits>
 #include <type_traits>
 
 #include "svg_kv4.h"
@@ -17,11 +18,14 @@ constexpr int kThreads = 256;
 // stack[count + R_b + j - want_b], and page j it takes is stack[count + R - 1 - (G_b + j - have_b)]: below `count` the stack's own entry,
 // from there on a page that some sequence gives back in the same call, found without the stack, so that nothing waits for another workgroup.
 //
-// A workgroup takes one sequence's tokens (kTokens of them at a time) and sums over all sequences by itself: 8 bytes a sequence out of L2
+// A workgroup takes kTokens of one sequence's tokens and sums over all sequences by itself: 8 bytes a sequence out of L2
 // instead of a launch in front.  The state (lengths, count) is written by the first workgroup, or by a launch of its own where it
 // lies where others still read it.  Bound: latency of a launch and of three dependent trips to memory; the slots' bytes for many tokens.
 
-constexpr int kTokens = 2048;
+// kTokens is 512 as long as all workgroups are on the card at once (200 sequences of up to 1560 tokens: 7.8 us, with 2048 8.6), else 2048:
+// more workgroups would only repeat the sums.
+
+constexpr int kTokens = 512, kTokensMany = 2048, kTogether = 8 * 256;
 
 struct ResizeArgs {
   Kv4Resize r;
@@ -51,43 +55,44 @@ struct Totals {
   int count;
 };
 
-// Sums over all threads of the workgroup, in all of them.
-__device__ __forceinline__ long long block_sum(long long x, long long* shared) {
-#pragma unroll
-  for (int m = 32; m > 0; m >>= 1) x += __shfl_xor(x, m, 64);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = x;
-  __syncthreads();
-  long long s = 0;
-#pragma unroll
-  for (int w = 0; w < kThreads / 64; ++w) s += shared[w];
-  return s;
-}
+// The sums that a call's totals are made of.
+struct Sums {
+  long long all_r, all_g, front_r, front_g;
+  int bad;
+};
 
-__device__ __forceinline__ Totals totals(const ResizeArgs& a, int b, long long* shared) {
-  // two sums to a number: a sequence's pages are at most 2^26, the sequences 2^16
-  long long all_r = 0, all_g = 0, bad = 0, front_r = 0, front_g = 0;
+__device__ __forceinline__ Totals totals(const ResizeArgs& a, int b, Sums* shared) {
+  Sums t = {};
   const int count = *a.r.free_count;
   for (int s = threadIdx.x; s < a.B; s += kThreads) {
     const Sequence q(a, s);
-    bad |= q.bad;
-    all_r += q.back();
-    all_g += q.take();
-    front_r += s < b ? q.back() : 0;
-    front_g += s < b ? q.take() : 0;
+    t.bad |= q.bad;
+    t.all_r += q.back();
+    t.all_g += q.take();
+    t.front_r += s < b ? q.back() : 0;
+    t.front_g += s < b ? q.take() : 0;
   }
-  Totals t;
-  t.count = count;
-  t.R = block_sum(all_r, shared);
-  t.G = block_sum(all_g, shared);
-  t.R_b = t.G_b = 0;
-  if (b > 0) {
-    t.R_b = block_sum(front_r, shared);
-    t.G_b = block_sum(front_g, shared);
+#pragma unroll
+  for (int m = 32; m > 0; m >>= 1) {
+    t.all_r += __shfl_xor(t.all_r, m, 64);
+    t.all_g += __shfl_xor(t.all_g, m, 64);
+    t.front_r += __shfl_xor(t.front_r, m, 64);
+    t.front_g += __shfl_xor(t.front_g, m, 64);
+    t.bad |= __shfl_xor(t.bad, m, 64);
   }
-  const bool wrong = block_sum(bad, shared) != 0 || count < 0 || count > a.pages || count + t.R > a.pages;
-  t.status = wrong ? SVG_KV4_LENGTHS : t.G > count + t.R ? SVG_KV4_FULL : SVG_KV4_OK;
-  return t;
+  if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = t;
+  __syncthreads();
+  t = shared[0];
+#pragma unroll
+  for (int w = 1; w < kThreads / 64; ++w) {
+    t.all_r += shared[w].all_r;
+    t.all_g += shared[w].all_g;
+    t.front_r += shared[w].front_r;
+    t.front_g += shared[w].front_g;
+    t.bad |= shared[w].bad;
+  }
+  const bool wrong = t.bad || count < 0 || count > a.pages || count + t.all_r > a.pages;
+  return {t.all_r, t.all_g, t.front_r, t.front_g, wrong ? SVG_KV4_LENGTHS : t.all_g > count + t.all_r ? SVG_KV4_FULL : SVG_KV4_OK, count};
 }
 
 __device__ __forceinline__ void write_state(const ResizeArgs& a, const Totals& t) {
@@ -99,12 +104,11 @@ __device__ __forceinline__ void write_state(const ResizeArgs& a, const Totals& t
 }
 
 __global__ __launch_bounds__(kThreads) void resize_kernel(ResizeArgs a) {
-  __shared__ long long shared[kThreads / 64];
-  __shared__ long long running[2];
+  __shared__ Sums shared[kThreads / 64];
+  __shared__ long long sums[kThreads / 64], running;
   const int b = blockIdx.x, part = blockIdx.y;
-  const Totals t = totals(a, b, shared);
   const Sequence own(a, b);
-  __syncthreads();                                       // every length has been read
+  const Totals t = totals(a, b, shared);                 // (its barrier stands behind every read of the lengths)
   if (a.state && b == 0 && part == 0) write_state(a, t);
   const bool ok = t.status == SVG_KV4_OK;
   // tokens first .. last - 1 of the new ones are this workgroup's
@@ -124,7 +128,7 @@ __global__ __launch_bounds__(kThreads) void resize_kernel(ResizeArgs a) {
     // those that other sequences give back in this call: ranks (from the first page given back) top - count - j
     if (j0 < j1 && top - j0 >= t.count) {
       const long long lo = max(0ll, top - t.count - (j1 - 1)), hi = top - t.count - j0;
-      if (threadIdx.x == 0) running[0] = 0;
+      if (threadIdx.x == 0) running = 0;
       for (int base = 0; base < a.B; base += kThreads) {
         const int s = base + threadIdx.x;
         int back = 0, want = 0;
@@ -141,15 +145,15 @@ __global__ __launch_bounds__(kThreads) void resize_kernel(ResizeArgs a) {
           if ((threadIdx.x & 63) >= d) sum += x;
         }
         __syncthreads();
-        if ((threadIdx.x & 63) == 63) shared[threadIdx.x >> 6] = sum;
+        if ((threadIdx.x & 63) == 63) sums[threadIdx.x >> 6] = sum;
         __syncthreads();
-        long long front = running[0];
-        for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) front += shared[w];
+        long long front = running;
+        for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) front += sums[w];
         const long long end = front + sum, begin = end - back;
         for (long long rank = max(begin, lo); rank < min(end, hi + 1); ++rank)
           row[top - t.count - rank] = a.table[(size_t)s * a.max_pages + want + (rank - begin)];
         __syncthreads();
-        if (threadIdx.x == kThreads - 1) running[0] = end;
+        if (threadIdx.x == kThreads - 1) running = end;
       }
     }
   }
@@ -168,9 +172,8 @@ __global__ __launch_bounds__(kThreads) void resize_kernel(ResizeArgs a) {
 }
 
 __global__ __launch_bounds__(kThreads) void resize_state_kernel(ResizeArgs a) {
-  __shared__ long long shared[kThreads / 64];
+  __shared__ Sums shared[kThreads / 64];
   const Totals t = totals(a, 0, shared);
-  __syncthreads();
   write_state(a, t);
 }
 
@@ -333,15 +336,17 @@ int launch_rows(const Kv4& c, const HeadRows& k, const HeadRows& v, const int64_
 }  // namespace
 
 int launch_kv4_resize(const Kv4& c, const Kv4Resize& r, bool in_place, hipStream_t stream) {
-  ResizeArgs a = {r, c.table, c.B, c.page_log2, c.pages, c.max_pages, kTokens, false};
-  if (r.slots && r.tokens == 0) a.each = 1;
-  if (!r.slots) a.each = 1 << 30;
-  const unsigned parts = r.slots ? (unsigned)std::max(1, (r.tokens + kTokens - 1) / kTokens) : 1u;
+  ResizeArgs a = {r, c.table, c.B, c.page_log2, c.pages, c.max_pages, std::numeric_limits<int>::max(), false};
+  unsigned parts = 1;
+  if (r.slots && r.tokens > 0) {
+    const long long tokens = r.tokens, fine = (tokens + kTokens - 1) / kTokens;
+    // (a second dimension has at most 65535 workgroups)
+    a.each = std::max(fine * c.B <= kTogether ? kTokens : kTokensMany, (int)((tokens + 65534) / 65535));
+    parts = (unsigned)((tokens + a.each - 1) / a.each);
+  }
   const bool one = (unsigned long long)c.B * parts <= 1;
   a.state = c.B > 0 && (one || !in_place);
   (void)hipGetLastError();
-  // (a second dimension has at most 65535 workgroups)
-  if (parts > 65535) return SVG_ERR_UNSUPPORTED;
   if (c.B) hipLaunchKernelGGL(resize_kernel, dim3((unsigned)c.B, parts), dim3(kThreads), 0, stream, a);
   if (!a.state) hipLaunchKernelGGL(resize_state_kernel, dim3(1), dim3(kThreads), 0, stream, a);
   return hip_status(hipGetLastError());

@@ -63,7 +63,8 @@ def check_resize(table, held, wanted, free, count, page_size, tokens, in_place=F
 @pytest.mark.parametrize("sequences, page_size, longest, chunk, shrinking, spare", [
     (1, 16, 0, 1, 0.0, 3), (1, 16, 272, 64, 0.0, 40), (1, 64, 500, 1, 0.0, 3), (2, 16, 100, 33, 0.5, 40), (7, 32, 1000, 200, 0.3, 90),
     (64, 16, 63, 17, 0.5, 200), (255, 64, 700, 64, 0.2, 600), (256, 16, 40, 16, 0.9, 0), (257, 16, 40, 16, 0.6, 300), (600, 16, 90, 40, 0.4, 900),
-    (3, 256, 30000, 2049, 0.0, 40), (2, 16, 5000, 6000, 0.0, 800), (1500, 16, 20, 5, 0.5, 1600)])
+    (3, 256, 30000, 2049, 0.0, 40), (2, 16, 5000, 6000, 0.0, 800), (1500, 16, 20, 5, 0.5, 1600),
+    (300, 64, 9000, 4200, 0.5, 20000)])
 def test_page_tables(sequences, page_size, longest, chunk, shrinking, spare, in_place):
     rng = np.random.default_rng(sequences * 1000 + page_size + longest)
     for _ in range(3):
