@@ -81,6 +81,7 @@ class SvgKv4(C.Structure):
 class SvgKv4Attn(C.Structure):
     _fields_ = [("softmax_scale", C.c_float), ("causal", C.c_int32), ("block", C.c_int32), ("window", C.c_int32), ("sink", C.c_int32),
                 ("max_kv", C.c_int32), ("kv_len", C.c_void_p), ("q_len", C.c_void_p)]
+    sequences = None          # lengths that the descriptor was made with, where they are known
 
 
 class SvgError(RuntimeError):
@@ -454,7 +455,7 @@ def svg_fp4_linear_rows(x_tokens, x, in_activation, N, w, w_scales, bias, activa
 # ---- a cache of keys and values in 4 bits ---------------------------------------------------------
 
 def _whole(x, kind, name, count=None):
-    """Address of a tensor of whole numbers, which the device reads as they lie; count: how many there have to be."""
+    """Address of a tensor that the device reads or writes as it lies; count: how many elements there have to be."""
     if not isinstance(x, torch.Tensor):
         return _ptr(x)
     if x.dtype is not kind or not x.is_contiguous():
@@ -477,8 +478,11 @@ def kv4_cache(sequences, pages, max_pages, heads, head_dim, page_size, data=None
 
 def kv4_attn(kv_len, q_len=None, max_kv=0, causal=False, block=1, window=-1, sink=0, softmax_scale=0.0) -> SvgKv4Attn:
     """The descriptor of svg_kv4_attn_fwd; lengths as int32 tensors [sequences], which the caller keeps alive."""
-    return SvgKv4Attn(softmax_scale, int(causal), block, window, sink, max_kv, _whole(kv_len, torch.int32, "kv_len"),
-                      _whole(q_len, torch.int32, "q_len"))
+    attn = SvgKv4Attn(softmax_scale, int(causal), block, window, sink, max_kv, _whole(kv_len, torch.int32, "kv_len"), None)
+    if isinstance(kv_len, torch.Tensor):
+        attn.sequences = kv_len.numel()
+    attn.q_len = _whole(q_len, torch.int32, "q_len", attn.sequences)
+    return attn
 
 
 def svg_kv4_bytes(cache) -> int:
@@ -509,5 +513,9 @@ def svg_kv4_attn_workspace_bytes(cache, attn, q_tokens) -> int:
 
 
 def svg_kv4_attn_fwd(cache, attn, q_tokens, q, o_tokens, o, lse=None, workspace=None, workspace_bytes=0, stream=None):
-    _check(lib().svg_kv4_attn_fwd(C.byref(cache), C.byref(attn), C.byref(q_tokens), _ptr(q), C.byref(o_tokens), _ptr(o), _ptr(lse),
+    if attn.sequences not in (None, cache.B):
+        raise ValueError(f"kv_len has {attn.sequences} lengths for {cache.B} sequences")
+    if lse is not None:
+        lse = _whole(lse, torch.float32, "lse", q_tokens.B * q_tokens.N * (q_tokens.H * q_tokens.D // max(cache.D, 1)))
+    _check(lib().svg_kv4_attn_fwd(C.byref(cache), C.byref(attn), C.byref(q_tokens), _ptr(q), C.byref(o_tokens), _ptr(o), lse,
                                   _ptr(workspace), int(workspace_bytes), _stream(stream)), "svg_kv4_attn_fwd")

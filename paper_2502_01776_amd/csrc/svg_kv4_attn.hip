@@ -32,6 +32,7 @@ using namespace attn;
 
 constexpr int kTile = 64;              // keys of a tile
 constexpr int kWaves = 4;
+constexpr float kLowest = -3.40282347e38f;      // the first reference: no finite score is below it
 constexpr int kGroups = kTile / 16;    // 16-key groups of a tile: pages begin and end between them
 
 // f(0), f(1), .. f(N - 1) with constants.
@@ -409,7 +410,7 @@ __global__ __launch_bounds__(64 * kWaves, rows_waves(D, QB)) void kv4_rows_kerne
   float m[QB], l[QB];
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
-    m[qb] = kNegBig;
+    m[qb] = kLowest;
     l[qb] = 0.f;
   }
   unsigned char* const own = lds + wave * OWN;
@@ -538,7 +539,7 @@ __global__ __launch_bounds__(64 * kWaves, rows_waves(D, QB)) void kv4_rows_kerne
     const int row = u / PIECES, piece = u % PIECES;
     const int mm = m0 + row, n = mm / a.group;
     if (n >= s.qn) continue;
-    float top = kNegBig, sum = 0.f;
+    float top = kLowest, sum = 0.f;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) top = fmaxf(top, merged[w][row].x);
 #pragma unroll
@@ -645,7 +646,7 @@ __device__ __forceinline__ void attend_tile(const Kv4AttnArgs& a, TileLds<D>& sh
   float m[QB], l[QB];
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
-    m[qb] = kNegBig;
+    m[qb] = kLowest;
     l[qb] = 0.f;
   }
 
@@ -903,7 +904,7 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a) {
   const size_t step = (size_t)a.c.H * a.rows, first = (size_t)cut.first * step + (size_t)kvh * a.rows + m;
   const int count = there ? cut.count : 0;
   // the reference of all parts, a part to a lane
-  float top = kNegBig;
+  float top = kLowest;
   for (int x = piece; x < count; x += LANES) top = fmaxf(top, a.stats[first + x * step].x);
 #pragma unroll
   for (int d = LANES / 2; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, LANES));

@@ -188,6 +188,18 @@ def test_whole_numbers_of_other_types_and_sizes_are_refused():
                 S.svg_kv4_resize(cache(), **{**good, name: torch.zeros(5, dtype=good[name].dtype)}, stream=0)
 
 
+def test_lengths_of_other_numbers_of_sequences_are_refused():
+    two, three = torch.zeros(2, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    with pytest.raises(ValueError, match="q_len"):
+        S.kv4_attn(kv_len=two, q_len=three)
+    qt = tokens(D=64, H=4)
+    with pytest.raises(ValueError, match="3 lengths for 2 sequences"):
+        S.svg_kv4_attn_fwd(cache(), S.kv4_attn(kv_len=three), qt, Q, qt, O, stream=0)
+    for lse in (torch.zeros(2 * 4 * qt.N - 1), torch.zeros(2 * 4 * qt.N, dtype=torch.float64), torch.zeros(2, 4, 2 * qt.N)[..., ::2]):
+        with pytest.raises(ValueError, match="lse"):
+            S.svg_kv4_attn_fwd(cache(head_dim=64), S.kv4_attn(kv_len=two), qt, Q, qt, O, lse, stream=0)
+
+
 def test_a_pool_that_is_too_small_is_refused():
     need = S.svg_kv4_bytes(cache())
     assert cache(data=torch.zeros(need, dtype=torch.uint8)).data

@@ -150,3 +150,37 @@ def test_the_same_operand_as_the_products_of_4_bit_activations():
     S.svg_fp4_dequantize(S.tokens_of(values), *wq, values)
     size = f64(x.abs()) @ f64(values.abs()).T
     assert (np.abs(f64(a) - f64(b)) <= size * (2 * K / 32 + 32) * 2.0 ** -23).all()
+
+
+@pytest.mark.parametrize("M, N", [(1, 40), (5, 40), (3, 400)])
+def test_blocks_of_every_magnitude(M, N):
+    """Scale bytes at both ends of their range, blocks of zeros, and blocks that are not finite, which spoil their own output only."""
+    K = 384
+    gen = torch.Generator().manual_seed(N + M)
+    w = torch.randn(N, K, generator=gen)
+    w[0, 32:64] = 0.0
+    w[1] *= 2.0 ** -126                                                  # bytes around 0: powers of two that are no normal fp32 numbers
+    w[2] *= 2.0 ** 124
+    w[3] = 0.0
+    w[3, 200] = 2.0 ** -125
+    w[4, 100], w[5, 383], w[6, 0] = float("nan"), float("inf"), -float("inf")
+    w = w.cuda()
+    operand = [torch.zeros(S.svg_fp4_buffer_bytes(N, K, p), dtype=torch.uint8, device="cuda") for p in (0, 1)]
+    S.svg_fp4_quantize(S.tokens_of(w), w, 0, *operand)
+    values = torch.zeros(N, K, device="cuda")
+    S.svg_fp4_dequantize(S.tokens_of(values), *operand, values)
+    values = f64(values)
+    spoilt = [4, 5, 6]
+    assert np.isnan(values[spoilt]).any(1).all() and np.isfinite(np.delete(values, spoilt, 0)).all() and values[3, 200] != 0
+    kept = np.setdiff1d(np.arange(N), spoilt)
+    for kind, power in (("f32", 100), ("bf16", 100), ("f32", -5), ("f16", 3)):
+        x = (torch.randn(M, K, generator=gen) * 2.0 ** power).to(TYPES[kind]).cuda()
+        out = torch.zeros(M, N, device="cuda")
+        S.svg_fp4_linear_rows(S.tokens_of(x), x, 0, N, *operand, None, 0, S.tokens_of(out), out)
+        got, xv = f64(out), f64(x)
+        assert np.isnan(got[:, spoilt]).all()
+        want, size = xv @ values[kept].T, np.abs(xv) @ np.abs(values[kept]).T
+        # sums beyond the largest number of fp32 may be infinite; parts of products below its smallest normal number may be lost
+        fits = size < 2.0 ** 127
+        noise = size * (3 * -(-K // 32) + 16) * 2.0 ** -23 + 3 * K * 2.0 ** -126
+        assert fits[:, kept != 2].all() and (np.abs(got[:, kept] - want)[fits] <= noise[fits]).all(), (kind, power)

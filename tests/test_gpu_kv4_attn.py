@@ -210,6 +210,28 @@ def test_sharp_rows(N, capacity, D):
     check(down, q, rows=range(0, N, 5), causal=True)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("N, capacity", [(1, 0), (30, 0), (140, 0), (140, 8 * LONG)])
+def test_scores_far_below_and_above(N, capacity, D):
+    """Scores of -D 2^109 and of D 2^109 beside lower ones: exact sums of powers of two, far outside of what an exponential can take."""
+    def equal(b, k, v):
+        k[:] = -2.0 ** 55 if b == 0 else 2.0 ** 55
+        if b == 1:
+            k[100:] *= 0.5
+    lens = [333, 200]
+    cache = Cache(lens, 1, D, 16, seed=9, odd=equal, capacity=capacity)
+    q = torch.full((2, 1, N, D), 2.0 ** 54, dtype=torch.bfloat16, device="cuda")
+    assert tile(cache, q) == (16 if N == 1 else 32 if N == 30 or not capacity else 128)
+    o, lse = run(cache, q)
+    for b, seen in ((0, 333), (1, 100)):
+        _, v = O.read(cache.host, cache.slots(b)[:seen], D, 16)
+        # weights of one: exact; sums of n keys, and the result's rounding
+        mean, size = v[:, 0].mean(0), np.abs(v[:, 0]).mean(0)
+        assert (np.abs(o[b, 0].double().cpu().numpy() - mean) <= 2.0 ** -8 * np.abs(mean) + (seen / 32 + 64) * 2.0 ** -23 * size).all()
+        score = (-1.0 if b == 0 else 1.0) * D ** 0.5 * 2.0 ** 109
+        assert (np.abs(lse[b, 0].double().cpu().numpy() - score) <= 2.0 ** -20 * abs(score)).all()
+
+
 @pytest.mark.parametrize("N, capacity", [(1, 0), (3, 0), (60, 0), (140, 0), (140, LONG)])
 @pytest.mark.parametrize("D", [64, 128])
 def test_values_that_are_not_finite(N, capacity, D):
