@@ -160,17 +160,22 @@ __device__ __forceinline__ void load8_any(const void* base, size_t element, floa
     }
   }
 }
-template <int TYPE>
+// STREAM: rows that this launch does not look at again go past the caches.
+template <int TYPE, bool STREAM = false>
 __device__ __forceinline__ void store8_any(void* base, size_t element, const float (&v)[8]) {
   const block_f32x8 f = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
+  auto put = [](const block_u32x4& x, auto* p) {
+    if constexpr (STREAM) __builtin_nontemporal_store(x, p);
+    else *p = x;
+  };
   if constexpr (TYPE == SVG_F32) {
     block_u32x4_of4* p = reinterpret_cast<block_u32x4_of4*>(static_cast<float*>(base) + element);
-    p[0] = __builtin_bit_cast(block_u32x4, block_f32x4{v[0], v[1], v[2], v[3]});
-    p[1] = __builtin_bit_cast(block_u32x4, block_f32x4{v[4], v[5], v[6], v[7]});
+    put(__builtin_bit_cast(block_u32x4, block_f32x4{v[0], v[1], v[2], v[3]}), p);
+    put(__builtin_bit_cast(block_u32x4, block_f32x4{v[4], v[5], v[6], v[7]}), p + 1);
   } else {
-    *reinterpret_cast<block_u32x4_of2*>(static_cast<unsigned short*>(base) + element) =
-        TYPE == SVG_BF16 ? __builtin_bit_cast(block_u32x4, __builtin_convertvector(f, block_bf16x8))
-                         : __builtin_bit_cast(block_u32x4, __builtin_convertvector(f, block_f16x8));
+    put(TYPE == SVG_BF16 ? __builtin_bit_cast(block_u32x4, __builtin_convertvector(f, block_bf16x8))
+                         : __builtin_bit_cast(block_u32x4, __builtin_convertvector(f, block_f16x8)),
+        reinterpret_cast<block_u32x4_of2*>(static_cast<unsigned short*>(base) + element));
   }
 }
 template <int TYPE>

@@ -180,9 +180,9 @@ __global__ __launch_bounds__(kThreads) void resize_state_kernel(ResizeArgs a) {
 // ---- rows into pages and out of them ---------------------------------------------------------------------------------
 //
 // A lane takes eight neighbouring elements of a row of keys and the same of values: D / 8 lanes a row, four of them a block of 32, whose largest
-// magnitude needs two lane moves.  Bound: HBM (2 or 4 bytes an element in, 17/32 out).  A thread has kRowsEach rows' loads on their way at once.
-
-constexpr int kRowsEach = 2;
+// magnitude needs two lane moves.  Bound: HBM (2 or 4 bytes an element in, 17/32 out; the other way round on the way back).  One row of each to a thread, and
+// results past the caches: 40 heads of 4680 x 128 in bf16 written and read 45.6 us, 4.2 TB/s, a large copy 4.7; two rows to a thread 57.5, 48.6 with the
+// stores alone changed, 52.5 with the rows alone; four rows 58.7.
 
 struct RowsArgs {
   Kv4 c;
@@ -227,39 +227,32 @@ template <int D, int KT, int VT>
 __global__ __launch_bounds__(kThreads) void write_kernel(RowsArgs a) {
   constexpr int LANES = D / 8, ROWS = kThreads / LANES;
   const int c = threadIdx.x % LANES;
-  const unsigned u0 = (blockIdx.y * gridDim.x + blockIdx.x) * (ROWS * kRowsEach) + threadIdx.x / LANES;
-  RowPlace at[kRowsEach];
-  float k[kRowsEach][8] = {}, v[kRowsEach][8] = {};
+  RowPlace at;
+  at.template find<D>(a, (blockIdx.y * gridDim.x + blockIdx.x) * ROWS + threadIdx.x / LANES);
+  float k[8] = {}, v[8] = {};
+  if (at.there) {
+    load8_any<KT>(a.kp, at.k_at + 8 * c, k);
+    load8_any<VT>(a.vp, at.v_at + 8 * c, v);
+  }
+  unsigned ks = fp4_scale(quad_max(magnitude8(k))), vs = fp4_scale(quad_max(magnitude8(v)));
+  const unsigned kc = fp4_codes8(k, ks), vc = fp4_codes8(v, vs);
+  // a row's scale bytes as one word, or one half of it
+  ks <<= 8 * (c >> 2);
+  vs <<= 8 * (c >> 2);
 #pragma unroll
-  for (int x = 0; x < kRowsEach; ++x) at[x].template find<D>(a, u0 + x * ROWS);
-#pragma unroll
-  for (int x = 0; x < kRowsEach; ++x)
-    if (at[x].there) {
-      load8_any<KT>(a.kp, at[x].k_at + 8 * c, k[x]);
-      load8_any<VT>(a.vp, at[x].v_at + 8 * c, v[x]);
-    }
-#pragma unroll
-  for (int x = 0; x < kRowsEach; ++x) {
-    unsigned ks = fp4_scale(quad_max(magnitude8(k[x]))), vs = fp4_scale(quad_max(magnitude8(v[x])));
-    const unsigned kc = fp4_codes8(k[x], ks), vc = fp4_codes8(v[x], vs);
-    // a row's scale bytes as one word, or one half of it
-    ks <<= 8 * (c >> 2);
-    vs <<= 8 * (c >> 2);
-#pragma unroll
-    for (int m = 4; m < LANES; m <<= 1) {
-      ks |= __shfl_xor(ks, m, 64);
-      vs |= __shfl_xor(vs, m, 64);
-    }
-    if (!at[x].there) continue;
-    unsigned char* const codes = at[x].record + at[x].place * (D / 2) + 4 * c;
-    *reinterpret_cast<unsigned*>(codes) = kc;
-    *reinterpret_cast<unsigned*>(codes + a.c.values()) = vc;
-    if (c < 2) {
-      unsigned char* const scales = at[x].record + (c ? a.c.value_scales() : a.c.key_scales()) + at[x].place * (D / 32);
-      const unsigned s = c ? vs : ks;
-      if constexpr (D == 128) *reinterpret_cast<unsigned*>(scales) = s;
-      else *reinterpret_cast<unsigned short*>(scales) = (unsigned short)s;
-    }
+  for (int m = 4; m < LANES; m <<= 1) {
+    ks |= __shfl_xor(ks, m, 64);
+    vs |= __shfl_xor(vs, m, 64);
+  }
+  if (!at.there) return;
+  unsigned char* const codes = at.record + at.place * (D / 2) + 4 * c;
+  *reinterpret_cast<unsigned*>(codes) = kc;
+  *reinterpret_cast<unsigned*>(codes + a.c.values()) = vc;
+  if (c < 2) {
+    unsigned char* const scales = at.record + (c ? a.c.value_scales() : a.c.key_scales()) + at.place * (D / 32);
+    const unsigned s = c ? vs : ks;
+    if constexpr (D == 128) *reinterpret_cast<unsigned*>(scales) = s;
+    else *reinterpret_cast<unsigned short*>(scales) = (unsigned short)s;
   }
 }
 
@@ -278,31 +271,18 @@ template <int D, int KT, int VT>
 __global__ __launch_bounds__(kThreads) void read_kernel(RowsArgs a, void* kp, void* vp) {
   constexpr int LANES = D / 8, ROWS = kThreads / LANES;
   const int c = threadIdx.x % LANES;
-  const unsigned u0 = (blockIdx.y * gridDim.x + blockIdx.x) * (ROWS * kRowsEach) + threadIdx.x / LANES;
-  RowPlace at[kRowsEach];
-  unsigned kc[kRowsEach] = {}, vc[kRowsEach] = {};
-  unsigned char ks[kRowsEach] = {}, vs[kRowsEach] = {};
-#pragma unroll
-  for (int x = 0; x < kRowsEach; ++x) at[x].template find<D>(a, u0 + x * ROWS);
-#pragma unroll
-  for (int x = 0; x < kRowsEach; ++x)
-    if (at[x].there) {
-      const unsigned char* const codes = at[x].record + at[x].place * (D / 2) + 4 * c;
-      const unsigned char* const scales = at[x].record + at[x].place * (D / 32) + (c >> 2);
-      kc[x] = *reinterpret_cast<const unsigned*>(codes);
-      vc[x] = *reinterpret_cast<const unsigned*>(codes + a.c.values());
-      ks[x] = scales[a.c.key_scales()];
-      vs[x] = scales[a.c.value_scales()];
-    }
-#pragma unroll
-  for (int x = 0; x < kRowsEach; ++x) {
-    if (!at[x].there) continue;
-    float v[8];
-    values8(kc[x], ks[x], v);
-    store8_any<KT>(kp, at[x].k_at + 8 * c, v);
-    values8(vc[x], vs[x], v);
-    store8_any<VT>(vp, at[x].v_at + 8 * c, v);
-  }
+  RowPlace at;
+  at.template find<D>(a, (blockIdx.y * gridDim.x + blockIdx.x) * ROWS + threadIdx.x / LANES);
+  if (!at.there) return;
+  const unsigned char* const codes = at.record + at.place * (D / 2) + 4 * c;
+  const unsigned char* const scales = at.record + at.place * (D / 32) + (c >> 2);
+  const unsigned kc = *reinterpret_cast<const unsigned*>(codes), vc = *reinterpret_cast<const unsigned*>(codes + a.c.values());
+  const unsigned ks = scales[a.c.key_scales()], vs = scales[a.c.value_scales()];
+  float v[8];
+  values8(kc, ks, v);
+  store8_any<KT, true>(kp, at.k_at + 8 * c, v);
+  values8(vc, vs, v);
+  store8_any<VT, true>(vp, at.v_at + 8 * c, v);
 }
 
 template <class F>
@@ -322,7 +302,7 @@ int launch_rows(const Kv4& c, const HeadRows& k, const HeadRows& v, const int64_
   a.rows = rows;
   // from the layout that lies in memory: heads of a token side by side, or tokens of a head
   a.heads_inner = k.sh <= k.sn;
-  const int per_block = kThreads / (c.D / 8) * kRowsEach;
+  const int per_block = kThreads / (c.D / 8);
   const long long all = rows * c.H;
   if (all > 0xfff00000ll) return SVG_ERR_UNSUPPORTED;          // (rows are counted in 32 bits, those of the last workgroups too)
   a.units = (unsigned)all;
