@@ -8,7 +8,9 @@
  * over the kept tiles (Sec. 4.3), and a dense forward pass as the in-library
  * baseline (the paper's baseline is dense FlashAttention, Sec. 5.3); further the
  * fused QK-norm + rotary embedding pass in front of the attention (Sec. 4.3,
- * Table 2) and the FP8 variant of the sparse pass (Sec. 4.3 "Quantization").
+ * Table 2) and the FP8 variant of the sparse pass (Sec. 4.3 "Quantization").  Around
+ * it: gates and norms with their gradients, 4-bit projections, and for video that is
+ * generated chunk by chunk a 4-bit cache of keys and values with its attention.
  *
  * Conventions for every entry point
  *   - Tensors q, k, v, o are DEVICE pointers to contiguous bf16 arrays of shape

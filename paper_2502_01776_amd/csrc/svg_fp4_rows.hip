@@ -87,9 +87,9 @@ __device__ __forceinline__ void by_type(int type, F f) {
 // the weights each.  CB: blocks of 16 columns of the instruction that the rows' parts take.
 // A wavefront asks for its first activations, then for its first DEPTH column tiles, and only then looks at the activations: silu, its parts and
 // the trip to LDS lie behind the weights' way.  (Loads arrive in order: activations asked for behind the weights would be waited for with them.)
-// Measured with weights out of memory: 4 x 20480 x 5120, silu in front and GELU behind, 17.3 us (3.2 TB/s; two tiles ahead, three 18, four 19.9), of which
-// the activations take 3; one row without them 13.7 (4.1 TB/s), 5120 x 5120 7.2, 5120 x 256 3.7.  One row tile to a workgroup instead of five: 16.9
-// for one row, 36 for four.
+// Measured with weights out of memory: 4 x 20480 x 5120, silu in front and GELU behind, 14.4 us among others (3.9 TB/s; 17.3 by itself, three tiles ahead 18, four
+// 19.9), of which the activations take 3; one row without them 13.7 by itself, 5120 x 5120 7.2, 5120 x 256 3.7.  One row tile to a workgroup instead of
+// five: 16.9 for one row, 36 for four.
 template <int RT, int CB, int WK, int DEPTH>
 __global__ __launch_bounds__(64 * kWaves, 2) void rows_kernel(RowsArgs a) {
   constexpr int GROUPS = kWaves / WK, UNITS = DEPTH == 1 ? 1 : 5;

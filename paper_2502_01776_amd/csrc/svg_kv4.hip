@@ -20,9 +20,9 @@ constexpr int kThreads = 256;
 //
 // A workgroup takes kTokens of one sequence's tokens and sums over all sequences by itself: 8 bytes a sequence out of L2
 // instead of a launch in front.  The state (lengths, count) is written by the first workgroup, or by a launch of its own where it
-// lies where others still read it.  Bound: latency of a launch and of three dependent trips to memory; the slots' bytes for many tokens.
-
-// kTokens is 512 as long as all workgroups are on the card at once (200 sequences of up to 1560 tokens: 7.8 us, with 2048 8.6), else 2048:
+// lies where others still read it.  Bound: latency of a launch and of three dependent trips to memory (one sequence 3.2 us); the slots' bytes for many tokens.
+//
+// kTokens is 512 as long as all workgroups are on the card at once (200 sequences of up to 1560 new tokens: 7.8 us, with 2048 8.6), else 2048:
 // more workgroups would only repeat the sums.
 
 constexpr int kTokens = 512, kTokensMany = 2048, kTogether = 8 * 256;
@@ -181,7 +181,7 @@ __global__ __launch_bounds__(kThreads) void resize_state_kernel(ResizeArgs a) {
 //
 // A lane takes eight neighbouring elements of a row of keys and the same of values: D / 8 lanes a row, four of them a block of 32, whose largest
 // magnitude needs two lane moves.  Bound: HBM (2 or 4 bytes an element in, 17/32 out; the other way round on the way back).  One row of each to a thread, and
-// results past the caches: 40 heads of 4680 x 128 in bf16 written and read 45.6 us, 4.2 TB/s, a large copy 4.7; two rows to a thread 57.5, 48.6 with the
+// results past the caches: 40 heads of 4680 x 128 in bf16 written and read 45.8 us, 4.2 TB/s, a large copy 4.7; two rows to a thread 57.5, 48.6 with the
 // stores alone changed, 52.5 with the rows alone; four rows 58.7.
 
 struct RowsArgs {

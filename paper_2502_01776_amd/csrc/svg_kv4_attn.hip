@@ -9,13 +9,17 @@
 // weights are the second product's operand as they are.  The weights are rounded to bf16 for it; sums take them unrounded.
 //
 // Every 4-bit value under its power of two is a bf16 number, so keys and values are dequantised exactly (two a v_cvt_scalef32_pk_bf16_fp4) and the
-// scores are exact products summed in fp32.  (The matrix instruction that takes 4-bit keys as they are, with a query as two 8-bit parts, costs the
-// same and cuts what is 2^-14 below the largest of 128 products: scores off by 4e-6 of their size.)
+// scores are exact products summed in fp32.  (The matrix instruction that takes 4-bit keys as they are, with a query as two 8-bit parts, made the form
+// with 128 rows 5 % faster, but cuts what is 2^-14.5 below the largest of 128 products: scores off by 4e-6 of their size.)
 //
 // Two forms:
 //  * 16 or 32 query rows: the wavefronts of a workgroup share them and split the keys, every one with its own tiles, straight
-//    from memory into registers one tile ahead; no barrier before the results are merged through LDS.  Bound: HBM.
-//  * 128 rows, 32 a wavefront: a tile of keys and values is dequantised once for all, a quarter by each wavefront, into LDS.  Bound: MFMA.
+//    from memory into registers one tile ahead; no barrier before the results are merged through LDS.  Bound: HBM: one token of eight sequences over
+//    up to 65536, 32 heads on 8 of 128 channels, 65 us with the join, 4.9 TB/s (a large copy 4.7).
+//  * 128 rows, 32 a wavefront: a tile of keys and values is dequantised once for all, a quarter by each wavefront, into LDS.  Bound: the matrix and the
+//    vector unit in turns.  40 heads of 4680 rows and 128 channels over 32760 keys 2.74-2.79 ms, 1.07-1.09 PFLOP/s (matrix cores busy 44 % of the cycles, vector
+//    instructions 48 %, workgroups on 94 % of the places); 48 heads of 4050 rows and 64 channels in a window of seven frames 680 us, 0.79 PFLOP/s (31, 57
+//    and 87 %: two equal rounds of workgroups, of which those across two frames take a quarter longer).
 // Few workgroups for the chip: the keys are cut into parts for several, whose results a second launch joins.
 #include <algorithm>
 #include <type_traits>
@@ -594,7 +598,7 @@ struct PageList {
 // The loop is skewed by one tile, as in svg_attn_kernel.h: with the scores of tile j in registers a wavefront takes their exponentials and then issues
 // the products of tile j + 1's scores and of tile j's output as one batch; the first operands of a batch are read in front of the exponentials, every
 // other one behind the products.  Keys of tile j + 2 and values of j + 1 are dequantised into LDS meanwhile, those behind them are on their way
-// from memory; one barrier a tile.
+// from memory; one barrier a tile.  Without the wavefront's priority over its batch +4 %, with batches that the compiler may reorder +8 %.
 template <int D>
 struct TileLds {
   static constexpr int HALF = kTile * 2 * D;             // a tile of keys, or of values
@@ -610,7 +614,10 @@ __device__ __forceinline__ void attend_tile(const Kv4AttnArgs& a, TileLds<D>& sh
   constexpr int WORDS = D / 32;                          // words of codes that a thread stages of a tile's keys, and of its values
   constexpr int HALF = TileLds<D>::HALF;
   constexpr int NS = kGroups * DS, NV = kGroups / 2 * CB; // operands of the two products
-  constexpr int AHEAD = D == 128 ? 8 : 4;                // of them in registers
+  // Of them in registers: at D = 128 (40 x 4680 rows over 32760 keys) 4 ahead 3.26 ms, 8 3.17, 12 3.22; at D = 64 2 and 4 alike.
+  constexpr int AHEAD = D == 128 ? 8 : 4;
+  // At D = 128 3.15 ms where one tile after the other takes 3.56; at D = 64, where three wavefronts to a SIMD overlap by themselves, 893 us and 890-899.
+  // (Both taken before masks were kept from rows that do not exist.)
   constexpr bool SKEWED = D == 128;
   unsigned char* const lds = shared.tiles;
   auto& odd_values = shared.odd_values;
@@ -887,7 +894,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 128 ? 2 : 3) void kv4_tiles_kerne
 // ---- parts of the keys joined -----------------------------------------------------------------------------------------
 
 // D / 4 lanes have four channels each and GROUPS such sets of lanes a row, every GROUPS-th part each; they add up through LDS in the order of their
-// number.  Eight sets where rows are few, so that all parts are on their way at once (one token over 64 parts 11 -> 5 us), else one.
+// number.  Eight sets where rows are few, so that all parts are on their way at once (64 parts of eight sequences' tokens 7 -> 4.8 us), else one.
 template <int D, int GROUPS>
 __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a) {
   constexpr int LANES = D / 4, ROWS = 256 / (LANES * GROUPS);
@@ -957,7 +964,8 @@ Kv4Plan kv4_plan(const Kv4& c, const svg_kv4_attn_t& attn, long long N, int grou
   const long long work = (long long)c.B * c.H * ((p.rows + 31) / 32) * units;
   p.tile = p.rows <= 16 ? 16 : p.rows <= 64 || work <= 16384 ? 32 : 128;
   p.tiles = std::max(1, (p.rows + p.tile - 1) / p.tile);
-  // parts for one round of workgroups, each of a few tiles at least
+  // Parts for one round of workgroups, each of a few tiles at least.  Few rows: 512 places 75 us and 7 for the join, 768 73 + 9, 1024 83 + 11 (one token
+  // of eight sequences over up to 65536).  128 rows: 226 rows of 48 heads and three sequences 63 us in 768 parts, 77 in 1152, 90 in 480 and 576.
   const long long places = p.tile == 128 ? kv4_places(c.D) : 512, least = p.tile == 128 ? 8 : 2 * kWaves;
   const long long parts = std::min(places / ((long long)c.H * p.tiles), c.B * std::max(1ll, units / least));
   p.parts = (int)(c.B <= 64 ? std::max<long long>(parts, c.B) : c.B * std::max(1ll, parts / c.B));
