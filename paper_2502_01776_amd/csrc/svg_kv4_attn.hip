@@ -22,6 +22,7 @@
 //    and 87 %: two equal rounds of workgroups, of which those across two frames take a quarter longer).
 // Few workgroups for the chip: the keys are cut into parts for several, whose results a second launch joins.
 #include <algorithm>
+#include <limits>
 #include <type_traits>
 #include <utility>
 
@@ -946,8 +947,22 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a) {
 
 }  // namespace
 
-// Workgroups of the form with 128 rows that the chip holds: two and three to a compute unit.
-constexpr int kv4_places(int D) { return D == 128 ? 512 : 768; }
+// Which form, and in how many parts?  What is estimated to take the least time: with c workgroups on the fullest of 256 compute units and t
+// turns of a workgroup (a tile for each of its four wavefronts, in the form with 128 rows one for all),
+//     begin + begin_more c + t (turn + turn_more c)       microseconds,
+// the last round of workgroups counted by its own c, and for parts the launch that joins them, 4.5 and what they take to write and read at 4.3 TB/s.
+// Fitted to the times of 276 calls with 1 to 64 heads of 1 to 1000 rows over 300 to 60000 keys, each cut in up to eight ways: the way
+// taken is within 15 % of the best of those measured, 2 % on the average.  Measured, chosen way and its neighbours: 4 x 64 rows of 64 channels over 272 keys 7.2 us
+// in tiles of 16 rows, 8.8 of 32; 24 x 48 of 128 over 20000 42 and 39; 24 x 226 of 128 over 12000 61 in tiles of 128, 81 of 32; 40 x 800 of 64 over 12000, which
+// leave the second places of the chip to few tiles of 128, 185 and 164.  8 x 64 of 128 over 1000 keys 12.3 in four parts, 13.2 in one; 24 x 48 14.9 and 13.3.
+struct FormTimes {
+  float begin, begin_more, turn, turn_more;
+};
+constexpr FormTimes kFormTimes[3][2] = {      // tiles of 16, 32 and 128 rows; 64 and 128 channels
+    {{3.7f, 1.23f, 0.87f, 0.34f}, {3.9f, 1.5f, 1.3f, 0.61f}},
+    {{4.2f, 1.8f, 0.77f, 0.58f}, {5.f, 2.1f, 0.98f, 1.f}},
+    {{7.1f, 1.f, 0.56f, 0.41f}, {9.1f, 0.6f, 1.01f, 0.4f}}};
+constexpr int kUnits = 256;                   // compute units
 
 Kv4Plan kv4_plan(const Kv4& c, const svg_kv4_attn_t& attn, long long N, int group) {
   Kv4Plan p = {};
@@ -957,18 +972,45 @@ Kv4Plan kv4_plan(const Kv4& c, const svg_kv4_attn_t& attn, long long N, int grou
   long long keys = attn.max_kv > 0 ? std::min<long long>(attn.max_kv, capacity) : capacity;
   if (attn.window >= 0 && attn.causal) keys = std::min(keys, (attn.window + 1ll) * attn.block + std::min<long long>(attn.sink, keys) + 128);
   p.reach = (int)keys;
-  const long long units = (keys + kTile - 1) / kTile;
-  // More than 64 rows go to the form with 128 where there is work for the whole chip.  Times of that form over those of the one with 32 rows, both
-  // head dimensions, by tiles of 32 rows times tiles of keys (4 to 64 heads, 128 and 256 rows, 272 to 16384 keys): up to 10240 1.04-1.5, at 16384 0.98-1.35,
-  // from 32768 on 0.79-0.94.  With 33 to 64 rows, which leave it half empty, 1.03-1.4.
-  const long long work = (long long)c.B * c.H * ((p.rows + 31) / 32) * units;
-  p.tile = p.rows <= 16 ? 16 : p.rows <= 64 || work <= 16384 ? 32 : 128;
-  p.tiles = std::max(1, (p.rows + p.tile - 1) / p.tile);
-  // Parts for one round of workgroups, each of a few tiles at least.  Few rows: 512 places 75 us and 7 for the join, 768 73 + 9, 1024 83 + 11 (one token
-  // of eight sequences over up to 65536).  128 rows: 226 rows of 48 heads and three sequences 63 us in 768 parts, 77 in 1152, 90 in 480 and 576.
-  const long long places = p.tile == 128 ? kv4_places(c.D) : 512, least = p.tile == 128 ? 8 : 2 * kWaves;
-  const long long parts = std::min(places / ((long long)c.H * p.tiles), c.B * std::max(1ll, units / least));
-  p.parts = (int)(c.B <= 64 ? std::max<long long>(parts, c.B) : c.B * std::max(1ll, parts / c.B));
+  const long long tiles = (keys + kTile - 1) / kTile;
+  float best = std::numeric_limits<float>::infinity();
+  auto consider = [&](int form, int rows, long long parts) {
+    const FormTimes& x = kFormTimes[form][c.D == 128];
+    const long long row_tiles = std::max(1, (p.rows + rows - 1) / rows), groups = c.H * row_tiles * parts;
+    // Parts are dealt by length: fewer than two for each sequence cut only some of them, from there on none is much longer than the others.
+    const long long cut = parts < 2ll * c.B ? std::min<long long>(parts, c.B) : parts, a_turn = (rows == 128 ? 1 : kWaves) * std::max(1ll, cut);
+    const long long turns = (tiles * c.B + a_turn - 1) / a_turn;
+    // (the forms with 16 and 32 rows slow down evenly with more workgroups, whether they are on the card or wait)
+    const long long together = rows == 128 ? (c.D == 128 ? 2 : 3) * kUnits : std::max(groups, 1ll);
+    const long long full = groups / together, rest = groups % together;
+    auto on = [&](long long n) { return (float)((n + kUnits - 1) / kUnits); };
+    float time = x.begin + x.begin_more * on(std::min(groups, together)) +
+                 (float)turns * ((float)full * (x.turn + x.turn_more * on(together)) + (rest ? x.turn + x.turn_more * on(rest) : 0.f));
+    if (parts > c.B) time += 4.5f + (float)parts * (float)c.H * (float)p.rows * (float)c.D * (8 / 5e6f);
+    if (time < best) {
+      best = time;
+      p.tile = rows;
+      p.tiles = (int)row_tiles;
+      p.parts = (int)parts;
+    }
+  };
+  constexpr int kRows[3] = {16, 32, 128};
+  for (int form = 0; form < 3; ++form) {
+    const int rows = kRows[form];
+    // (32 rows for 16, or 128 for 64 and fewer, are never faster)
+    if ((rows == 32 && p.rows <= 16) || (rows == 128 && p.rows <= 64)) continue;
+    const long long each = (long long)c.H * std::max(1, (p.rows + rows - 1) / rows);
+    // (with more the form with 128 rows is faster: 48 x 4050 of 64 channels 681 us and 801)
+    if ((rows == 16 && p.rows > 16 && each * c.B > 4 * kUnits) || (rows == 32 && p.rows > 64 && each * c.B > 5 * kUnits)) continue;
+    consider(form, rows, c.B);
+    // parts for one, two or three workgroups to a compute unit, of a turn (128 rows: 8 tiles) at least
+    const long long most = c.B * (rows == 128 ? tiles / 8 : (tiles + kWaves - 1) / kWaves);
+    for (int places = kUnits; places <= (rows == 128 && c.D == 64 ? 3 : 2) * kUnits; places += kUnits) {
+      long long parts = std::min(places / each, most);
+      if (c.B > 64) parts -= parts % c.B;
+      if (parts > c.B) consider(form, rows, parts);
+    }
+  }
   return p;
 }
 
@@ -1005,7 +1047,7 @@ int launch_kv4_attn(const Kv4& c, const svg_kv4_attn_t& attn, const Kv4Plan& pla
   const float scale = attn.softmax_scale > 0.f ? attn.softmax_scale : 1.f / sqrtf((float)c.D);
   a.scale_log2 = scale * 1.4426950408889634f;
   const long long blocks = (long long)c.H * plan.tiles * plan.parts;
-  if (blocks > (1ll << 24)) return SVG_ERR_UNSUPPORTED;       // a launch has fewer than 2^32 threads
+  if (blocks > (1ll << 24) - 8) return SVG_ERR_UNSUPPORTED;      // a launch has fewer than 2^32 threads
   (void)hipGetLastError();
   const bool wide = c.D == 128;
   if (plan.tile == 128) {

@@ -215,13 +215,17 @@ def test_how_a_call_is_cut():
         p = kv4_plan.plan(c, a, N, group)
         q = tokens(B=B, H=H * group, N=N, D=D)
         assert S.svg_kv4_attn_workspace_bytes(c, a, q) == (p.parts * H * N * group * (4 * D + 8) if p.parts > B else 0)
-        assert p.rows == N * group and p.tiles == -(-p.rows // p.tile) and p.parts >= B and (B <= 64 or p.parts % B == 0)
+        assert p.rows == N * group and p.tiles == max(1, -(-p.rows // p.tile)) and p.parts >= B and (B <= 64 or p.parts % B == 0)
         assert p.parts == B or p.parts * H * p.tiles <= (768 if p.tile == 128 and D == 64 else 512)
         return p
-    assert [plan(N=n).tile for n in (1, 16, 17, 32, 33, 64, 65)] == [16, 16, 32, 32, 32, 32, 32] and plan(N=1000).tile == 128
-    assert plan(N=1, group=17).tile == 32 and plan(N=70, keys=512).tile == 32 and plan(N=70, H=100).tile == 128
-    assert plan(N=1).parts == 128 and plan(N=1, keys=64).parts == 2 and plan(N=1, max_kv=1024).parts == 4
-    assert plan(N=1, B=70).parts == 70 and plan(N=1, B=70, H=1).parts == 490 and plan(N=4000, H=40).parts == 2
+    # few rows, or little work: 16 rows a tile; more: 32; work for the whole chip: 128
+    assert [plan(N=n).tile for n in (1, 16, 17, 32, 64, 200, 1000)] == [16, 16, 32, 32, 32, 128, 128]
+    assert [plan(N=n, keys=512).tile for n in (17, 70, 200)] == [16, 16, 16] and plan(N=1000, keys=512).tile == 32
+    assert plan(N=1, group=17).tile == 32 and plan(N=70, H=100).tile == 128 and plan(N=800, H=40, B=1, keys=12032).tile == 32
+    assert plan(N=1).parts == 128 and plan(N=1, keys=64).parts == 2 and plan(N=1, max_kv=1024).parts == 8
+    # cut where the turns saved are worth the launch that joins the parts
+    assert plan(N=64, B=1, H=4, D=64, keys=1024).parts == 1 and plan(N=64, B=1, H=4, D=64, keys=2048).parts == 8
+    assert plan(N=1, B=70).parts == 70 and plan(N=1, B=70, H=1).parts == 490 and plan(N=4000, H=40).parts == 2 and plan(N=0).tiles == 1
     assert plan(N=1, causal=True, block=64, window=3, sink=0).reach == 4 * 64 + 128 and plan(N=1, block=64, window=3).reach == 32768
     for H in (1, 3, 40):
         for N in (1, 30, 100, 5000):

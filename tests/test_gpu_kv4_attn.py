@@ -111,23 +111,28 @@ def check(cache, q, kv_len=None, q_len=None, max_kv=0, scale=0.0, rows=None, hea
     return o, lse
 
 
-# Cases of few sequences and short caches take the form whose wavefronts split the keys; the page tables of the others could hold so many keys that the
-# form with 128 rows is taken (its parts are then many and short, some of them empty), or have so many heads.
-LONG = 1 << 18
+# The same rows take another form where the page table could hold more keys: its parts are then many and short, some of them empty.
+def room(form, lens, H, D, page_size, N, group=1):
+    """A capacity of the page table with which N rows of `group` heads take the form with `form` rows."""
+    pages = [max(-(-max(lens) // page_size), -(-n // page_size)) for n in (0,) + tuple(1 << i for i in range(9, 25))]
+    for n in pages:
+        cache = S.kv4_cache(len(lens), 1, n, H, D, page_size)
+        if n * page_size <= 1 << 23 and kv4_plan.plan(cache, S.kv4_attn(kv_len=None), N, group).tile == form:
+            return n * page_size
+    raise AssertionError("no capacity makes this form the best")
 
 
-def tile(cache, q, **kw):
-    return kv4_plan.plan(cache.desc(), S.kv4_attn(kv_len=i32(cache.lens), **kw), q.shape[2], q.shape[1] // cache.H).tile
+def plan(cache, q, **kw):
+    return kv4_plan.plan(cache.desc(), S.kv4_attn(kv_len=i32(cache.lens), **kw), q.shape[2], q.shape[1] // cache.H)
 
 
 @pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("N", [1, 3, 16, 17, 31, 33, 129, 200])
-@pytest.mark.parametrize("capacity", [0, LONG])
-def test_lengths_of_queries_and_keys(capacity, N, D):
+@pytest.mark.parametrize("N, form", [(n, f) for n in (1, 3, 16, 17, 31, 33, 129, 200) for f in (16, 32, 128) if f == 16 or n > f // 2])
+def test_lengths_of_queries_and_keys(form, N, D):
     lens = [1, 15, 16, 17, 63, 64, 65, 200, 517]
-    cache = Cache(lens, 2, D, 16, seed=N, capacity=capacity)
+    cache = Cache(lens, 2, D, 16, seed=N, capacity=room(form, lens, 2, D, 16, N))
     q = queries(len(lens), 2, N, D, "heads", N)
-    assert tile(cache, q) == (16 if N <= 16 else 128 if capacity and N > 64 else 32)
+    assert plan(cache, q).tile == form
     check(cache, q, rows=range(0, N, 1 if N < 20 else 13))                # queries without a token of their own among them
     check(cache, q, rows=range(0, N, 1 if N < 20 else 13), causal=True)
 
@@ -144,16 +149,29 @@ def test_form_with_128_rows_in_one_part(B, group, D):
     q = queries(B, H * group, N, D, "packed", B)
     q_len = [N] + [int(x) for x in rng.integers(0, N + 1, B - 1)]
     for mask in (dict(causal=True), dict(causal=True, block=100, window=2, sink=70), dict()):
-        p = kv4_plan.plan(cache.desc(), S.kv4_attn(kv_len=i32(lens), q_len=i32(q_len), **mask), N, group)
+        p = plan(cache, q, **mask)
         assert p.tile == 128 and p.parts == B
         check(cache, q, q_len=q_len, rows=range(0, N, 41), heads=[0, H * group // 2, H * group - 1], **mask)
 
 
-@pytest.mark.parametrize("N, capacity", [(1, 0), (40, 0), (71, LONG)])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("form, B, heads, N", [(16, 3, 9, 70), (32, 1, 100, 210), (32, 70, 2, 130)])
+def test_forms_with_fewer_rows_in_one_part(form, B, heads, N, D):
+    """Results straight from the sums of the workgroup."""
+    lens = [960] + [int(x) for x in np.random.default_rng(B).integers(1, 961, B - 1)]
+    cache = Cache(lens, heads, D, 32, seed=B)
+    q = queries(B, heads, N, D, "packed", B)
+    for mask in (dict(causal=True, block=100, window=5, sink=70), dict(causal=True, window=800), dict(causal=True, block=230, window=3)):
+        p = plan(cache, q, **mask)
+        assert p.tile == form and p.parts == B
+        check(cache, q, rows=range(0, N, 31), heads=[0, heads // 2, heads - 1], **mask)
+
+
+@pytest.mark.parametrize("N, form", [(1, 16), (40, 32), (71, 128)])
 @pytest.mark.parametrize("layout", ["packed", "odd"])
 @pytest.mark.parametrize("group, D, page_size", [(1, 64, 32), (3, 128, 64), (4, 64, 16), (7, 128, 16), (16, 64, 256)])
-def test_shared_heads_and_layouts(group, D, page_size, layout, N, capacity):
-    cache = Cache([300, 77], 2, D, page_size, seed=group, capacity=capacity)
+def test_shared_heads_and_layouts(group, D, page_size, layout, N, form):
+    cache = Cache([300, 77], 2, D, page_size, seed=group, capacity=room(form, [300, 77], 2, D, page_size, N, group))
     q = queries(2, 2 * group, N, D, layout, group)
     check(cache, q, rows=range(0, N, 7), causal=True)
     check(cache, q, rows=range(0, N, 13), scale=0.31)
@@ -163,18 +181,18 @@ def test_shared_heads_and_layouts(group, D, page_size, layout, N, capacity):
 @pytest.mark.parametrize("block, window, sink, causal", [(1, -1, 0, True), (1, 0, 0, True), (1, 20, 3, True), (10, 1, 10, True), (64, 1, 0, True),
                                                         (50, 2, 64, True), (37, 0, 5, False), (37, 3, 0, False), (1000, 1, 70, True), (7, 0, 0, True)])
 def test_masks(block, window, sink, causal, D):
-    cache = Cache([400, 131, 9], 1, D, 16, seed=block)
-    large = Cache([400, 131, 9], 1, D, 16, seed=block, capacity=8 * LONG)
-    for N, cache in ((1, cache), (9, cache), (24, cache), (150, cache), (150, large)):
+    lens = [400, 131, 9]
+    for N, form in ((1, 16), (9, 16), (24, 16), (24, 32), (150, 16), (150, 32), (150, 128)):
+        cache = Cache(lens, 1, D, 16, seed=block, capacity=room(form, lens, 1, D, 16, N))
         q = queries(3, 1, N, D, "heads", N)
         check(cache, q, rows=range(0, N, 1 if N < 10 else 7), block=block, window=window, sink=sink, causal=causal)
     q = queries(3, 1, 150, D, "heads", 3)
     check(cache, q, q_len=[150, 20, 0], rows=range(0, 150, 7), block=block, window=window, sink=sink, causal=causal)
 
 
-@pytest.mark.parametrize("N, capacity", [(1, 0), (2, 0), (100, 0), (100, LONG)])
-def test_pages_that_are_not_there(N, capacity):
-    cache = Cache([500, 300, 64], 2, 64, 16, seed=9, capacity=capacity)
+@pytest.mark.parametrize("N, form", [(1, 16), (2, 16), (100, 16), (100, 32), (100, 128)])
+def test_pages_that_are_not_there(N, form):
+    cache = Cache([500, 300, 64], 2, 64, 16, seed=9, capacity=room(form, [500, 300, 64], 2, 64, 16, N))
     cache.table[0, [0, 3, 4, 5, 6, 20]] = [-1, -1, -1, cache.pages, 2 ** 30, -1]
     cache.table[1, :] = -1                                                # nothing at all
     cache.table[2, 3] = -5
@@ -184,10 +202,11 @@ def test_pages_that_are_not_there(N, capacity):
     check(cache, q, rows=range(0, N, 9), causal=True, block=16, window=3, sink=16)
 
 
-@pytest.mark.parametrize("N, capacity", [(1, 0), (20, 0), (300, 0), (300, LONG)])
-def test_lengths_of_the_call(N, capacity):
+@pytest.mark.parametrize("N, form", [(1, 16), (20, 16), (20, 32), (300, 16), (300, 32), (300, 128)])
+def test_lengths_of_the_call(N, form):
     """Empty sequences and query lists, lengths out of range (cut off), no more keys than the hint says."""
-    cache = Cache([200, 90, 40, 130], 2, 128, 32, seed=2, capacity=capacity)
+    lens = [200, 90, 40, 130]
+    cache = Cache(lens, 2, 128, 32, seed=2, capacity=room(form, lens, 2, 128, 32, N))
     q = queries(4, 2, N, 128, "heads", 2)
     check(cache, q, kv_len=[0, 90, -5, 129], q_len=[N, 0, N, -1], rows=range(0, N, 17))
     check(cache, q, kv_len=[0, 1, 40, 2], q_len=[N, N + 100, 1, 2], rows=range(0, N, 17), causal=True)
@@ -198,11 +217,12 @@ def test_lengths_of_the_call(N, capacity):
 
 
 @pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("N, capacity", [(1, 0), (32, 0), (128, 0), (128, 8 * LONG)])
-def test_sharp_rows(N, capacity, D):
+@pytest.mark.parametrize("N, form", [(1, 16), (32, 16), (32, 32), (128, 16), (128, 32), (128, 128)])
+def test_sharp_rows(N, form, D):
     """Scores of +-60 and more: the reference maximum moves again and again, most weights are zero."""
     def grow(b, k, v):
         k *= np.linspace(0.1, 3, len(k))[:, None, None]
+    capacity = room(form, [700], 1, D, 64, N)
     cache = Cache([700], 1, D, 64, seed=4, spread=2.0, odd=grow, capacity=capacity)
     q = queries(1, 1, N, D, "heads", 4, scale=6.0)
     check(cache, q, rows=range(0, N, 5))
@@ -211,17 +231,17 @@ def test_sharp_rows(N, capacity, D):
 
 
 @pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("N, capacity", [(1, 0), (30, 0), (140, 0), (140, 8 * LONG)])
-def test_scores_far_below_and_above(N, capacity, D):
+@pytest.mark.parametrize("N, form", [(1, 16), (30, 16), (30, 32), (140, 32), (140, 128)])
+def test_scores_far_below_and_above(N, form, D):
     """Scores of -D 2^109 and of D 2^109 beside lower ones: exact sums of powers of two, far outside of what an exponential can take."""
     def equal(b, k, v):
         k[:] = -2.0 ** 55 if b == 0 else 2.0 ** 55
         if b == 1:
             k[100:] *= 0.5
     lens = [333, 200]
-    cache = Cache(lens, 1, D, 16, seed=9, odd=equal, capacity=capacity)
+    cache = Cache(lens, 1, D, 16, seed=9, odd=equal, capacity=room(form, lens, 1, D, 16, N))
     q = torch.full((2, 1, N, D), 2.0 ** 54, dtype=torch.bfloat16, device="cuda")
-    assert tile(cache, q) == (16 if N == 1 else 32 if N == 30 or not capacity else 128)
+    assert plan(cache, q).tile == form
     o, lse = run(cache, q)
     for b, seen in ((0, 333), (1, 100)):
         _, v = O.read(cache.host, cache.slots(b)[:seen], D, 16)
@@ -232,10 +252,11 @@ def test_scores_far_below_and_above(N, capacity, D):
         assert (np.abs(lse[b, 0].double().cpu().numpy() - score) <= 2.0 ** -20 * abs(score)).all()
 
 
-@pytest.mark.parametrize("N, capacity", [(1, 0), (3, 0), (60, 0), (140, 0), (140, LONG)])
+@pytest.mark.parametrize("N, form", [(1, 16), (3, 16), (60, 16), (60, 32), (140, 32), (140, 128)])
 @pytest.mark.parametrize("D", [64, 128])
-def test_values_that_are_not_finite(N, capacity, D):
+def test_values_that_are_not_finite(N, form, D):
     """They spoil the results of the queries that see them, in their 32 channels (values) or whole (keys), and nothing else, bit for bit."""
+    capacity = room(form, [333, 200], 2, D, 16, N)
     plain = Cache([333, 200], 2, D, 16, seed=6, capacity=capacity)
     at = 333 - N // 2 - 1                                                # the queries behind it see it, those in front do not
 
