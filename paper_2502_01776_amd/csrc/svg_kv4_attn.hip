@@ -950,11 +950,11 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a) {
 // Which form, and in how many parts?  What is estimated to take the least time: with c workgroups on the fullest of 256 compute units and t
 // turns of a workgroup (a tile for each of its four wavefronts, in the form with 128 rows one for all),
 //     begin + begin_more c + t (turn + turn_more c)       microseconds,
-// the last round of workgroups counted by its own c, and for parts the launch that joins them, 4.5 and what they take to write and read at 4.3 TB/s.
+// the last round of workgroups counted by its own c, and for parts the launch that joins them, 4.5 and what they take to write and read at 5 TB/s.
 // Fitted to the times of 276 calls with 1 to 64 heads of 1 to 1000 rows over 300 to 60000 keys, each cut in up to eight ways: the way
 // taken is within 15 % of the best of those measured, 2 % on the average.  Measured, chosen way and its neighbours: 4 x 64 rows of 64 channels over 272 keys 7.2 us
 // in tiles of 16 rows, 8.8 of 32; 24 x 48 of 128 over 20000 42 and 39; 24 x 226 of 128 over 12000 61 in tiles of 128, 81 of 32; 40 x 800 of 64 over 12000, which
-// leave the second places of the chip to few tiles of 128, 185 and 164.  8 x 64 of 128 over 1000 keys 12.3 in four parts, 13.2 in one; 24 x 48 14.9 and 13.3.
+// are 280 tiles of 128 for 768 places, 164 in tiles of 32, 185 of 128.  8 x 64 of 128 over 1000 keys 12.3 in four parts, 13.2 in one; 24 x 48 14.9 and 13.3.
 struct FormTimes {
   float begin, begin_more, turn, turn_more;
 };
