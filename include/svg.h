@@ -563,16 +563,19 @@ size_t svg_kv4_bytes(const svg_kv4_t* cache);
  *   wanted     int32 [B]: tokens that they are to hold (0: finished)
  *   free_pages int32 [pages], free_count int32 [1]: a stack, free_pages[*free_count - 1] on top
  * Pages are given back first, of every sequence with fewer pages wanted than held those behind, sequences and pages ascending, and
- * pushed; then every sequence that needs more takes pages from the top, sequences and pages ascending.  Table entries of pages given
- * back keep what they held.
+ * pushed; then every sequence that needs more takes pages from the top, sequences and pages ascending.  An entry that is a page that is not there
+ * (outside of 0 .. pages - 1) is nothing to give back.  Table entries of pages given back keep what they held.  Pages that a window has left behind
+ * are the caller's to give back: the entry to -1, the page's number onto the stack, both before the next call.
  *   new_lengths int32 [B], new_count int32 [1]: written; each may be lengths or free_count itself
- *   slots      int64 [B, tokens], or NULL: the slots of tokens lengths[b], lengths[b] + 1, .. of sequence b up to wanted[b], then -1
+ *   slots      int64 [B, tokens], or NULL: the slots of tokens lengths[b], lengths[b] + 1, .. of sequence b up to wanted[b], then -1; -1 too for tokens
+ *              in the rest of a page that the sequence held and that is not there
  *   status     int32 [1]: SVG_KV4_OK; SVG_KV4_FULL: too few free pages; SVG_KV4_LENGTHS: a length or count out of range, a sequence that
- *              grows by more than `tokens` (where slots are wanted), or a stack with no room for what is given back.  In the last two
- *              cases nothing but new_lengths (= lengths), new_count (= *free_count) and slots (-1) is written.
+ *              grows by more than `tokens` (where slots are wanted), or a stack with no room for what is given back; SVG_KV4_PAGES: a number that would
+ *              be taken from the stack is outside of 0 .. pages - 1.  Unless it is SVG_KV4_OK, nothing
+ *              but new_lengths (= lengths), new_count (= *free_count), slots (-1) and status is written.
  * Uses B, page_size, pages, max_pages and page_table of the cache.  Overlaps of what is written with anything else: SVG_ERR_ALIAS.
  */
-enum { SVG_KV4_OK = 0, SVG_KV4_FULL = 1, SVG_KV4_LENGTHS = 2 };
+enum { SVG_KV4_OK = 0, SVG_KV4_FULL = 1, SVG_KV4_LENGTHS = 2, SVG_KV4_PAGES = 3 };
 int svg_kv4_resize(const svg_kv4_t* cache, const int32_t* lengths, const int32_t* wanted, int32_t* free_pages, const int32_t* free_count,
                    int32_t* new_lengths, int32_t* new_count, int64_t* slots, int32_t tokens, int32_t* status, void* stream);
 

@@ -87,34 +87,37 @@ def attention(q, k, v, exists, scale, block=1, causal=False, window=-1, sink=0, 
     return o, lse, size, slack
 
 
-OK, FULL, LENGTHS = 0, 1, 2
+OK, FULL, LENGTHS, PAGES = 0, 1, 2, 3
 
 
 def resize(table, lengths, wanted, free, count, page_size, tokens, with_slots=True):
-    """(table, free, new_lengths, new_count, slots, status): lists walked one page after the other."""
-    table, free = table.copy(), free.copy()
+    """(table, free, new_lengths, new_count, slots, status): lists walked one page after the other.  Entries outside of the pool are pages that
+    are not there: nothing to give back, and never granted."""
     Bn, max_pages = table.shape
     most, pages = max_pages * page_size, len(free)
+    none = np.full((Bn, tokens), -1, dtype=np.int64)
+    refused = lambda why: (table.copy(), free.copy(), lengths.copy(), count, none, why)  # noqa: E731
+    if any(not 0 <= a <= most or not 0 <= b <= most or (with_slots and b - a > tokens) for a, b in zip(lengths, wanted)):
+        return refused(LENGTHS)
+    if not 0 <= count <= pages:
+        return refused(LENGTHS)
     held, need = -(-lengths // page_size), -(-wanted // page_size)
-    slots = np.full((Bn, tokens), -1, dtype=np.int64)
-    bad = any(not 0 <= a <= most or not 0 <= b <= most or (with_slots and b - a > tokens) for a, b in zip(lengths, wanted))
-    back = 0 if bad else int(np.maximum(held - need, 0).sum())
-    take = 0 if bad else int(np.maximum(need - held, 0).sum())
-    if bad or not 0 <= count <= pages or count + back > pages:
-        return table, free, lengths.copy(), count, slots, LENGTHS
-    if take > count + back:
-        return table, free, lengths.copy(), count, slots, FULL
-    top = count
-    for b in range(Bn):
-        for j in range(need[b], held[b]):
-            free[top] = table[b, j]
-            top += 1
+    back = [int(table[b, j]) for b in range(Bn) for j in range(need[b], held[b]) if 0 <= table[b, j] < pages]
+    if count + len(back) > pages:
+        return refused(LENGTHS)
+    stack = [int(x) for x in free[:count]] + back
+    new_free, new_table = free.copy(), table.copy()
+    new_free[:len(stack)] = stack
     for b in range(Bn):
         for j in range(held[b], need[b]):
-            top -= 1
-            table[b, j] = free[top]
+            if not stack:
+                return refused(FULL)
+            new_table[b, j] = stack.pop()
+    if any(not 0 <= new_table[b, j] < pages for b in range(Bn) for j in range(held[b], need[b])):
+        return refused(PAGES)
+    slots = none
     for b in range(Bn):
         for i in range(min(tokens, max(0, wanted[b] - lengths[b]))):
-            page, place = table[b, (lengths[b] + i) // page_size], (lengths[b] + i) % page_size
+            page, place = new_table[b, (lengths[b] + i) // page_size], (lengths[b] + i) % page_size
             slots[b, i] = page * page_size + place if 0 <= page < pages else -1
-    return table, free, wanted.copy(), top, slots, OK
+    return new_table, new_free, wanted.copy(), len(stack), slots, OK

@@ -15,7 +15,7 @@ from .binding import (SvgShape, SVG_HEAD_SPATIAL, SVG_HEAD_TEMPORAL, SVG_LIST_TE
                       SVG_ACT_GELU_TANH, svg_gate_norm_fwd, svg_gate_norm_workspace_bytes, svg_gate_norm_bwd,
                       svg_fp4_buffer_bytes, svg_fp4_quantize, svg_fp4_dequantize,
                       svg_fp4_linear_workspace_bytes, svg_fp4_linear, svg_fp4_linear_quantize, svg_fp4_linear_rows,
-                      SvgKv4, SvgKv4Attn, SVG_KV4_OK, SVG_KV4_FULL, SVG_KV4_LENGTHS, kv4_cache, kv4_attn, svg_kv4_bytes, svg_kv4_resize,
+                      SvgKv4, SvgKv4Attn, SVG_KV4_OK, SVG_KV4_FULL, SVG_KV4_LENGTHS, SVG_KV4_PAGES, kv4_cache, kv4_attn, svg_kv4_bytes, svg_kv4_resize,
                       svg_kv4_write, svg_kv4_read, svg_kv4_attn_workspace_bytes, svg_kv4_attn_fwd)
 
 __all__ = ["SvgShape", "SVG_HEAD_SPATIAL", "SVG_HEAD_TEMPORAL", "SVG_LIST_TEMPORAL_FRAME_MAJOR", "SVG_ATTN_QO_TOKEN_ORDER", "SVG_ATTN_ELEMENT_MASK", "SVG_ATTN_KV_TOKEN_ORDER", "SvgError", "lib", "shape_from_config",
@@ -29,5 +29,5 @@ __all__ = ["SvgShape", "SVG_HEAD_SPATIAL", "SVG_HEAD_TEMPORAL", "SVG_LIST_TEMPOR
            "SVG_ACT_SILU", "SVG_ACT_GELU_TANH", "svg_gate_norm_fwd", "svg_gate_norm_workspace_bytes",
            "svg_gate_norm_bwd", "svg_fp4_buffer_bytes", "svg_fp4_quantize", "svg_fp4_dequantize",
            "svg_fp4_linear_workspace_bytes", "svg_fp4_linear", "svg_fp4_linear_quantize", "svg_fp4_linear_rows",
-           "SvgKv4", "SvgKv4Attn", "SVG_KV4_OK", "SVG_KV4_FULL", "SVG_KV4_LENGTHS", "kv4_cache", "kv4_attn", "svg_kv4_bytes",
+           "SvgKv4", "SvgKv4Attn", "SVG_KV4_OK", "SVG_KV4_FULL", "SVG_KV4_LENGTHS", "SVG_KV4_PAGES", "kv4_cache", "kv4_attn", "svg_kv4_bytes",
            "svg_kv4_resize", "svg_kv4_write", "svg_kv4_read", "svg_kv4_attn_workspace_bytes", "svg_kv4_attn_fwd"]

@@ -28,7 +28,7 @@ SVG_ATTN_KV_TOKEN_ORDER = 4          # svg_sparse_attn_fwd_ex: k, v of temporal 
 SVG_BF16, SVG_F16, SVG_F32 = 0, 1, 2                            # element types of the operators around the attention
 SVG_FP4_CODES, SVG_FP4_SCALES = 0, 1                            # svg_fp4_buffer_bytes
 SVG_ACT_NONE, SVG_ACT_SILU, SVG_ACT_GELU_TANH = 0, 1, 2
-SVG_KV4_OK, SVG_KV4_FULL, SVG_KV4_LENGTHS = 0, 1, 2              # status of svg_kv4_resize
+SVG_KV4_OK, SVG_KV4_FULL, SVG_KV4_LENGTHS, SVG_KV4_PAGES = 0, 1, 2, 3      # status of svg_kv4_resize
 SVG_OK = 0
 
 EXPORTS = ("svg_strerror", "svg_version", "svg_last_hip_error", "svg_workspace_bytes", "svg_profile_plan", "svg_tile_counts",

@@ -13,19 +13,28 @@ constexpr int kThreads = 256;
 
 // ---- page tables -------------------------------------------------------------------------------------------------------
 //
-// With have_b and want_b the pages that sequence b holds and needs, sequence b gives back r_b = max(0, have_b - want_b) pages and
-// takes g_b = max(0, want_b - have_b).  With sums R_b, G_b over the sequences in front of b and R, G over all of them, page j it gives back goes to
-// stack[count + R_b + j - want_b], and page j it takes is stack[count + R - 1 - (G_b + j - have_b)]: below `count` the stack's own entry,
-// from there on a page that some sequence gives back in the same call, found without the stack, so that nothing waits for another workgroup.
+// With have_b and want_b the pages that sequence b holds and needs, b gives back those of its entries want_b .. have_b - 1 that name a page of the
+// pool, r_b pages (an entry may be a page that is not there), and takes g_b = max(0, want_b - have_b).  With sums R_b, G_b over the sequences in front of
+// b and R, G over all of them, the i-th page that it gives back goes to stack[count + R_b + i], and its entry j that is new gets
+// stack[count + R - 1 - (G_b + j - have_b)]: below `count` the stack's own entry, from there on a page that some sequence gives back in the same call,
+// found without the stack, so that nothing waits for another workgroup.
 //
-// A workgroup takes kTokens of one sequence's tokens and sums over all sequences by itself: 8 bytes a sequence out of L2
-// instead of a launch in front.  The state (lengths, count) is written by the first workgroup, or by a launch of its own where it
-// lies where others still read it.  Bound: latency of a launch and of three dependent trips to memory (one sequence 3.2 us); the slots' bytes for many tokens.
+// A workgroup takes `each` of one sequence's tokens and makes the sums by itself: 8 bytes a sequence out of L2 instead of a launch in front.  R_b and R
+// need the entries that are given back; a workgroup that neither gives nor takes does without where their number can not change the answer.
+// A call that would grant a number outside of the pool grants nothing, so every workgroup looks at all that are taken from the
+// stack.  The state (lengths, count) is written by the first workgroup, or by a launch of its own where it
+// lies where others still read it.
 //
-// kTokens is 512 as long as all workgroups are on the card at once (200 sequences of up to 1560 new tokens: 7.8 us, with 2048 8.6), else 2048:
-// more workgroups would only repeat the sums.
+// Bound: latency of a launch and of dependent trips to memory, then the slots' bytes, then what every workgroup reads for itself.  In a graph: one sequence
+// 4.2 us; 200 sequences that grow by up to 1560 tokens 6.1, and 9.8 with every eighth cut off, 4800 pages given back; 200 that are cut off, 150000 pages given back,
+// 62; 200 that grow by 30000 tokens in pages of 16, 190000 numbers looked at, 84.
+//
+// `each` is 512 as long as that makes at most two workgroups to a compute unit, else 2048: more would repeat the sums more often than they
+// share the rest (32 sequences of 8000 new tokens 5.5 us, with 2048 6.2; 200 of 1560, every eighth cut off, 9.8, with 512 11.0).
 
-constexpr int kTokens = 512, kTokensMany = 2048, kTogether = 8 * 256;
+constexpr int kTokens = 512, kTokensMany = 2048, kTogether = 2 * 256;
+constexpr int kRun = 16;              // neighbouring entries of a row that a thread looks at together
+constexpr int kList = 2 * kThreads * kRun;      // pages given back that a workgroup keeps
 
 struct ResizeArgs {
   Kv4Resize r;
@@ -49,52 +58,184 @@ struct Sequence {
   __device__ __forceinline__ int take() const { return max(0, want - have); }
 };
 
+// The sums that a call's totals are made of.
+struct Sums {
+  long long back, take, front_take;
+  int bad;
+};
+
+struct Shared {
+  Sums sums[kThreads / 64];
+  unsigned waves[kThreads / 64];
+  unsigned end[kThreads];                                // runs of a round's sequences up to each
+  int from[kThreads], to[kThreads];                      // their entries
+  unsigned own;                                          // pages that sequence b gives back
+  int list[kList];
+};
+
+// The sum of x over the threads up to this one; all: over the workgroup.
+__device__ __forceinline__ unsigned running_sum(unsigned x, Shared& shared, unsigned* all) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const unsigned y = __shfl_up(x, d, 64);
+    if ((threadIdx.x & 63) >= d) x += y;
+  }
+  __syncthreads();                                       // (what was there has been read)
+  if ((threadIdx.x & 63) == 63) shared.waves[threadIdx.x >> 6] = x;
+  __syncthreads();
+  *all = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) {
+    if (w < (int)(threadIdx.x >> 6)) x += shared.waves[w];
+    *all += shared.waves[w];
+  }
+  return x;
+}
+
+typedef int i32x4_of4 __attribute__((ext_vector_type(4), aligned(4)));
+
+// The pages that sequences s0 .. s1 - 1 give back, sequences and entries ascending, up to number `last` of them at least.  A thread takes a run of up to kRun
+// neighbours of a row, the workgroup a run to each thread a round.
+// KEEP: they are counted, R in all and R_b of sequences in front of b (b's own in shared.own, which is zero before), and put into the list while they fit.
+// Otherwise f(first, n) behind each round, with pages first .. first + n - 1 in the list.  All threads of the workgroup.
+template <bool KEEP, class F>
+__device__ __forceinline__ void given_back(const ResizeArgs& a, int s0, int s1, int b, long long last, Shared& shared, long long* R, long long* R_b, F f) {
+  const size_t entries = (size_t)a.B * a.max_pages;
+  *R = *R_b = 0;
+  for (int base = s0; base < s1; base += kThreads) {
+    int from = 0, to = 0;
+    if (base + (int)threadIdx.x < s1) {
+      const Sequence q(a, base + threadIdx.x);
+      from = q.want;
+      to = from + q.back();
+    }
+    unsigned runs;                                       // (at most 256 times 2^26 / kRun)
+    const unsigned end = running_sum((unsigned)(to - from + kRun - 1) / kRun, shared, &runs);
+    if (runs == 0) continue;
+    shared.end[threadIdx.x] = end;                       // (the sum's barriers stand behind the reads of the round in front)
+    shared.from[threadIdx.x] = from;
+    shared.to[threadIdx.x] = to;
+    __syncthreads();
+    for (unsigned first = 0; first < runs; first += kThreads) {
+      const unsigned run = first + threadIdx.x;
+      int s = 0, n = 0, page[kRun] = {};
+      size_t at = 0;                                     // of the run's first entry in the table
+      if (run < runs) {
+        // the first sequence whose runs end behind this one
+#pragma unroll
+        for (int step = kThreads / 2; step > 0; step >>= 1) s += shared.end[s + step - 1] <= run ? step : 0;
+        const int entry = shared.from[s] + kRun * (int)(run - (s ? shared.end[s - 1] : 0));
+        n = min(kRun, shared.to[s] - entry);
+        at = (size_t)(base + s) * a.max_pages + entry;
+      }
+      // four at a time, also where the run ends between them; at the table's end one at a time
+#pragma unroll
+      for (int i = 0; i < kRun; i += 4) {
+        if (__builtin_amdgcn_ballot_w64(i < n) == 0) continue;
+        if (i < n) {
+          if (at + i + 4 <= entries) {
+            const i32x4_of4 y = *reinterpret_cast<const i32x4_of4*>(a.table + at + i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) page[i + j] = y[j];
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) page[i + j] = i + j < n ? a.table[at + i + j] : -1;
+          }
+        }
+      }
+      unsigned there = 0;
+#pragma unroll
+      for (int i = 0; i < kRun; ++i) there |= i < n && (unsigned)page[i] < (unsigned)a.pages ? 1u << i : 0;
+      // pages of the runs up to this one, and in the upper half of those in front of b (at most kThreads kRun each)
+      const unsigned own = __builtin_popcount(there);
+      if (KEEP && base + s == b && own) atomicAdd(&shared.own, own);
+      unsigned all;
+      const unsigned upto = running_sum(own | (base + s < b ? own : 0) << 16, shared, &all);
+      if (!KEEP || *R + (all & 0xffff) <= kList) {
+        unsigned to = (upto & 0xffff) - own + (KEEP ? (unsigned)*R : 0);
+#pragma unroll
+        for (int i = 0; i < kRun; ++i)
+          if (there >> i & 1) shared.list[to++] = page[i];
+      }
+      if constexpr (!KEEP) {
+        __syncthreads();
+        f(*R, (int)(all & 0xffff));
+      }
+      *R += all & 0xffff;
+      *R_b += all >> 16;
+      if (*R > last) return;
+    }
+  }
+}
+
 struct Totals {
   long long R, G, R_b, G_b;      // over all sequences, over those in front of b
+  int r_b;
   int status;
   int count;
 };
 
-// The sums that a call's totals are made of.
-struct Sums {
-  long long all_r, all_g, front_r, front_g;
-  int bad;
-};
-
-__device__ __forceinline__ Totals totals(const ResizeArgs& a, int b, Sums* shared) {
+// A thread's share of the sums.
+__device__ __forceinline__ Sums share(const ResizeArgs& a, int b) {
   Sums t = {};
-  const int count = *a.r.free_count;
   for (int s = threadIdx.x; s < a.B; s += kThreads) {
     const Sequence q(a, s);
     t.bad |= q.bad;
-    t.all_r += q.back();
-    t.all_g += q.take();
-    t.front_r += s < b ? q.back() : 0;
-    t.front_g += s < b ? q.take() : 0;
+    t.back += q.back();
+    t.take += q.take();
+    t.front_take += s < b ? q.take() : 0;
   }
-#pragma unroll
-  for (int m = 32; m > 0; m >>= 1) {
-    t.all_r += __shfl_xor(t.all_r, m, 64);
-    t.all_g += __shfl_xor(t.all_g, m, 64);
-    t.front_r += __shfl_xor(t.front_r, m, 64);
-    t.front_g += __shfl_xor(t.front_g, m, 64);
-    t.bad |= __shfl_xor(t.bad, m, 64);
-  }
-  if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = t;
-  __syncthreads();
-  t = shared[0];
-#pragma unroll
-  for (int w = 1; w < kThreads / 64; ++w) {
-    t.all_r += shared[w].all_r;
-    t.all_g += shared[w].all_g;
-    t.front_r += shared[w].front_r;
-    t.front_g += shared[w].front_g;
-    t.bad |= shared[w].bad;
-  }
-  const bool wrong = t.bad || count < 0 || count > a.pages || count + t.all_r > a.pages;
-  return {t.all_r, t.all_g, t.front_r, t.front_g, wrong ? SVG_KV4_LENGTHS : t.all_g > count + t.all_r ? SVG_KV4_FULL : SVG_KV4_OK, count};
+  return t;
 }
 
+// exact: R and R_b are needed.
+__device__ __forceinline__ Totals totals(const ResizeArgs& a, int b, Sums t, const int count, bool exact, Shared& shared) {
+  if (threadIdx.x == 0) shared.own = 0;
+#pragma unroll
+  for (int m = 32; m > 0; m >>= 1) {
+    t.back += __shfl_xor(t.back, m, 64);
+    t.take += __shfl_xor(t.take, m, 64);
+    t.front_take += __shfl_xor(t.front_take, m, 64);
+    t.bad |= __shfl_xor(t.bad, m, 64);
+  }
+  if ((threadIdx.x & 63) == 0) shared.sums[threadIdx.x >> 6] = t;
+  __syncthreads();
+  t = shared.sums[0];
+#pragma unroll
+  for (int w = 1; w < kThreads / 64; ++w) {
+    t.back += shared.sums[w].back;
+    t.take += shared.sums[w].take;
+    t.front_take += shared.sums[w].front_take;
+    t.bad |= shared.sums[w].bad;
+  }
+  Totals r = {0, t.take, 0, t.front_take, 0, SVG_KV4_LENGTHS, count};
+  if (t.bad || count < 0 || count > a.pages) return r;
+  // At most t.back pages come back: the answer may be the same whatever their number.
+  bool known = t.back == 0, count_them = !known && (exact || count + t.back > a.pages || r.G > count);
+  for (;;) {
+    if (count_them) {
+      known = true;
+      given_back<true>(a, 0, a.B, b, std::numeric_limits<long long>::max(), shared, &r.R, &r.R_b, [](long long, int) {});
+    }
+    if (count + r.R > a.pages) return r;
+    if (r.G > count + r.R) {
+      r.status = SVG_KV4_FULL;
+      return r;
+    }
+    // the numbers that are taken from the stack (with R = 0 for an unknown one no fewer)
+    int wrong = 0;
+#pragma unroll 4
+    for (int i = (int)max(0ll, count + r.R - r.G) + (int)threadIdx.x; i < count; i += kThreads)
+      wrong |= (unsigned)a.r.free_pages[i] >= (unsigned)a.pages;
+    wrong = __syncthreads_or(wrong);                     // (the list can be read)
+    r.r_b = (int)shared.own;
+    r.status = wrong ? SVG_KV4_PAGES : SVG_KV4_OK;
+    if (!wrong || known) return r;
+    count_them = true;
+  }
+}
+
+// (behind the last read of the lengths)
 __device__ __forceinline__ void write_state(const ResizeArgs& a, const Totals& t) {
   for (int s = threadIdx.x; s < a.B; s += kThreads) a.r.new_lengths[s] = t.status == SVG_KV4_OK ? a.r.wanted[s] : a.r.lengths[s];
   if (threadIdx.x == 0) {
@@ -104,60 +245,50 @@ __device__ __forceinline__ void write_state(const ResizeArgs& a, const Totals& t
 }
 
 __global__ __launch_bounds__(kThreads) void resize_kernel(ResizeArgs a) {
-  __shared__ Sums shared[kThreads / 64];
-  __shared__ long long sums[kThreads / 64], running;
+  __shared__ Shared shared;
   const int b = blockIdx.x, part = blockIdx.y;
+  // (all loads in front of the first branch)
   const Sequence own(a, b);
-  const Totals t = totals(a, b, shared);                 // (its barrier stands behind every read of the lengths)
-  if (a.state && b == 0 && part == 0) write_state(a, t);
-  const bool ok = t.status == SVG_KV4_OK;
+  const int count = *a.r.free_count;
+  const Sums sums = share(a, b);
   // tokens first .. last - 1 of the new ones are this workgroup's
   const long long first = (long long)part * a.each;
-  const long long last = min(first + a.each, (long long)max(0, own.wanted - own.len));
+  const long long last = min(first + a.each, own.bad ? 0ll : (long long)max(0, own.wanted - own.len));
+  // its new entries; the first may be another workgroup's too, which writes the same
+  const int j0 = max(own.have, (int)((own.len + first) >> a.log2)), j1 = first < last ? min(own.want, (int)((own.len + last - 1) >> a.log2) + 1) : 0;
+  const bool state = a.state && b == 0 && part == 0, gives = part == 0 && own.back() > 0, takes = j0 < j1;
   int32_t* const row = a.table + (size_t)b * a.max_pages;
   const int mask = (1 << a.log2) - 1;
-  if (ok && part == 0)                                   // pages given back
-    for (int j = own.want + threadIdx.x; j < own.have; j += kThreads) a.r.free_pages[t.count + t.R_b + (j - own.want)] = row[j];
-  // (own.take() > 0: the row of a sequence that takes pages is written, one that gives pages back is only read)
-  if (ok && own.take() > 0 && first < last) {
-    // pages whose tokens are here; the first may be another workgroup's too, which writes the same
-    const int j0 = max(own.have, (int)((own.len + first) >> a.log2)), j1 = min(own.want, (int)((own.len + last - 1) >> a.log2) + 1);
-    const long long top = t.count + t.R - 1 - t.G_b + own.have;      // page j: stack[top - j]
-    for (int j = j0 + threadIdx.x; j < j1; j += kThreads)
-      if (top - j < t.count) row[j] = a.r.free_pages[top - j];
-    // those that other sequences give back in this call: ranks (from the first page given back) top - count - j
-    if (j0 < j1 && top - j0 >= t.count) {
-      const long long lo = max(0ll, top - t.count - (j1 - 1)), hi = top - t.count - j0;
-      if (threadIdx.x == 0) running = 0;
-      for (int base = 0; base < a.B; base += kThreads) {
-        const int s = base + threadIdx.x;
-        int back = 0, want = 0;
-        if (s < a.B) {
-          const Sequence q(a, s);
-          back = q.back();
-          want = q.want;
+  bool ok = false;
+  if (first < last || gives || state) {                  // (the others have no slots to name)
+    const Totals t = totals(a, b, sums, count, gives || takes || state, shared);
+    ok = t.status == SVG_KV4_OK;
+    // entry j: stack[top - j]; pages that other sequences give back in this call have the numbers (from the first one) top - count - j
+    const long long top = t.count + t.R - 1 - t.G_b + own.have, lo = max(0ll, top - t.count - (j1 - 1)), hi = top - t.count - j0;
+    if (ok && takes)
+      for (int j = j0 + threadIdx.x; j < j1; j += kThreads)
+        if (top - j < t.count) row[j] = a.r.free_pages[top - j];
+    // Pages given back: this sequence's go to the stack, those that it takes into its row.  (The row of a sequence that takes pages is written, one that
+    // gives pages back is only read.)
+    if (ok && (gives ? t.r_b > 0 : takes && t.R > 0 && hi >= 0)) {
+      auto put = [&](long long list, int n) {            // pages list .. list + n - 1 are in the list
+        if (gives) {
+          const long long from = max(t.R_b, list), to = min(t.R_b + t.r_b, list + n);
+          for (long long i = from + threadIdx.x; i < to; i += kThreads) a.r.free_pages[t.count + i] = shared.list[i - list];
+        } else {
+          const long long from = max(lo, list), to = min(hi + 1, list + n);
+          for (long long i = from + threadIdx.x; i < to; i += kThreads) row[top - t.count - i] = shared.list[i - list];
         }
-        // sum in front of each thread: inside the wavefront, then over the wavefronts
-        long long sum = back;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-          const long long x = __shfl_up(sum, d, 64);
-          if ((threadIdx.x & 63) >= d) sum += x;
-        }
-        __syncthreads();
-        if ((threadIdx.x & 63) == 63) sums[threadIdx.x >> 6] = sum;
-        __syncthreads();
-        long long front = running;
-        for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) front += sums[w];
-        const long long end = front + sum, begin = end - back;
-        for (long long rank = max(begin, lo); rank < min(end, hi + 1); ++rank)
-          row[top - t.count - rank] = a.table[(size_t)s * a.max_pages + want + (rank - begin)];
-        __syncthreads();
-        if (threadIdx.x == kThreads - 1) running = end;
-      }
+      };
+      long long all, front;
+      if (t.R <= kList) put(0, (int)t.R);
+      else
+        given_back<false>(a, gives ? b : 0, gives ? b + 1 : a.B, b, gives ? t.r_b : hi, shared, &all, &front,
+                          [&](long long first, int n) { put(first + (gives ? t.R_b : 0), n); });
     }
+    __syncthreads();                                     // the row's new entries can be read, the lengths are not any more
+    if (state) write_state(a, t);
   }
-  __syncthreads();                                       // the row's new entries can be read
   if (a.r.slots == nullptr) return;
   int64_t* const slots = a.r.slots + (size_t)b * a.r.tokens;
   const long long end = min(first + a.each, (long long)a.r.tokens);
@@ -172,8 +303,9 @@ __global__ __launch_bounds__(kThreads) void resize_kernel(ResizeArgs a) {
 }
 
 __global__ __launch_bounds__(kThreads) void resize_state_kernel(ResizeArgs a) {
-  __shared__ Sums shared[kThreads / 64];
-  const Totals t = totals(a, 0, shared);
+  __shared__ Shared shared;
+  const Totals t = totals(a, 0, share(a, 0), *a.r.free_count, true, shared);
+  __syncthreads();
   write_state(a, t);
 }
 
