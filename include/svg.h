@@ -613,8 +613,8 @@ typedef struct svg_kv4_attn {
 /*
  * q, o  bf16 token matrices [B,Hq,N,D] (or of Hq*D columns where B is 1), Hq a multiple of the cache's H: query head h reads head h / (Hq / H)
  * lse   device fp32 [B,Hq,N]: natural log of the sum of exponentials of the scaled scores, or NULL
- * Rows of o and lse from q_len[b] on are left as they were.  Scores are fp32 sums of exact products, the weights are rounded to bf16 for the
- * second product, sums are fp32.  Results repeat bit for bit.
+ * Rows of o and lse from q_len[b] on are left as they were.  Scores are fp32 sums of exact products, of any size that times scale / log 2 is finite
+ * in fp32; the weights are rounded to bf16 for the second product, sums are fp32.  Results repeat bit for bit.
  * workspace: >= svg_kv4_attn_workspace_bytes(cache, attn, q_desc) bytes, 16-byte aligned (0: may be NULL).
  * Overlaps of o, lse or the workspace with each other or an input: SVG_ERR_ALIAS.
  */

@@ -38,6 +38,7 @@ using namespace attn;
 constexpr int kTile = 64;              // keys of a tile
 constexpr int kWaves = 4;
 constexpr float kLowest = -3.40282347e38f;      // the first reference: no finite score is below it
+constexpr float kFar = 1073741824.f;            // 2^30 (take_tile)
 constexpr int kGroups = kTile / 16;    // 16-key groups of a tile: pages begin and end between them
 
 // f(0), f(1), .. f(N - 1) with constants.
@@ -168,12 +169,31 @@ __device__ __forceinline__ int key_piece(int row, int piece) {
   return row * (2 * D) + ((piece ^ (D == 128 ? row & 15 : (row >> 1) & 7)) << 4);
 }
 
+// Scores of rows with a far reference as what is left of them against it.
+template <int QB>
+__device__ __forceinline__ void far_scores(f32x4 (&s)[kGroups][QB], const float (&m)[QB], const float c) {
+#pragma clang fp contract(off)
+  const float inverse = 1.f / c;
+#pragma unroll
+  for (int kb = 0; kb < kGroups; ++kb)
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float left = s[kb][qb][j] * c - m[qb];
+        s[kb][qb][j] = fabsf(m[qb]) >= kFar ? left * inverse : s[kb][qb][j];
+      }
+}
+
 // Online softmax of a wavefront's tile.  s: scores; on return p is the second product's operand.
+// An exponent is c s - m in one rounding, against a reference m that is itself a rounded c s.  All weights of a row share the factor that this makes, 2^(2^-24 |m|)
+// at the most, which leaves fp32's range where |m| is far beyond 2^30 (scores of hundreds of millions).  From there on c s is rounded first: neighbours are 64
+// apart or more then, so the largest score's weight is one and the others' are none beside it.
 template <int QB, int CB>
 __device__ __forceinline__ void take_tile(f32x4 (&s)[kGroups][QB], bf16x8 (&p)[kGroups / 2][QB], float (&m)[QB], float (&l)[QB],
                                           f32x4 (&o)[CB][QB], const float c) {
   float sum[QB];
-  auto exponentials = [&]() {
+  auto exponentials = [&](const float (&reference)[QB]) {
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       sum[qb] = 0.f;
@@ -181,7 +201,7 @@ __device__ __forceinline__ void take_tile(f32x4 (&s)[kGroups][QB], bf16x8 (&p)[k
       for (int ks = 0; ks < kGroups / 2; ++ks) {
         f32x8 e;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * ks + j / 4][qb][j % 4], c, -m[qb]));
+        for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * ks + j / 4][qb][j % 4], c, -reference[qb]));
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum[qb] += e[j];
         // rounded here, not where they are used: eight fewer registers for every eight weights while the scores are still needed
@@ -191,10 +211,10 @@ __device__ __forceinline__ void take_tile(f32x4 (&s)[kGroups][QB], bf16x8 (&p)[k
       }
     }
   };
-  exponentials();
+  exponentials(m);
   bool over = false;
 #pragma unroll
-  for (int qb = 0; qb < QB; ++qb) over |= sum[qb] > kLazySum;
+  for (int qb = 0; qb < QB; ++qb) over |= sum[qb] > kLazySum || fabsf(m[qb]) >= kFar;
   if (__builtin_amdgcn_ballot_w64(over)) {
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
@@ -210,7 +230,15 @@ __device__ __forceinline__ void take_tile(f32x4 (&s)[kGroups][QB], bf16x8 (&p)[k
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) o[cb][qb] *= f;
     }
-    exponentials();
+    float reference[QB];
+    bool far = false;
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      reference[qb] = fabsf(m[qb]) >= kFar ? 0.f : m[qb];
+      far |= fabsf(m[qb]) >= kFar;
+    }
+    if (__builtin_amdgcn_ballot_w64(far)) far_scores<QB>(s, m, c);
+    exponentials(reference);
   }
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) l[qb] += sum[qb];
