@@ -169,6 +169,9 @@ __device__ __forceinline__ int key_piece(int row, int piece) {
   return row * (2 * D) + ((piece ^ (D == 128 ? row & 15 : (row >> 1) & 7)) << 4);
 }
 
+// (A row that has seen nothing yet is none: whatever it sees makes a new reference.)
+__device__ __forceinline__ bool far_reference(float m) { return fabsf(m) >= kFar && m != kLowest; }
+
 // Scores of rows with a far reference as what is left of them against it.
 template <int QB>
 __device__ __forceinline__ void far_scores(f32x4 (&s)[kGroups][QB], const float (&m)[QB], const float c) {
@@ -181,7 +184,7 @@ __device__ __forceinline__ void far_scores(f32x4 (&s)[kGroups][QB], const float 
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const float left = s[kb][qb][j] * c - m[qb];
-        s[kb][qb][j] = fabsf(m[qb]) >= kFar ? left * inverse : s[kb][qb][j];
+        s[kb][qb][j] = far_reference(m[qb]) ? left * inverse : s[kb][qb][j];
       }
 }
 
@@ -189,9 +192,10 @@ __device__ __forceinline__ void far_scores(f32x4 (&s)[kGroups][QB], const float 
 // An exponent is c s - m in one rounding, against a reference m that is itself a rounded c s.  All weights of a row share the factor that this makes, 2^(2^-24 |m|)
 // at the most, which leaves fp32's range where |m| is far beyond 2^30 (scores of hundreds of millions).  From there on c s is rounded first: neighbours are 64
 // apart or more then, so the largest score's weight is one and the others' are none beside it.
+// far_lanes: the wavefront's lanes of such rows.  (A comparison for each row and tile instead: 40 x 4680 rows over 32760 keys 2.78 -> 2.81 ms.)
 template <int QB, int CB>
 __device__ __forceinline__ void take_tile(f32x4 (&s)[kGroups][QB], bf16x8 (&p)[kGroups / 2][QB], float (&m)[QB], float (&l)[QB],
-                                          f32x4 (&o)[CB][QB], const float c) {
+                                          f32x4 (&o)[CB][QB], const float c, unsigned long long& far_lanes) {
   float sum[QB];
   auto exponentials = [&](const float (&reference)[QB]) {
 #pragma unroll
@@ -214,8 +218,8 @@ __device__ __forceinline__ void take_tile(f32x4 (&s)[kGroups][QB], bf16x8 (&p)[k
   exponentials(m);
   bool over = false;
 #pragma unroll
-  for (int qb = 0; qb < QB; ++qb) over |= sum[qb] > kLazySum || fabsf(m[qb]) >= kFar;
-  if (__builtin_amdgcn_ballot_w64(over)) {
+  for (int qb = 0; qb < QB; ++qb) over |= sum[qb] > kLazySum;
+  if (far_lanes | __builtin_amdgcn_ballot_w64(over)) {
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       float top = s[0][qb][0];
@@ -234,10 +238,12 @@ __device__ __forceinline__ void take_tile(f32x4 (&s)[kGroups][QB], bf16x8 (&p)[k
     bool far = false;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
-      reference[qb] = fabsf(m[qb]) >= kFar ? 0.f : m[qb];
-      far |= fabsf(m[qb]) >= kFar;
+      reference[qb] = far_reference(m[qb]) ? 0.f : m[qb];
+      far |= far_reference(m[qb]);
     }
-    if (__builtin_amdgcn_ballot_w64(far)) far_scores<QB>(s, m, c);
+    far_lanes = __builtin_amdgcn_ballot_w64(far);
+    asm volatile("" : "+s"(far_lanes));                  // (known to be none, the compiler would double the exponentials, and spill)
+    if (far_lanes) far_scores<QB>(s, m, c);
     exponentials(reference);
   }
 #pragma unroll
@@ -446,6 +452,7 @@ __global__ __launch_bounds__(64 * kWaves, rows_waves(D, QB)) void kv4_rows_kerne
     m[qb] = kLowest;
     l[qb] = 0.f;
   }
+  unsigned long long far_lanes = 0;
   unsigned char* const own = lds + wave * OWN;
   int v_off[CB];
 #pragma unroll
@@ -491,7 +498,7 @@ __global__ __launch_bounds__(64 * kWaves, rows_waves(D, QB)) void kv4_rows_kerne
     const bool whole = key0 + kTile <= lo.end && (key0 >= hi.begin || key0 + kTile <= sink) && !missing;
     if (!whole) mask_tile<QB>(sc, Seen<QB>(a, s, m0).v, sink, key0, missing, g);
     bf16x8 p[kGroups / 2][QB];
-    take_tile<QB, CB>(sc, p, m, l, o, a.scale_log2);
+    take_tile<QB, CB>(sc, p, m, l, o, a.scale_log2, far_lanes);
     // values that are not finite, and those that nobody sees, which may be anything
     unsigned long long odd[LOADS];
     bool any_odd = false;
@@ -685,6 +692,7 @@ __device__ __forceinline__ void attend_tile(const Kv4AttnArgs& a, TileLds<D>& sh
     m[qb] = kLowest;
     l[qb] = 0.f;
   }
+  unsigned long long far_lanes = 0;
 
   // ---- staging: a wavefront has 16 keys of a tile, which are in one page; four threads a key
   struct Raw {
@@ -852,7 +860,7 @@ __device__ __forceinline__ void attend_tile(const Kv4AttnArgs& a, TileLds<D>& sh
         const bool whole = key0 + kTile <= wlo.end && (key0 >= whi.begin || key0 + kTile <= sink) && !gone;
         if (!whole) mask_tile<QB>(sc, Seen<QB>(a, s, wm0).v, sink, key0, gone, g);
         bf16x8 p[kGroups / 2][QB];
-        take_tile<QB, CB>(sc, p, m, l, o, a.scale_log2);
+        take_tile<QB, CB>(sc, p, m, l, o, a.scale_log2, far_lanes);
         __builtin_amdgcn_s_setprio(1);
         if constexpr (SKEWED) scores(buffer ^ 1, std::true_type{}, buffer);
 #pragma unroll
