@@ -144,3 +144,41 @@ def test_a_window_moves_and_its_pages_come_back():
     wanted.zero_()
     S.svg_kv4_resize(cache, lengths, wanted, f, c, lengths, c, slots, frame, status)
     assert status.item() == S.SVG_KV4_OK and c.item() == pages and sorted(f.tolist()) == list(range(pages))
+
+
+def test_a_captured_call_on_tables_with_holes():
+    """Replayed with the caller's own edits between the replays, every one against the lists walked by hand."""
+    rng, n, ps, chunk = np.random.default_rng(8), 40, 16, 90
+    table, held, wanted, free, count = state(rng, n, ps, 300, chunk, 0.4, 400)
+    count = punch(rng, table, held, free, count, ps, 0.3)
+    t, f, lengths, c, w, status = dev(table), dev(free), dev(held), dev([count]), dev(wanted), dev([-9])
+    slots = torch.zeros(n, chunk, dtype=torch.int64, device="cuda")
+    cache = S.kv4_cache(n, len(free), table.shape[1], 1, 64, ps, page_table=t)
+    before = [x.clone() for x in (t, f, lengths, c)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    call = lambda: S.svg_kv4_resize(cache, lengths, w, f, c, lengths, c, slots, chunk, status)  # noqa: E731
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        call()
+    for x, y in zip((t, f, lengths, c), before):
+        x.copy_(y)
+    seen = set()
+    for _ in range(8):
+        graph.replay()
+        scratch = torch.randn(1 << 18, device="cuda").sum()               # eager work of our own between the replays
+        torch.cuda.synchronize()
+        assert torch.isfinite(scratch)
+        ref = O.resize(table, held, wanted, free, count, ps, chunk)
+        seen.add(ref[5])
+        for name, got, want in zip(("table", "free", "lengths", "count", "slots", "status"), (t, f, lengths, c, slots, status), ref):
+            assert np.array_equal(got.cpu().numpy().reshape(np.shape(want)), want), name
+        table, free, held, count = ref[:4]
+        count = punch(rng, table, held, free, count, ps, 0.1)
+        wanted = np.clip(held + rng.integers(-200, chunk + 1, n), 0, table.shape[1] * ps)
+        for x, y in ((t, table), (f, free), (w, wanted), (c, [count])):
+            x.copy_(dev(y))
+    assert O.OK in seen
