@@ -519,7 +519,7 @@ int svg_fp4_linear_quantize(int64_t M, int64_t N, int64_t K, const void* a, cons
  * Few rows of activations (a timestep's embedding, the newest token of a sequence) times weights kept in 4 bits:
  *     out[m, n] = act(sum_k in_act(x[m, k]) w[n, k] + bias[n])        m < M, n < N, k < K
  * as svg_fp4_linear, but the activations stay as they are: x is a token matrix of B*N = M rows and H*D = K columns, in_act is taken in
- * fp32 and not rounded, and every product is exact in the accumulation's fp32.  w, w_scales: an operand [N, K] (svg_fp4_quantize).  out: a token
+ * fp32 and not rounded, and every product is exact in the accumulation's fp32 (but for an activation's bits below 2^-133).  w, w_scales: an operand [N, K] (svg_fp4_quantize).  out: a token
  * matrix of M rows and N columns, which must not overlap an input (SVG_ERR_ALIAS).  M <= 1024; made for up to 16 rows (every further
  * 16 read the weights once more).  An infinite or NaN activation makes its row NaN or infinite.  K >= 1, N >= 1; results repeat bit for bit and do not
  * depend on the other rows of the call.
@@ -616,7 +616,8 @@ typedef struct svg_kv4_attn {
  * Rows of o and lse from q_len[b] on are left as they were.  Scores are fp32 sums of exact products, of any size that times scale / log 2 is finite
  * in fp32; the weights are rounded to bf16 for the second product, sums are fp32.  Results repeat bit for bit.
  * workspace: >= svg_kv4_attn_workspace_bytes(cache, attn, q_desc) bytes, 16-byte aligned (0: may be NULL).
- * Overlaps of o, lse or the workspace with each other or an input: SVG_ERR_ALIAS.
+ * Overlaps of o, lse or the workspace with each other or an input: SVG_ERR_ALIAS.  Calls of 2^24 workgroups and more (heads of the cache times row tiles of
+ * 16, 32 or 128 rows of a head times sequences, or parts of them): SVG_ERR_UNSUPPORTED.
  */
 size_t svg_kv4_attn_workspace_bytes(const svg_kv4_t* cache, const svg_kv4_attn_t* attn, const svg_tokens_t* q_desc);
 int svg_kv4_attn_fwd(const svg_kv4_t* cache, const svg_kv4_attn_t* attn, const svg_tokens_t* q_desc, const void* q,

@@ -42,7 +42,7 @@ struct Kv4Plan {
   int tile;              // rows of a workgroup: 16 or 32 (its wavefronts share the rows and split the keys) or 128 (32 rows a wavefront)
   int tiles;             // row tiles of a head of a sequence
   int parts;             // parts that the keys of all sequences are cut into, one each at least
-  int reach;             // keys that a row tile sees at the most
+  int reach;             // an estimate of the keys that a row tile visits: for dealing the parts only
 };
 Kv4Plan kv4_plan(const Kv4& c, const svg_kv4_attn_t& attn, long long N, int group);
 size_t kv4_workspace_bytes(const Kv4& c, const Kv4Plan& plan);

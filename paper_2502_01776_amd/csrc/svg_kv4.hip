@@ -313,8 +313,8 @@ __global__ __launch_bounds__(kThreads) void resize_state_kernel(ResizeArgs a) {
 //
 // A lane takes eight neighbouring elements of a row of keys and the same of values: D / 8 lanes a row, four of them a block of 32, whose largest
 // magnitude needs two lane moves.  Bound: HBM (2 or 4 bytes an element in, 17/32 out; the other way round on the way back).  One row of each to a thread, and
-// results past the caches: 40 heads of 4680 x 128 in bf16 written and read 45.8 us, 4.2 TB/s, a large copy 4.7; two rows to a thread 57.5, 48.6 with the
-// stores alone changed, 52.5 with the rows alone; four rows 58.7.
+// results past the caches: 40 heads of 4680 x 128 in bf16 written 22.5 us and read 18-19, 121 MB each, 5.4 and 6.3-6.7 TB/s (more than a large copy's 4.7-4.9: the
+// caches hold part of it), 45.9 us as two calls; two rows to a thread 57.5, 48.6 with the stores alone changed, 52.5 with the rows alone; four rows 58.7.
 
 struct RowsArgs {
   Kv4 c;

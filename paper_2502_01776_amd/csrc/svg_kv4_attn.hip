@@ -15,10 +15,10 @@
 // Two forms:
 //  * 16 or 32 query rows: the wavefronts of a workgroup share them and split the keys, every one with its own tiles, straight
 //    from memory into registers one tile ahead; no barrier before the results are merged through LDS.  Bound: HBM: one token of eight sequences over
-//    up to 65536, 32 heads on 8 of 128 channels, 65 us with the join, 4.9 TB/s (a large copy 4.7).
+//    up to 65536, 32 heads on 8 of 128 channels, 312 MB of cache: 61 us under the profiler, and 5 for the join; 68-74 in a graph, 4.2-4.6 TB/s (a large copy 4.7-4.9).
 //  * 128 rows, 32 a wavefront: a tile of keys and values is dequantised once for all, a quarter by each wavefront, into LDS.  Bound: the matrix and the
-//    vector unit in turns.  40 heads of 4680 rows and 128 channels over 32760 keys 2.74-2.79 ms, 1.07-1.09 PFLOP/s (matrix cores busy 44 % of the cycles, vector
-//    instructions 48 %, workgroups on 94 % of the places); 48 heads of 4050 rows and 64 channels in a window of seven frames 680 us, 0.79 PFLOP/s (31, 57
+//    vector unit in turns.  40 heads of 4680 rows and 128 channels over 32760 keys 2.78-2.83 ms, 1.06-1.07 PFLOP/s (matrix cores busy 44 % of the cycles, vector
+//    instructions 48 %, workgroups on 94 % of the places); 48 heads of 4050 rows and 64 channels in a window of seven frames 690-740 us, 0.73-0.78 PFLOP/s (31, 57
 //    and 87 %: two equal rounds of workgroups, of which those across two frames take a quarter longer).
 // Few workgroups for the chip: the keys are cut into parts for several, whose results a second launch joins.
 #include <algorithm>
@@ -60,7 +60,7 @@ struct Kv4AttnArgs {
   float2* stats;
   int N, group, rows, tiles;
   int parts;                 // of all sequences together
-  int reach;                 // keys that a row tile sees at the most
+  int reach;                 // an estimate of the keys that a row tile visits: parts are dealt by it, no result depends on it
   int causal, block, window, sink, capacity;
   float scale_log2;
 };
@@ -634,7 +634,8 @@ struct PageList {
 // The loop is skewed by one tile, as in svg_attn_kernel.h: with the scores of tile j in registers a wavefront takes their exponentials and then issues
 // the products of tile j + 1's scores and of tile j's output as one batch; the first operands of a batch are read in front of the exponentials, every
 // other one behind the products.  Keys of tile j + 2 and values of j + 1 are dequantised into LDS meanwhile, those behind them are on their way
-// from memory; one barrier a tile.  Without the wavefront's priority over its batch +4 %, with batches that the compiler may reorder +8 %.
+// from memory; one barrier a tile.  At D = 128 (40 x 4680 rows over 32760 keys, three runs each in turn) 2.80-2.81 ms; with batches that the compiler may
+// reorder 3.02; without the wavefront's priority over its batch the same, at D = 64 (48 x 4050 rows in a window) 750-775 us for 716-765.
 template <int D>
 struct TileLds {
   static constexpr int HALF = kTile * 2 * D;             // a tile of keys, or of values
@@ -650,10 +651,10 @@ __device__ __forceinline__ void attend_tile(const Kv4AttnArgs& a, TileLds<D>& sh
   constexpr int WORDS = D / 32;                          // words of codes that a thread stages of a tile's keys, and of its values
   constexpr int HALF = TileLds<D>::HALF;
   constexpr int NS = kGroups * DS, NV = kGroups / 2 * CB; // operands of the two products
-  // Of them in registers: at D = 128 (40 x 4680 rows over 32760 keys) 4 ahead 3.26 ms, 8 3.17, 12 3.22; at D = 64 2 and 4 alike.
+  // Of them in registers, measured on the calls above: at D = 128 4 and 8 ahead alike, 12 2.86-2.90 ms; at D = 64 2 and 4 alike, 8 845-865 us.
   constexpr int AHEAD = D == 128 ? 8 : 4;
-  // At D = 128 3.15 ms where one tile after the other takes 3.56; at D = 64, where three wavefronts to a SIMD overlap by themselves, 893 us and 890-899.
-  // (Both taken before masks were kept from rows that do not exist.)
+  // At D = 128 2.80-2.81 ms where one tile after the other takes 2.88-2.90; at D = 64 733-751 us skewed (with 8 ahead 919, two wavefronts to a SIMD 822) and
+  // 716-765 not: alike, so the shorter program.
   constexpr bool SKEWED = D == 128;
   unsigned char* const lds = shared.tiles;
   auto& odd_values = shared.odd_values;
@@ -988,7 +989,7 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a) {
 //     begin + begin_more c + t (turn + turn_more c)       microseconds,
 // the last round of workgroups counted by its own c, and for parts the launch that joins them, 4.5 and what they take to write and read at 5 TB/s.
 // Fitted to the times of 276 calls with 1 to 64 heads of 1 to 1000 rows over 300 to 60000 keys, each cut in up to eight ways: the way
-// taken is within 15 % of the best of those measured, 2 % on the average.  Measured, chosen way and its neighbours: 4 x 64 rows of 64 channels over 272 keys 7.2 us
+// taken is within 15 % of the best of these ways, 2 % on the average (which says nothing of how far all of them are from a floor).  Measured, chosen way and its neighbours: 4 x 64 rows of 64 channels over 272 keys 7.2 us
 // in tiles of 16 rows, 8.8 of 32; 24 x 48 of 128 over 20000 42 and 39; 24 x 226 of 128 over 12000 61 in tiles of 128, 81 of 32; 40 x 800 of 64 over 12000, which
 // are 280 tiles of 128 for 768 places, 164 in tiles of 32, 185 of 128.  8 x 64 of 128 over 1000 keys 12.3 in four parts, 13.2 in one; 24 x 48 14.9 and 13.3.
 struct FormTimes {
@@ -1003,7 +1004,7 @@ constexpr int kUnits = 256;                   // compute units
 Kv4Plan kv4_plan(const Kv4& c, const svg_kv4_attn_t& attn, long long N, int group) {
   Kv4Plan p = {};
   p.rows = (int)(N * group);
-  // keys that a row tile may have to visit
+  // keys that a row tile visits, about (one across two blocks visits up to a block more)
   const long long capacity = (long long)c.max_pages << c.page_log2;
   long long keys = attn.max_kv > 0 ? std::min<long long>(attn.max_kv, capacity) : capacity;
   if (attn.window >= 0 && attn.causal) keys = std::min(keys, (attn.window + 1ll) * attn.block + std::min<long long>(attn.sink, keys) + 128);
@@ -1036,7 +1037,9 @@ Kv4Plan kv4_plan(const Kv4& c, const svg_kv4_attn_t& attn, long long N, int grou
     // (32 rows for 16, or 128 for 64 and fewer, are never faster)
     if ((rows == 32 && p.rows <= 16) || (rows == 128 && p.rows <= 64)) continue;
     const long long each = (long long)c.H * std::max(1, (p.rows + rows - 1) / rows);
-    // (with more the form with 128 rows is faster: 48 x 4050 of 64 channels 681 us and 801)
+    // Beyond the calls that the times were fitted to (several sequences, whole rounds of workgroups) the form with more rows.  90 calls of 3 to 64 sequences of 33 to
+    // 581 rows that this decides, both ways: the estimate's own choice takes 1.02 times as long on the geometric average, 0.64 to 1.35 (128 rows for 32: D = 64 0.98,
+    // D = 128 1.05; 32 for 16: 1.02 and 0.99).
     if ((rows == 16 && p.rows > 16 && each * c.B > 4 * kUnits) || (rows == 32 && p.rows > 64 && each * c.B > 5 * kUnits)) continue;
     consider(form, rows, c.B);
     // parts for one, two or three workgroups to a compute unit, of a turn (128 rows: 8 tiles) at least
