@@ -616,7 +616,7 @@ typedef struct svg_kv4_attn {
  * Rows of o and lse from q_len[b] on are left as they were.  Scores are fp32 sums of exact products, of any size that times scale / log 2 is finite
  * in fp32; the weights are rounded to bf16 for the second product, sums are fp32.  Results repeat bit for bit.
  * workspace: >= svg_kv4_attn_workspace_bytes(cache, attn, q_desc) bytes, 16-byte aligned (0: may be NULL).
- * Overlaps of o, lse or the workspace with each other or an input: SVG_ERR_ALIAS.  Calls of 2^24 workgroups and more (heads of the cache times row tiles of
+ * Overlaps of o, lse or the workspace with each other or an input: SVG_ERR_ALIAS.  Calls of more than 2^24 - 8 workgroups (heads of the cache times row tiles of
  * 16, 32 or 128 rows of a head times sequences, or parts of them): SVG_ERR_UNSUPPORTED.
  */
 size_t svg_kv4_attn_workspace_bytes(const svg_kv4_t* cache, const svg_kv4_attn_t* attn, const svg_tokens_t* q_desc);

@@ -232,3 +232,11 @@ def test_how_a_call_is_cut():
             for B in (1, 7, 64, 65, 600):
                 for D in (64, 128):
                     plan(N=N, B=B, H=H, D=D)
+
+
+def test_calls_of_too_many_workgroups_are_refused():
+    """One query of every head of 65536 sequences: 2^24 workgroups."""
+    c, t = cache(sequences=65536, heads=256, head_dim=64), tokens(B=65536, N=1, H=256, D=64)
+    far = 1 << 44                                                     # (results that long overlap nothing)
+    assert kv4_plan.plan(c, S.kv4_attn(kv_len=LEN), 1, 1).parts == 65536
+    assert attn(c, qt=t, ot=t, q=far, o=2 * far, lse=3 * far) == -2
